@@ -300,6 +300,69 @@ int hata_prefill_write_paged(hata_ctx* ctx, const void* K_new, const void* V_new
                              uint32_t* codes_pool, const int32_t* block_table, int32_t max_blocks,
                              int32_t page_rows, int32_t n_pages, const float* W_H, void* stream);
 
+/*
+ * Serving from a paged cache: pages are handed out, packed rows written and dense layers attended without the host, in
+ * the layout above.
+ *
+ * Slots.  Row r of page p is slot p * page_rows + r.  A slot map names, for every row of a packed batch (the new tokens of all
+ * sequences, one sequence behind the other, no padding between them), the slot that the row goes to; -1: nowhere.
+ *
+ * hata_plan_pages: block tables and slot map from request lengths.
+ *   len_now, len_next [B]   rows that sequence b has in the cache and is to have: more (new tokens), fewer (a request
+ *                           that ended, 0, or was set back; its pages become free), or as many
+ *   fork_from   [B] or NULL >= 0: sequence b begins as a copy of that sequence's first len_now[b] rows, whose pages it
+ *                           shares: their entries of the block table are copied.  Whole pages (len_now[b] a multiple of page_rows),
+ *                           which the source keeps (page_rows * whole pages of min(len_now, len_next) of the source), from a
+ *                           source that is not itself forked in this call; len_next[b] >= len_now[b].  -1: no fork
+ *   shared_blocks [B] or NULL  leading blocks of sequence b whose pages are not its own: never released
+ *   block_table [B, max_blocks]  read and written: entries of new blocks and of forks; nothing else
+ *   free_pages  [n_pages]   the free pages are free_pages[0 .. n_free[0]), the last one is taken first; read and
+ *                           written: pages released in this call are put behind them, in the order of sequences and blocks, and
+ *                           taken in the same call already
+ *   n_free, n_free_out [1]  their number before and after the call (may be the same address)
+ *   seq_len     [B]         output: len_next[b] where the request was granted, else len_now[b] (0 for a fork); may be
+ *                           len_now or len_next
+ *   token_start [B + 1] or NULL  output: the packed rows of sequence b are token_start[b] .. token_start[b + 1] - 1, whether
+ *                           granted or not; values above max_tokens are given as max_tokens
+ *   slots       [max_tokens]  output, all of it: the slot map; -1 for rows of requests not granted and behind the last
+ *   positions   [max_tokens] or NULL  output, the same way: the row's number in its sequence
+ * Requests are granted in order.  One that is not valid (a length below 0 or above min(L_cap, max_blocks * page_rows), a fork that
+ * breaks a rule above, packed rows that end behind max_tokens) is not granted and takes nothing; from the first one on for
+ * which too few pages are left, no request that needs a page is granted.  max_tokens: host value, 0 .. 2^23 (0: slots may be
+ * NULL); B <= 8191, else HATA_EUNSUPPORTED.  Page numbers are clamped to [0, n_pages) as everywhere.  Outputs must not overlap
+ * each other or an input, but for what is named above.  One launch; may be captured.
+ */
+int hata_plan_pages(hata_ctx* ctx, const int32_t* len_now, const int32_t* len_next, int32_t B, const int32_t* fork_from,
+                    const int32_t* shared_blocks, int32_t* block_table, int32_t max_blocks, int32_t page_rows, int32_t n_pages,
+                    int32_t* free_pages, const int32_t* n_free, int32_t* n_free_out, int32_t* seq_len, int32_t* token_start,
+                    int32_t* slots, int32_t* positions, int32_t max_tokens, void* stream);
+
+/* Packed rows into pages, through a slot map, with their key codes:
+ *   K_pool, V_pool [slot] = K_new, V_new [t, h],  codes_pool [slot] = BitPack(Sign(K_new[t, h] . W_H[h])),  slot = slots[t],
+ * for 0 <= t < n_tokens and every KV head h.  K_new, V_new: row (t, h) starts at t * stride_t + h * stride_h elements (the
+ * same strides for both, e.g. those of the columns of a fused projection's output; multiples of 8, not negative), its d
+ * values contiguous.  Rows whose slot is negative or not in the pools go nowhere; rows of the pools that no slot names are
+ * left as they are.  No two rows may have the same slot.  codes_pool and W_H both NULL: no codes (the cache of a dense
+ * layer; a row that hata_decode_step_paged appends).  Any r.  The codes are those of an evaluation in fp64, whatever the
+ * number of rows: equal to what hata_decode_step appends.  (hata_prepare_weights of the same W_H makes calls with many rows
+ * faster.)  n_tokens is not bounded by L_cap or B_max. */
+int hata_write_slots(hata_ctx* ctx, const void* K_new, const void* V_new, int64_t stride_t, int64_t stride_h, const int32_t* slots,
+                     int32_t n_tokens, void* K_pool, void* V_pool, uint32_t* codes_pool, int32_t page_rows, int32_t n_pages,
+                     const float* W_H, void* stream);
+
+/* hata_dense_decode on the paged layout, where the first rows of some sequences are the same pages (a system prompt, a
+ * document, samples of one prompt): those are read once for all of them.
+ *   group_start [n_groups + 1], shared_len [n_groups] (device; may be NULL with n_groups = 0): the sequences group_start[g] ..
+ *   group_start[g + 1] - 1 have the same pages in their block tables over rows 0 .. shared_len[g] - 1.
+ * Every sequence attends over its rows 0 .. seq_len[b] - 1 as in hata_dense_decode, the groups decide only how often
+ * rows are read: shared_len is clamped to the shortest sequence of the group that has rows at all (sequences without rows
+ * give zeros and do not count), sequences outside every group share nothing.  group_start is ascending; entries are
+ * clamped to [the entry before, B].  0 <= n_groups <= B.  Needs no residency and no waits. */
+int hata_dense_decode_paged(hata_ctx* ctx, const void* q, const void* K_pool, const void* V_pool, const int32_t* block_table,
+                            int32_t max_blocks, int32_t page_rows, int32_t n_pages, const int32_t* seq_len, int32_t B,
+                            const int32_t* group_start, const int32_t* shared_len, int32_t n_groups, float sm_scale, void* out,
+                            float* out_f32, void* stream);
+
 /* Host-side query of how hata_decode_step() runs a batch of B sequences; nothing is enqueued.
  * *n_launches: 1 (single-launch form) or 3 (the form without in-kernel waits, also where its first two launches go as one: see
  * hata_decode_step); *chunk: cached keys per scoring workgroup for a batch of this size (the launch that encodes and scores may give one up

@@ -42,7 +42,7 @@ inline size_t align_up(size_t v) { return (v + kAlign - 1) / kAlign * kAlign; }
 struct Plan {
     int G, Wd, NB, NBP, chunk, n_chunks, coop_chunk, HT, sparse_rows, sparse_splits;
     int64_t dense_wgs_max;
-    size_t off_qcodes, off_scores, off_idx, off_hist, off_cinfo, off_uinfo, off_ucnt, off_acnt, off_cum, off_epoch, off_qrec, off_err, off_uhist, off_partials, off_wplanes, total;
+    size_t off_qcodes, off_scores, off_idx, off_hist, off_cinfo, off_uinfo, off_ucnt, off_acnt, off_cum, off_epoch, off_qrec, off_err, off_plan, off_uhist, off_partials, off_wplanes, total;
 };
 
 int validate_config(const hata_config* f) {
@@ -134,6 +134,7 @@ int make_plan(const hata_config* f, const hata_tuning* t, Plan* p) {
     p->off_epoch = o;    o = align_up(o + (size_t)units * HATA_COUNTER_STRIDE * 4);
     p->off_qrec = o;     o = align_up(o + (size_t)f->B_max * f->Hq * p->Wd * p->n_chunks * 8);
     p->off_err = o;      o = align_up(o + 4);
+    p->off_plan = o;     o = align_up(o + 4);
     p->off_uhist = o;    o = align_up(o + (size_t)units * p->NB * 4);
     size_t n_partials = (size_t)f->B_max * f->Hq * max_splits;
     const size_t dense_partials = (size_t)256 * HATA_DENSE_ROUNDS * G;  // a workgroup has one per head of its group
@@ -224,16 +225,25 @@ inline bool takes_unit_step(const hata_ctx* c, int B, bool paged = false) {
 }
 inline bool aligned(const void* p, size_t a) { return ((uintptr_t)p % a) == 0; }
 
+// Validates the shape of the pools; *shift: log2 of page_rows.
+inline int check_pools(const hata_ctx* c, int32_t page_rows, int32_t n_pages, int* shift) {
+    if (n_pages < 1) return HATA_EINVAL;
+    if (page_rows < 16 || page_rows > (1 << 20) || (page_rows & (page_rows - 1)) != 0) return HATA_EINVAL;
+    // rows of the pools are indexed with 32-bit integers on the device
+    if ((int64_t)n_pages * c->cfg.Hkv * page_rows > 0x7fffffffll) return HATA_EINVAL;
+    *shift = 0;
+    while ((1 << *shift) < page_rows) ++*shift;
+    return HATA_OK;
+}
+
 // Validates a block-table description and fills the view the launchers take.
 inline int make_page_view(const hata_ctx* c, const int32_t* block_table, int32_t max_blocks,
                           int32_t page_rows, int32_t n_pages, hata::PageView* pv) {
-    if (!block_table || max_blocks < 1 || n_pages < 1) return HATA_EINVAL;
-    if (page_rows < 16 || page_rows > (1 << 20) || (page_rows & (page_rows - 1)) != 0) return HATA_EINVAL;
-    if ((int64_t)max_blocks * page_rows > (1ll << 30)) return HATA_EINVAL;
-    // rows of the pools are indexed with 32-bit integers on the device
-    if ((int64_t)n_pages * c->cfg.Hkv * page_rows > 0x7fffffffll) return HATA_EINVAL;
+    if (!block_table || max_blocks < 1) return HATA_EINVAL;
     int shift = 0;
-    while ((1 << shift) < page_rows) ++shift;
+    const int rc = check_pools(c, page_rows, n_pages, &shift);
+    if (rc != HATA_OK) return rc;
+    if ((int64_t)max_blocks * page_rows > (1ll << 30)) return HATA_EINVAL;
     pv->table = block_table; pv->max_blocks = max_blocks; pv->shift = shift; pv->n_pages = n_pages;
     return HATA_OK;
 }
@@ -298,6 +308,7 @@ int hata_create_tuned(hata_ctx** ctx_out, const hata_config* cfg, const hata_tun
     c->unit_epoch = (uint32_t*)(w + p.off_epoch);
     c->coop_qrec = (unsigned long long*)(w + p.off_qrec);
     c->error_word = (uint32_t*)(w + p.off_err);
+    c->plan_counter = (uint32_t*)(w + p.off_plan);
     c->coop_opts = 0;
     c->partials = (float*)(w + p.off_partials);
     c->wplanes = (f_has_mfma_width(cfg->r)) ? (void*)(w + p.off_wplanes) : nullptr;
@@ -308,7 +319,8 @@ int hata_create_tuned(hata_ctx** ctx_out, const hata_config* cfg, const hata_tun
         delete c;
         return HATA_EHIP;
     }
-    if (hata::prepare_topk() != hipSuccess || hata::prepare_attention(c) != hipSuccess || hata::prepare_dense() != hipSuccess) {
+    if (hata::prepare_topk() != hipSuccess || hata::prepare_attention(c) != hipSuccess || hata::prepare_dense() != hipSuccess ||
+        hata::prepare_pages() != hipSuccess) {
         delete c;
         return HATA_EHIP;
     }
@@ -625,6 +637,63 @@ int hata_decode_step_paged(hata_ctx* ctx, const void* q, const void* K_pool, con
     }
     if (e == hipErrorNotSupported) return HATA_EUNSUPPORTED;
     return hip_rc(e);
+}
+
+int hata_plan_pages(hata_ctx* ctx, const int32_t* len_now, const int32_t* len_next, int32_t B, const int32_t* fork_from,
+                    const int32_t* shared_blocks, int32_t* block_table, int32_t max_blocks, int32_t page_rows, int32_t n_pages,
+                    int32_t* free_pages, const int32_t* n_free, int32_t* n_free_out, int32_t* seq_len, int32_t* token_start,
+                    int32_t* slots, int32_t* positions, int32_t max_tokens, void* stream) {
+    int rc = check_call(ctx, B);
+    if (rc != HATA_OK) return rc;
+    if (!len_now || !len_next || !free_pages || !n_free || !n_free_out || !seq_len) return HATA_EINVAL;
+    if (max_tokens < 0 || max_tokens > (1 << 23) || (max_tokens > 0 && !slots)) return HATA_EINVAL;
+    for (const void* p : {(const void*)len_now, (const void*)len_next, (const void*)fork_from, (const void*)shared_blocks,
+                          (const void*)block_table, (const void*)free_pages, (const void*)n_free, (const void*)n_free_out,
+                          (const void*)seq_len, (const void*)token_start, (const void*)slots, (const void*)positions})
+        if (!aligned(p, 4)) return HATA_EINVAL;
+    hata::PageView pv;
+    rc = make_page_view(ctx, block_table, max_blocks, page_rows, n_pages, &pv);
+    if (rc != HATA_OK) return rc;
+    if (B > HATA_PLAN_MAX_B) return HATA_EUNSUPPORTED;
+    const int64_t cap = (int64_t)max_blocks * page_rows;
+    const hata::PagePlan p = {len_now, len_next, fork_from, shared_blocks, n_free, block_table, free_pages, n_free_out, seq_len,
+                              token_start, slots, positions, B, max_blocks, pv.shift, n_pages, max_tokens,
+                              cap < ctx->cfg.L_cap ? (int)cap : ctx->cfg.L_cap};
+    return hip_rc(hata::launch_plan_pages(ctx, p, (hipStream_t)stream));
+}
+
+int hata_write_slots(hata_ctx* ctx, const void* K_new, const void* V_new, int64_t stride_t, int64_t stride_h, const int32_t* slots,
+                     int32_t n_tokens, void* K_pool, void* V_pool, uint32_t* codes_pool, int32_t page_rows, int32_t n_pages,
+                     const float* W_H, void* stream) {
+    if (!ctx || n_tokens < 0) return HATA_EINVAL;
+    if (!K_new || !V_new || !slots || !K_pool || !V_pool || !codes_pool != !W_H) return HATA_EINVAL;
+    if (stride_t < 0 || stride_h < 0 || stride_t % 8 != 0 || stride_h % 8 != 0) return HATA_EINVAL;
+    if (!aligned(K_new, 16) || !aligned(V_new, 16) || !aligned(K_pool, 16) || !aligned(V_pool, 16) || !aligned(codes_pool, 16) ||
+        !aligned(W_H, 16) || !aligned(slots, 4))
+        return HATA_EINVAL;
+    int shift = 0;
+    const int rc = check_pools(ctx, page_rows, n_pages, &shift);
+    if (rc != HATA_OK) return rc;
+    if (n_tokens == 0) return HATA_OK;
+    return hip_rc(hata::launch_write_slots(ctx, K_new, V_new, stride_t, stride_h, slots, n_tokens, K_pool, V_pool, codes_pool, shift,
+                                           n_pages, W_H, (hipStream_t)stream));
+}
+
+int hata_dense_decode_paged(hata_ctx* ctx, const void* q, const void* K_pool, const void* V_pool, const int32_t* block_table,
+                            int32_t max_blocks, int32_t page_rows, int32_t n_pages, const int32_t* seq_len, int32_t B,
+                            const int32_t* group_start, const int32_t* shared_len, int32_t n_groups, float sm_scale, void* out,
+                            float* out_f32, void* stream) {
+    int rc = check_call(ctx, B);
+    if (rc != HATA_OK) return rc;
+    if (!q || !K_pool || !V_pool || !seq_len || !out) return HATA_EINVAL;
+    if (n_groups < 0 || n_groups > B || (n_groups > 0 && (!group_start || !shared_len))) return HATA_EINVAL;
+    if (!aligned(q, 16) || !aligned(K_pool, 16) || !aligned(V_pool, 16) || !aligned(out, 2) || !aligned(out_f32, 4) ||
+        !aligned(block_table, 4) || !aligned(seq_len, 4) || !aligned(group_start, 4) || !aligned(shared_len, 4))
+        return HATA_EINVAL;
+    hata::PageView pv;
+    rc = make_page_view(ctx, block_table, max_blocks, page_rows, n_pages, &pv);
+    if (rc != HATA_OK) return rc;
+    return hip_rc(hata::launch_dense(ctx, q, K_pool, V_pool, seq_len, B, sm_scale, out, out_f32, (hipStream_t)stream, &pv));
 }
 
 int hata_step_plan(const hata_ctx* ctx, int32_t B, int32_t* n_launches, int32_t* chunk, int32_t* n_chunks) {

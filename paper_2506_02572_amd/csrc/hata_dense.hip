@@ -45,6 +45,7 @@ struct DenseArgs {
     int Hq, Hkv, G, B, L_cap;
     int64_t sb, sh, sn;
     float scale_log2;
+    PageView pv;  // PAGED: the caches are pools of pages (sb, sh, sn are not used)
 };
 
 // two heads in the even and odd lanes: the neighbour's value
@@ -125,7 +126,9 @@ __device__ __forceinline__ bool dense_share(const int32_t* __restrict__ seq_len,
 }
 
 enum DenseForm { DENSE_BF16X2, DENSE_FP32_ONE_HEAD, DENSE_FP32_TWO_HEADS, DENSE_FP32 };
-template <DenseForm FORM>
+// PAGED: the rows lie in pools of pages.  A tile of 16 rows lies inside a page, so a wave looks up one page a tile, 64 tiles'
+// at a time (a lane each).
+template <DenseForm FORM, bool PAGED>
 __global__ __launch_bounds__(DENSE_WAVES * 64) void dense_kernel(const DenseArgs a) {
     // ring[wave][DENSE_RING][DENSE_TILE_BYTES]; afterwards the waves' states, the merge weights and sums
     extern __shared__ __attribute__((aligned(16))) char smem[];
@@ -156,24 +159,35 @@ __global__ __launch_bounds__(DENSE_WAVES * 64) void dense_kernel(const DenseArgs
     const int t_begin = (int)((int64_t)tiles * split / ns), t_end = (int)((int64_t)tiles * (split + 1) / ns);
     const int mine = max(0, (t_end - t_begin - wave + DENSE_WAVES - 1) / DENSE_WAVES);  // tiles t_begin + wave + 8 j
 
-    const uint16_t* Kb = a.K + b * a.sb + h * a.sh;
-    const uint16_t* Vb = a.V + b * a.sb + h * a.sh;
+    const uint16_t* Kb = PAGED ? a.K : a.K + b * a.sb + h * a.sh;
+    const uint16_t* Vb = PAGED ? a.V : a.V + b * a.sb + h * a.sh;
+    const int64_t sn = PAGED ? HATA_D : a.sn;
+    [[maybe_unused]] int page = 0;  // of tile 64 x + lane of this wave, x the last multiple that was requested
     char* ring = smem + wave * (DENSE_RING * DENSE_TILE_BYTES);
     const uint32_t ring_lds = __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)(__attribute__((address_space(3))) void*)ring);
     // request: lane l of instruction i fetches piece (l % 16) ^ swizzle(row) of row 4 i + l / 16
     int64_t off[4];
 #pragma unroll
-    for (int i = 0; i < 4; ++i) off[i] = (4 * i + kg) * a.sn + (n ^ dense_swizzle(4 * i + kg)) * 8;
+    for (int i = 0; i < 4; ++i) off[i] = (4 * i + kg) * sn + (n ^ dense_swizzle(4 * i + kg)) * 8;
     auto request = [&](int j) {
         const int row0 = (t_begin + wave + DENSE_WAVES * j) * 16;
-        const uint16_t* kt = Kb + row0 * a.sn;
-        const uint16_t* vt = Vb + row0 * a.sn;
+        int64_t at = row0 * sn;
+        if constexpr (PAGED) {
+            if (j % 64 == 0) {
+                const int n0 = min(row0 + lane * (16 * DENSE_WAVES), L - 1);
+                page = clampi(a.pv.table[(int64_t)b * a.pv.max_blocks + (n0 >> a.pv.shift)], 0, a.pv.n_pages - 1);
+            }
+            const int p = __builtin_amdgcn_readlane(page, j % 64);
+            at = ((((int64_t)p * a.Hkv + h) << a.pv.shift) + (row0 & ((1 << a.pv.shift) - 1))) * HATA_D;
+        }
+        const uint16_t* kt = Kb + at;
+        const uint16_t* vt = Vb + at;
         const uint32_t dst = ring_lds + (uint32_t)(j % DENSE_RING) * DENSE_TILE_BYTES;
         const int last = L - 1 - row0;  // rows past the end repeat the last one
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
             int64_t o = off[i];
-            if (last < 15 && 4 * i + kg > last) o += (int64_t)(last - 4 * i - kg) * a.sn;
+            if (last < 15 && 4 * i + kg > last) o += (int64_t)(last - 4 * i - kg) * sn;
             // (written as instructions: behind the compiler's builtin for it, every LDS read waits for all
             // requests outstanding.  nt: the rows are read once, and marked so they stream at 6.1 instead of
             // 5.35 TB/s, 131072 rows)
@@ -183,7 +197,7 @@ __global__ __launch_bounds__(DENSE_WAVES * 64) void dense_kernel(const DenseArgs
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
             int64_t o = off[i];
-            if (last < 15 && 4 * i + kg > last) o += (int64_t)(last - 4 * i - kg) * a.sn;
+            if (last < 15 && 4 * i + kg > last) o += (int64_t)(last - 4 * i - kg) * sn;
             asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off nt"
                          ::"s"(dst + 4096 + i * 1024), "v"(vt + o) : "memory", "m0");
         }
@@ -491,8 +505,10 @@ static int dense_splits(int64_t units, int L_cap) {
 }
 
 hipError_t prepare_dense() {  // (more than 64 KB of dynamic LDS has to be asked for)
-    for (const void* fn : {(const void*)dense_kernel<DENSE_BF16X2>, (const void*)dense_kernel<DENSE_FP32>,
-                           (const void*)dense_kernel<DENSE_FP32_ONE_HEAD>, (const void*)dense_kernel<DENSE_FP32_TWO_HEADS>}) {
+    for (const void* fn : {(const void*)dense_kernel<DENSE_BF16X2, false>, (const void*)dense_kernel<DENSE_FP32, false>,
+                           (const void*)dense_kernel<DENSE_FP32_ONE_HEAD, false>, (const void*)dense_kernel<DENSE_FP32_TWO_HEADS, false>,
+                           (const void*)dense_kernel<DENSE_BF16X2, true>, (const void*)dense_kernel<DENSE_FP32, true>,
+                           (const void*)dense_kernel<DENSE_FP32_ONE_HEAD, true>, (const void*)dense_kernel<DENSE_FP32_TWO_HEADS, true>}) {
         const hipError_t e = hipFuncSetAttribute(fn, hipFuncAttributeMaxDynamicSharedMemorySize, (int)dense_lds());
         if (e != hipSuccess) return e;
     }
@@ -500,7 +516,7 @@ hipError_t prepare_dense() {  // (more than 64 KB of dynamic LDS has to be asked
 }
 
 hipError_t launch_dense(const hata_ctx* c, const void* q, const void* K, const void* V, const int32_t* seq_len, int B,
-                        float sm_scale, void* out, float* out_f32, hipStream_t s) {
+                        float sm_scale, void* out, float* out_f32, hipStream_t s, const PageView* pages) {
     const hata_config& f = c->cfg;
     DenseArgs a;
     a.q = (const uint16_t*)q; a.K = (const uint16_t*)K; a.V = (const uint16_t*)V;
@@ -509,14 +525,21 @@ hipError_t launch_dense(const hata_ctx* c, const void* q, const void* K, const v
     a.out = (uint16_t*)out; a.out_f32 = out_f32;
     a.Hq = f.Hq; a.Hkv = f.Hkv; a.G = c->G; a.L_cap = f.L_cap;
     a.B = B;
+    a.pv = PageView{nullptr, 0, 0, 0};
+    if (pages) {
+        a.pv = *pages;
+        a.L_cap = (int)std::min((int64_t)f.L_cap, (int64_t)pages->max_blocks << pages->shift);
+    }
     // one run a unit is even only among sequences of one length: workgroups to spare for the long ones
-    const int64_t units = (int64_t)f.Hkv * B, splits = dense_splits(units, f.L_cap);
+    const int64_t units = (int64_t)f.Hkv * B, splits = dense_splits(units, a.L_cap);
     const int64_t spare = splits == 1 && B > 1 ? std::max((int64_t)0, std::min((int64_t)256, c->dense_wgs_max - units)) : 0;
     a.sb = f.kv_stride_b; a.sh = f.kv_stride_h; a.sn = f.kv_stride_n;
     a.scale_log2 = sm_scale * 1.4426950408889634f;
     const dim3 grid = B == 1 ? dim3((unsigned)splits, f.Hkv) : dim3((unsigned)(units * splits + spare));
-    const auto fn = c->HT >= 4 ? dense_kernel<DENSE_BF16X2> : c->G == 1 ? dense_kernel<DENSE_FP32_ONE_HEAD>
-                    : c->G == 2 ? dense_kernel<DENSE_FP32_TWO_HEADS> : dense_kernel<DENSE_FP32>;
+#define HATA_DENSE_FORM(F_) (pages ? dense_kernel<F_, true> : dense_kernel<F_, false>)
+    const auto fn = c->HT >= 4 ? HATA_DENSE_FORM(DENSE_BF16X2) : c->G == 1 ? HATA_DENSE_FORM(DENSE_FP32_ONE_HEAD)
+                    : c->G == 2 ? HATA_DENSE_FORM(DENSE_FP32_TWO_HEADS) : HATA_DENSE_FORM(DENSE_FP32);
+#undef HATA_DENSE_FORM
     hipLaunchKernelGGL(fn, grid, dim3(DENSE_WAVES * 64), dense_lds(), s, a);
     return hipGetLastError();
 }

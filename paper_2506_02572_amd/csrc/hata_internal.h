@@ -43,6 +43,7 @@ struct hata_ctx {
     unsigned long long* coop_cum;  // [B_max*Hkv, coop_cum_pitch()] cumulative chunk histograms, two scores and the unit's launch a word, and marks (cooperative step)
     uint32_t* unit_epoch;          // [B_max*Hkv, HATA_COUNTER_STRIDE] launches of the cooperative step on a unit, and whether chunk 0 gave the last one up
     unsigned long long* coop_qrec; // [B_max*Hkv, n_chunks, G*Wd] query code words, one copy per chunk, stamped with the unit's launch (cooperative step)
+    uint32_t* plan_counter;  // [1] finished workgroups of a page plan (self-resetting)
     uint32_t* error_word;    // [1] set by a cooperative launch that gave up waiting
     int spin_limit;          // polls an in-kernel wait makes before it gives up (0 = the default)
     int keep_scores;         // single-launch step also writes the score array
@@ -90,7 +91,19 @@ hipError_t launch_encode_score(const hata_ctx* c, const void* q, const void* K, 
                                const int32_t* seq_len, const int32_t* k, int B, hipStream_t s);
 hipError_t prepare_dense();  // once per context
 hipError_t launch_dense(const hata_ctx* c, const void* q, const void* K, const void* V, const int32_t* seq_len, int B,
-                        float sm_scale, void* out, float* out_f32, hipStream_t s);
+                        float sm_scale, void* out, float* out_f32, hipStream_t s, const PageView* pages = nullptr);
+// What hata_plan_pages is given, and the L_cap of its context
+struct PagePlan {
+    const int32_t *len_now, *len_next, *fork_from, *shared_blocks, *n_free;
+    int32_t *table, *free_pages, *n_free_out, *seq_len, *token_start, *slots, *positions;
+    int B, max_blocks, shift, n_pages, max_tokens, cap;
+};
+#define HATA_PLAN_MAX_B 8191  // sequences of a page plan (their sums lie in LDS)
+hipError_t prepare_pages();   // once per context
+hipError_t launch_plan_pages(const hata_ctx* c, const PagePlan& p, hipStream_t s);
+hipError_t launch_write_slots(const hata_ctx* c, const void* K_new, const void* V_new, int64_t stride_t, int64_t stride_h,
+                              const int32_t* slots, int n_tokens, void* K_pool, void* V_pool, uint32_t* codes, int shift, int n_pages,
+                              const float* W_H, hipStream_t s);
 hipError_t prepare_topk();   // once per context
 hipError_t prepare_attention(const hata_ctx* c);  // once per context
 hipError_t launch_topk(const hata_ctx* c, const uint16_t* scores, const int32_t* seq_len,

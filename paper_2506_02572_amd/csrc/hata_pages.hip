@@ -1,0 +1,266 @@
+// Pages of a paged cache: block tables and slot maps from request lengths, and packed rows written through a slot map.
+#include <algorithm>
+#include "hata_device.h"
+#include "hata_hash.h"
+#include "hata_internal.h"
+
+namespace hata {
+
+// ---- block tables and slot map (hata_plan_pages) ----
+//
+// With blocks(n) = ceil(n / page_rows), sequence b needs need[b] = max(0, blocks(next) - blocks(now)) pages and, where it
+// shrinks, releases the blocks from max(blocks(next), shared) up to blocks(now).  Page j of all that are needed, in the order of
+// the sequences, is number avail - 1 - j of the free list with the released pages behind it (avail: their sum), so that
+// neither the tables nor the list need an exchange between workgroups: a page that is released and taken in the same call is
+// looked up in the table that releases it.  Written are rows of growing sequences and list entries from n_free on, read are
+// rows of shrinking sequences and list entries below n_free.  What every workgroup reads and the caller may have given as an
+// output too (lengths, n_free) is written by the last workgroup to arrive.
+// Bound by latency: the lengths, a page, a slot, one after the other.
+// (uint32_t sums: HATA_PLAN_MAX_B sequences of 2^19 blocks, the most an L_cap of 2^23 rows has)
+#define PLAN_THREADS 256
+#define PLAN_TOKENS_SAT ((1u << 23) + 1)  // above every max_tokens; 256 of them still are a 32-bit number
+
+struct PlanRequest {
+    int now, next, src;  // rows cached and wanted, clamped at 0; the sequence that is forked, or -1
+    int have, want, keep, n_new;
+    bool valid;          // the sums left aside
+};
+
+__device__ __forceinline__ PlanRequest plan_request(const PagePlan& p, int b) {
+    PlanRequest r;
+    const int P1 = (1 << p.shift) - 1;
+    const int now = p.len_now[b], next = p.len_next[b];
+    r.src = p.fork_from ? p.fork_from[b] : -1;
+    r.valid = now >= 0 && next >= 0 && now <= p.cap && next <= p.cap;
+    r.now = max(now, 0);
+    r.next = max(next, 0);
+    r.n_new = max(r.next - r.now, 0);
+    r.have = (min(r.now, p.cap) + P1) >> p.shift;
+    r.want = (min(r.next, p.cap) + P1) >> p.shift;
+    r.keep = max(r.want, p.shared_blocks ? p.shared_blocks[b] : 0);
+    if (r.src >= 0) {
+        const int s = min(r.src, p.B - 1);
+        const int held = min(min(p.len_now[s], p.len_next[s]), p.cap) >> p.shift;  // whole pages the source keeps
+        r.valid = r.valid && r.src < p.B && r.src != b && p.fork_from[s] < 0 && (r.now & P1) == 0 && r.next >= r.now &&
+                  r.now >> p.shift <= held;
+    }
+    return r;
+}
+
+// sums over the workgroup's threads below this one
+__device__ __forceinline__ uint32_t plan_before(uint32_t v, uint32_t* lds4) {
+    uint32_t total;
+    return block_excl_scan_256(v, lds4, &total);
+}
+
+__global__ __launch_bounds__(PLAN_THREADS) void plan_pages_kernel(const PagePlan p, uint32_t* counter) {
+    extern __shared__ uint32_t plan_lds[];
+    __shared__ uint32_t lds4[4];
+    __shared__ int s_last;
+    uint32_t* tok_end = plan_lds;         // [B] packed rows up to and with sequence b's, at most PLAN_TOKENS_SAT; top bit: the request is valid and its rows fit
+    uint32_t* need_end = tok_end + p.B;   // [B] the same for the pages that are needed
+    uint32_t* gone_end = need_end + p.B;  // [B] for the pages that are released
+    uint32_t* copy_end = gone_end + p.B;  // [B] for the blocks that forks copy
+    const int tid = threadIdx.x, B = p.B;
+    const int per = (B + PLAN_THREADS - 1) / PLAN_THREADS, b0 = min(tid * per, B), b1 = min(b0 + per, B);
+    const int n_free = clampi(*p.n_free, 0, p.n_pages);
+    constexpr uint32_t OK = 0x80000000u;
+    {
+        uint32_t sum = 0;
+        for (int b = b0; b < b1; ++b) sum += (uint32_t)min(max(p.len_next[b], 0) - min(max(p.len_now[b], 0), max(p.len_next[b], 0)), 1 << 23);
+        uint32_t at = plan_before(min(sum, PLAN_TOKENS_SAT), lds4), need = 0, gone = 0, copy = 0;
+        for (int pass = 0; pass < 2; ++pass) {
+            for (int b = b0; b < b1; ++b) {
+                const PlanRequest r = plan_request(p, b);
+                if (pass == 0) {
+                    at += (uint32_t)min(r.n_new, 1 << 23);
+                    const uint32_t end = min(at, PLAN_TOKENS_SAT);
+                    tok_end[b] = end | (r.valid && (r.n_new == 0 || end <= (uint32_t)p.max_tokens) ? OK : 0u);
+                }
+                const bool ok = tok_end[b] & OK;
+                if (ok) {
+                    need += (uint32_t)max(r.want - r.have, 0);
+                    if (r.next < r.now) gone += (uint32_t)max(r.have - r.keep, 0);
+                    if (r.src >= 0) copy += (uint32_t)(r.now >> p.shift);
+                }
+                if (pass == 1) {
+                    need_end[b] = need;
+                    gone_end[b] = gone;
+                    copy_end[b] = copy;
+                }
+            }
+            if (pass == 0) {
+                need = plan_before(need, lds4);
+                gone = plan_before(gone, lds4);
+                copy = plan_before(copy, lds4);
+            }
+        }
+    }
+    __syncthreads();
+    const uint32_t all_gone = gone_end[B - 1], all_need = need_end[B - 1], all_copy = copy_end[B - 1];
+    const uint32_t all_tokens = tok_end[B - 1] & ~OK;
+    const int64_t avail = (int64_t)n_free + all_gone;
+    auto value = [&](const uint32_t* end, int b) { return end == tok_end ? end[b] & ~OK : end[b]; };
+    auto before = [&](const uint32_t* end, int b) { return b ? value(end, b - 1) : 0u; };
+    auto granted = [&](int b) {
+        const uint32_t to = need_end[b];
+        return (tok_end[b] & OK) && (to == before(need_end, b) || (int64_t)to <= avail);
+    };
+    // the first sequence whose sum is above i
+    auto find = [&](const uint32_t* end, uint32_t i) {
+        int lo = 0, n = B;
+        while (n > 1) {
+            const int half = n / 2;
+            if (value(end, lo + half - 1) <= i) { lo += half; n -= half; }
+            else n = half;
+        }
+        return lo;
+    };
+    // pages taken: those up to the last sequence that gets what it needs
+    uint32_t used = all_need;
+    if ((int64_t)all_need > avail) {
+        // (the sums grow: the last one not above avail)
+        const int b = find(need_end, (uint32_t)avail);  // need_end[b] > avail
+        used = before(need_end, b);
+    }
+    const int64_t left = avail - used;
+    auto released = [&](uint32_t i) {  // page number i of those released
+        const int b = find(gone_end, i);
+        const PlanRequest r = plan_request(p, b);
+        return clampi(p.table[(int64_t)b * p.max_blocks + r.keep + (int)(i - before(gone_end, b))], 0, p.n_pages - 1);
+    };
+    auto taken = [&](uint32_t j) {  // page number j of those needed
+        const int64_t i = avail - 1 - j;
+        return i >= n_free ? released((uint32_t)(i - n_free)) : clampi(p.free_pages[i], 0, p.n_pages - 1);
+    };
+    const uint32_t first = blockIdx.x * PLAN_THREADS + tid, step = gridDim.x * PLAN_THREADS;
+    for (uint32_t t = first; t < (uint32_t)p.max_tokens; t += step) {
+        int slot = -1, pos = -1;
+        if (t < all_tokens) {
+            const int b = find(tok_end, t);
+            if (granted(b)) {
+                const PlanRequest r = plan_request(p, b);
+                pos = r.now + (int)(t - before(tok_end, b));
+                const int block = pos >> p.shift;
+                const int page = block < r.have ? clampi(p.table[(int64_t)b * p.max_blocks + block], 0, p.n_pages - 1)
+                                                : taken(before(need_end, b) + (uint32_t)(block - r.have));
+                slot = (page << p.shift) + (pos & ((1 << p.shift) - 1));
+            }
+        }
+        p.slots[t] = slot;
+        if (p.positions) p.positions[t] = pos;
+    }
+    for (uint32_t j = first; j < used; j += step) {
+        const int b = find(need_end, j);
+        p.table[(int64_t)b * p.max_blocks + plan_request(p, b).have + (int)(j - before(need_end, b))] = taken(j);
+    }
+    for (uint32_t i = first; i < all_copy; i += step) {
+        const int b = find(copy_end, i), k = (int)(i - before(copy_end, b));
+        if (granted(b)) p.table[(int64_t)b * p.max_blocks + k] = p.table[(int64_t)p.fork_from[b] * p.max_blocks + k];
+    }
+    for (uint32_t i = first; i < all_gone && (int64_t)n_free + i < min(left, (int64_t)p.n_pages); i += step) p.free_pages[n_free + i] = released(i);
+    if (gridDim.x > 1) {
+        __syncthreads();  // nothing of this workgroup reads lengths or n_free after this
+        if (tid == 0) {
+            const int last = atomicAdd(counter, 1u) == gridDim.x - 1;
+            if (last) *counter = 0;
+            s_last = last;
+        }
+        __syncthreads();
+        if (!s_last) return;
+    } else {
+        __syncthreads();
+    }
+    for (int b = tid; b < B; b += PLAN_THREADS) {
+        const int now = clampi(p.len_now[b], 0, p.cap), next = p.len_next[b];
+        const int forked = p.fork_from && p.fork_from[b] >= 0;
+        p.seq_len[b] = granted(b) ? next : forked ? 0 : now;
+        if (p.token_start) p.token_start[b] = (int)min(before(tok_end, b), (uint32_t)p.max_tokens);
+    }
+    if (tid == 0) {
+        if (p.token_start) p.token_start[B] = (int)min(all_tokens, (uint32_t)p.max_tokens);
+        *p.n_free_out = (int)min(left, (int64_t)p.n_pages);
+    }
+}
+
+hipError_t prepare_pages() {  // (more than 64 KB of dynamic LDS has to be asked for)
+    return hipFuncSetAttribute((const void*)plan_pages_kernel, hipFuncAttributeMaxDynamicSharedMemorySize, HATA_PLAN_MAX_B * 16);
+}
+
+hipError_t launch_plan_pages(const hata_ctx* c, const PagePlan& p, hipStream_t s) {
+    hipLaunchKernelGGL(plan_pages_kernel, dim3(1), dim3(PLAN_THREADS), (size_t)p.B * 16, s, p, c->plan_counter);
+    return hipGetLastError();
+}
+
+// ---- packed rows into pages (hata_write_slots) ----
+//
+// grid = (slices of COLS hash columns, Hkv, runs of WRITE_ROWS packed rows); the first slice copies the rows.  Codes in fp64
+// (hata_hash.h), four rows at a time.
+#define WRITE_ROWS 16
+struct WriteSlots {
+    const uint16_t *K_new, *V_new;
+    const int32_t* slots;
+    uint16_t *K, *V;
+    uint32_t* codes;
+    const float* W_H;
+    int64_t st, sh;
+    int n, Hkv, r, shift, rows;  // rows: of one head in the pools
+};
+
+__device__ __forceinline__ int64_t slot_row(const WriteSlots& a, int slot, int h) {
+    return (((int64_t)(slot >> a.shift) * a.Hkv + h) << a.shift) + (slot & ((1 << a.shift) - 1));
+}
+
+template <int COLS>
+__global__ __launch_bounds__(256) void write_few_kernel(const WriteSlots a) {
+    constexpr int WPS = COLS / 32;
+    __shared__ uint32_t s_codes[(WRITE_ROWS + 4) * WPS];
+    const int tid = threadIdx.x, h = blockIdx.y, t0 = blockIdx.z * WRITE_ROWS, nv = min(WRITE_ROWS, a.n - t0);
+    if (blockIdx.x == 0) {
+        const int t = t0 + (tid >> 4), o = (tid & 15) * 8;
+        const int slot = t < a.n ? a.slots[t] : -1;
+        if (slot >= 0 && slot < a.rows) {
+            const int64_t from = t * a.st + h * a.sh + o, to = slot_row(a, slot, h) * HATA_D + o;
+            *reinterpret_cast<uint4*>(a.K + to) = *reinterpret_cast<const uint4*>(a.K_new + from);
+            *reinterpret_cast<uint4*>(a.V + to) = *reinterpret_cast<const uint4*>(a.V_new + from);
+        }
+    }
+    if (!a.codes) return;
+    HashWeights<COLS> hw;
+    hw.fetch(a.W_H + (int64_t)h * HATA_D * a.r + blockIdx.x * COLS, a.r);
+    for (int v0 = 0; v0 < nv; v0 += 4) {
+        uint4 x[4];
+        hash_load_x(a.K_new + (int64_t)(t0 + min(v0 + (tid & 3), nv - 1)) * a.st + h * a.sh, x);
+        hash_pass<COLS>(hw, x, s_codes, WPS, v0, nv);
+    }
+    __syncthreads();
+    for (int i = tid; i < nv * WPS; i += 256) {
+        const int slot = a.slots[t0 + i / WPS];
+        if (slot >= 0 && slot < a.rows) a.codes[slot_row(a, slot, h) * (a.r / 32) + blockIdx.x * WPS + i % WPS] = s_codes[i];
+    }
+}
+
+hipError_t launch_write_slots(const hata_ctx* c, const void* K_new, const void* V_new, int64_t stride_t, int64_t stride_h,
+                              const int32_t* slots, int n_tokens, void* K_pool, void* V_pool, uint32_t* codes, int shift, int n_pages,
+                              const float* W_H, hipStream_t s) {
+    const hata_config& f = c->cfg;
+    const WriteSlots all = {(const uint16_t*)K_new, (const uint16_t*)V_new, slots, (uint16_t*)K_pool, (uint16_t*)V_pool, codes, W_H,
+                            stride_t, stride_h, n_tokens, f.Hkv, f.r, shift, n_pages << shift};
+    const int most = 65535 * WRITE_ROWS;  // rows of a launch
+    for (int t0 = 0; t0 < n_tokens; t0 += most) {
+        WriteSlots a = all;
+        a.K_new += t0 * stride_t;
+        a.V_new += t0 * stride_t;
+        a.slots += t0;
+        a.n = std::min(most, n_tokens - t0);
+        const int cols = f.r % 64 == 0 ? 64 : 32;
+        hipLaunchKernelGGL((cols == 64 ? write_few_kernel<64> : write_few_kernel<32>),
+                           dim3(codes ? f.r / cols : 1, f.Hkv, (a.n + WRITE_ROWS - 1) / WRITE_ROWS), dim3(256), 0, s, a);
+        const hipError_t e = hipGetLastError();
+        if (e != hipSuccess) return e;
+        if (n_tokens - t0 <= most) break;  // (t0 stays below 2^31)
+    }
+    return hipSuccess;
+}
+
+}  // namespace hata

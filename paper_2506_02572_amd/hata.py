@@ -18,7 +18,8 @@ EXPORTS = (
     "hata_strerror", "hata_workspace_bytes", "hata_workspace_bytes_tuned", "hata_create", "hata_create_tuned",
     "hata_destroy", "hata_encode_keys", "hata_prepare_weights",
     "hata_prefill_write", "hata_prefill_write_paged", "hata_encode_query", "hata_hamming_score", "hata_topk", "hata_sparse_decode",
-    "hata_sparse_decode_static", "hata_gather_rows", "hata_dense_decode", "hata_decode_step", "hata_select_step", "hata_decode_step_paged", "hata_step_plan", "hata_step_sub_batches", "hata_set_step_mode", "hata_keep_step_scores", "hata_set_wait_limit",
+    "hata_sparse_decode_static", "hata_gather_rows", "hata_dense_decode", "hata_decode_step", "hata_select_step", "hata_decode_step_paged", "hata_plan_pages", "hata_write_slots",
+    "hata_dense_decode_paged", "hata_step_plan", "hata_step_sub_batches", "hata_set_step_mode", "hata_keep_step_scores", "hata_set_wait_limit",
     "hata_check",
     "hata_host_device_pointer", "hata_step_buffers", "hata_probe_mfma_stream",
 )
@@ -89,6 +90,11 @@ def load_library(build_if_missing: bool = True) -> ctypes.CDLL:
                                      ctypes.c_float, _vp, _vp, _vp]
     lib.hata_decode_step_paged.argtypes = [_vp, _vp, _vp, _vp, _vp, _vp, _vp, _i32, _i32, _i32, _vp, _vp,
                                            _i32, _i32, ctypes.c_float, _vp, _vp, _vp]
+    lib.hata_plan_pages.argtypes = [_vp, _vp, _vp, _i32, _vp, _vp, _vp, _i32, _i32, _i32, _vp, _vp, _vp, _vp, _vp, _vp, _vp,
+                                    _i32, _vp]
+    lib.hata_write_slots.argtypes = [_vp, _vp, _vp, ctypes.c_int64, ctypes.c_int64, _vp, _i32, _vp, _vp, _vp, _i32, _i32, _vp, _vp]
+    lib.hata_dense_decode_paged.argtypes = [_vp, _vp, _vp, _vp, _vp, _i32, _i32, _i32, _vp, _i32, _vp, _vp, _i32, ctypes.c_float,
+                                            _vp, _vp, _vp]
     lib.hata_step_plan.argtypes = [_vp, _i32, ctypes.POINTER(_i32), ctypes.POINTER(_i32), ctypes.POINTER(_i32)]
     lib.hata_step_sub_batches.argtypes = [_vp, _i32, ctypes.POINTER(_i32)]
     lib.hata_set_step_mode.argtypes = [_vp, _i32]
@@ -295,6 +301,31 @@ class Context:
                                               _ptr(out), _ptr(out_f32), _stream(stream))
         if rc:
             _check(rc, "hata_decode_step_paged")
+
+    def hata_plan_pages(self, len_now, len_next, B, fork_from, shared_blocks, block_table, max_blocks, page_rows, n_pages,
+                        free_pages, n_free, n_free_out, seq_len, token_start, slots, positions, max_tokens, stream=None):
+        rc = self._lib.hata_plan_pages(self._h, _ptr(len_now), _ptr(len_next), B, _ptr(fork_from), _ptr(shared_blocks),
+                                       _ptr(block_table), max_blocks, page_rows, n_pages, _ptr(free_pages), _ptr(n_free),
+                                       _ptr(n_free_out), _ptr(seq_len), _ptr(token_start), _ptr(slots), _ptr(positions),
+                                       max_tokens, _stream(stream))
+        if rc:
+            _check(rc, "hata_plan_pages")
+
+    def hata_write_slots(self, K_new, V_new, stride_t, stride_h, slots, n_tokens, K_pool, V_pool, codes_pool, page_rows,
+                         n_pages, W_H, stream=None):
+        rc = self._lib.hata_write_slots(self._h, _ptr(K_new), _ptr(V_new), stride_t, stride_h, _ptr(slots), n_tokens,
+                                        _ptr(K_pool), _ptr(V_pool), _ptr(codes_pool), page_rows, n_pages, _ptr(W_H),
+                                        _stream(stream))
+        if rc:
+            _check(rc, "hata_write_slots")
+
+    def hata_dense_decode_paged(self, q, K_pool, V_pool, block_table, max_blocks, page_rows, n_pages, seq_len, B,
+                                group_start, shared_len, n_groups, sm_scale, out, out_f32=None, stream=None):
+        rc = self._lib.hata_dense_decode_paged(self._h, _ptr(q), _ptr(K_pool), _ptr(V_pool), _ptr(block_table), max_blocks,
+                                               page_rows, n_pages, _ptr(seq_len), B, _ptr(group_start), _ptr(shared_len),
+                                               n_groups, sm_scale, _ptr(out), _ptr(out_f32), _stream(stream))
+        if rc:
+            _check(rc, "hata_dense_decode_paged")
 
     def hata_step_plan(self, B):
         """(n_launches, chunk, n_chunks) of hata_decode_step for a batch of B sequences."""
