@@ -42,7 +42,7 @@ inline size_t align_up(size_t v) { return (v + kAlign - 1) / kAlign * kAlign; }
 struct Plan {
     int G, Wd, NB, NBP, chunk, n_chunks, coop_chunk, HT, sparse_rows, sparse_splits;
     int64_t dense_wgs_max;
-    size_t off_qcodes, off_scores, off_idx, off_hist, off_cinfo, off_uinfo, off_ucnt, off_acnt, off_cum, off_epoch, off_qrec, off_err, off_plan, off_uhist, off_partials, off_wplanes, total;
+    size_t off_qcodes, off_scores, off_idx, off_hist, off_cinfo, off_uinfo, off_ucnt, off_acnt, off_cum, off_epoch, off_qrec, off_err, off_plan, off_uhist, off_partials, off_wplanes, off_pre, off_pinfo, total;
 };
 
 int validate_config(const hata_config* f) {
@@ -142,6 +142,8 @@ int make_plan(const hata_config* f, const hata_tuning* t, Plan* p) {
     p->dense_wgs_max = (int64_t)(n_partials / G);
     p->off_partials = o; o = align_up(o + n_partials * (128 + 2) * 4);
     p->off_wplanes = o;  o = align_up(o + (size_t)f->Hkv * 2 * 128 * f->r * 2);  // two fp16 planes
+    p->off_pre = o;      o = align_up(o + hata::prefix_part_floats(f->B_max, f->Hkv, G) * 4);
+    p->off_pinfo = o;    o = align_up(o + (f->B_max > 1 ? (size_t)f->B_max * 16 : 0));
     p->total = o;
     return HATA_OK;
 }
@@ -311,6 +313,8 @@ int hata_create_tuned(hata_ctx** ctx_out, const hata_config* cfg, const hata_tun
     c->plan_counter = (uint32_t*)(w + p.off_plan);
     c->coop_opts = 0;
     c->partials = (float*)(w + p.off_partials);
+    c->prefix_part = (float*)(w + p.off_pre);
+    c->prefix_info = (int32_t*)(w + p.off_pinfo);
     c->wplanes = (f_has_mfma_width(cfg->r)) ? (void*)(w + p.off_wplanes) : nullptr;
     c->prepared_W_H = nullptr;
     c->control_bytes = p.off_partials - p.off_cinfo;
@@ -320,7 +324,7 @@ int hata_create_tuned(hata_ctx** ctx_out, const hata_config* cfg, const hata_tun
         return HATA_EHIP;
     }
     if (hata::prepare_topk() != hipSuccess || hata::prepare_attention(c) != hipSuccess || hata::prepare_dense() != hipSuccess ||
-        hata::prepare_pages() != hipSuccess) {
+        hata::prepare_pages() != hipSuccess || hata::prepare_prefix() != hipSuccess) {
         delete c;
         return HATA_EHIP;
     }
@@ -693,7 +697,14 @@ int hata_dense_decode_paged(hata_ctx* ctx, const void* q, const void* K_pool, co
     hata::PageView pv;
     rc = make_page_view(ctx, block_table, max_blocks, page_rows, n_pages, &pv);
     if (rc != HATA_OK) return rc;
-    return hip_rc(hata::launch_dense(ctx, q, K_pool, V_pool, seq_len, B, sm_scale, out, out_f32, (hipStream_t)stream, &pv));
+    int pre_rows = 0;
+    if (n_groups > 0 && B > 1) {
+        const hipError_t e = hata::launch_prefix(ctx, q, K_pool, V_pool, pv, seq_len, B, group_start, shared_len,
+                                                 n_groups < HATA_PREFIX_GROUPS ? n_groups : HATA_PREFIX_GROUPS, sm_scale, &pre_rows,
+                                                 (hipStream_t)stream);
+        if (e != hipSuccess) return HATA_EHIP;
+    }
+    return hip_rc(hata::launch_dense(ctx, q, K_pool, V_pool, seq_len, B, sm_scale, out, out_f32, (hipStream_t)stream, &pv, pre_rows));
 }
 
 int hata_step_plan(const hata_ctx* ctx, int32_t B, int32_t* n_launches, int32_t* chunk, int32_t* n_chunks) {

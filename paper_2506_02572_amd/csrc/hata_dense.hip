@@ -46,6 +46,11 @@ struct DenseArgs {
     int64_t sb, sh, sn;
     float scale_log2;
     PageView pv;  // PAGED: the caches are pools of pages (sb, sh, sn are not used)
+    // PAGED: what the launch before has of rows that sequences share (prefix_kernel; null: nothing).  Of sequence b: rows that are done
+    // (whole tiles), the first partial result, their number | its query row << 16, the distance between them
+    const int4* info;
+    const float* pre;  // [..][pre_rows][HATA_D], then [pre_rows][2]
+    int pre_rows;
 };
 
 // two heads in the even and odd lanes: the neighbour's value
@@ -66,25 +71,26 @@ __device__ __forceinline__ void wait_tile(int tiles_after) {
 
 // What a workgroup of the launch works on: split `split` of the ns runs that unit (b, h) is cut into, `first` the
 // workgroup that has its first one
-struct DenseShare { int b, h, L, split, ns, first; };
+struct DenseShare { int b, h, L, split, ns, first; };  // (L: rows of its own, where some are shared)
 
 // The launch's workgroups (at least one per unit) in proportion to the sequences' lengths: the shortest run length, from
 // an even share of all tiles and a tile per wave up in steps of an eighth, at which the units' runs are no more than
 // the workgroups.  (Cut by the longest sequence there could be, 16 sequences of which one has 32768 rows and the others
 // 2048 took 167 us, this takes 50; 8 KV heads.)  Every wave of every workgroup computes the same; false: nothing left for this one.
-__device__ __forceinline__ bool dense_share(const int32_t* __restrict__ seq_len, int B, int Hkv, int L_cap, DenseShare& d) {
+// info: of sequences that share rows, how many are done already (x); may be null.
+__device__ __forceinline__ bool dense_share(const int32_t* __restrict__ seq_len, const int4* __restrict__ info, int B, int Hkv, int L_cap, DenseShare& d) {
     if (B == 1) {  // nothing to weigh up: which head this is does not wait for the length
         const int per = gridDim.x;
         d.b = 0;
         d.h = blockIdx.y;
         d.split = blockIdx.x;
         d.first = d.h * per;
-        d.L = clampi(seq_len[0], 0, L_cap);
+        d.L = clampi(seq_len[0], 0, L_cap) - (info ? info[0].x : 0);
         d.ns = clampi(((d.L + 15) / 16 + DENSE_WAVES - 1) / DENSE_WAVES, 1, per);
         return d.split < d.ns;
     }
     const int lane = threadIdx.x & 63, wg = blockIdx.x, wgs = gridDim.x;
-    auto length = [&](int b) { return b < B ? clampi(seq_len[b], 0, L_cap) : -1; };
+    auto length = [&](int b) { return b < B ? clampi(seq_len[b], 0, L_cap) - (info ? info[b].x : 0) : -1; };
     const int own = length(lane);  // the only round trip for up to 64 sequences
     auto of = [&](int b0) { return b0 == 0 ? own : length(b0 + lane); };
     // (a sequence without rows: one workgroup writes zeros)
@@ -137,7 +143,7 @@ __global__ __launch_bounds__(DENSE_WAVES * 64) void dense_kernel(const DenseArgs
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int n = lane & 15, kg = lane >> 4;
     DenseShare d;
-    if (!dense_share(a.seq_len, a.B, a.Hkv, a.L_cap, d)) return;
+    if (!dense_share(a.seq_len, PAGED ? a.info : nullptr, a.B, a.Hkv, a.L_cap, d)) return;
     const int split = d.split, ns = d.ns, h = d.h, b = d.b, L = d.L, G = a.G;
     const int64_t u = (int64_t)b * a.Hkv + h, hq0 = (int64_t)b * a.Hq + (int64_t)h * G;
     uint16_t* outp = a.out + hq0 * HATA_D;
@@ -148,7 +154,18 @@ __global__ __launch_bounds__(DENSE_WAVES * 64) void dense_kernel(const DenseArgs
 #pragma unroll
         for (int s = 0; s < 4; ++s) qb[s] = *reinterpret_cast<const uint4*>(q0 + 32 * s);
     }
-    if (L == 0) {  // no row at all
+    // rows in front of this sequence's own, and the partial results of those
+    int row_first = 0, np = 0, np_row = 0, np_step = 0;
+    const float* pre = nullptr;
+    if (PAGED && a.info) {
+        const int4 x = a.info[b];
+        row_first = x.x;
+        np = x.z & 0xffff;
+        np_row = x.z >> 16;
+        np_step = x.w;
+        pre = a.pre + (x.y + (int64_t)h * np * np_step) * a.pre_rows * (HATA_D + 2);
+    }
+    if (L == 0 && np == 0) {  // no row at all
         for (int i = tid; i < G * HATA_D; i += DENSE_WAVES * 64) {
             outp[i] = 0;
             if (outp32) outp32[i] = 0.f;
@@ -174,11 +191,11 @@ __global__ __launch_bounds__(DENSE_WAVES * 64) void dense_kernel(const DenseArgs
         int64_t at = row0 * sn;
         if constexpr (PAGED) {
             if (j % 64 == 0) {
-                const int n0 = min(row0 + lane * (16 * DENSE_WAVES), L - 1);
+                const int n0 = row_first + min(row0 + lane * (16 * DENSE_WAVES), L - 1);
                 page = clampi(a.pv.table[(int64_t)b * a.pv.max_blocks + (n0 >> a.pv.shift)], 0, a.pv.n_pages - 1);
             }
             const int p = __builtin_amdgcn_readlane(page, j % 64);
-            at = ((((int64_t)p * a.Hkv + h) << a.pv.shift) + (row0 & ((1 << a.pv.shift) - 1))) * HATA_D;
+            at = ((((int64_t)p * a.Hkv + h) << a.pv.shift) + ((row_first + row0) & ((1 << a.pv.shift) - 1))) * HATA_D;
         }
         const uint16_t* kt = Kb + at;
         const uint16_t* vt = Vb + at;
@@ -385,7 +402,7 @@ __global__ __launch_bounds__(DENSE_WAVES * 64) void dense_kernel(const DenseArgs
             av = fmaf(f, s_acc[(w * G + g) * (HATA_D + 4) + ch], av);
             l = fmaf(f, s_l[w][g], l);
         }
-        if (ns == 1) {
+        if (ns + np == 1) {
             const float o = l > 0.f ? av / l : 0.f;
             outp[i] = (uint16_t)f32_to_bf16(o);
             if (outp32) outp32[i] = o;
@@ -395,7 +412,7 @@ __global__ __launch_bounds__(DENSE_WAVES * 64) void dense_kernel(const DenseArgs
             if (ch == 0) { st_dev(pp, M); st_dev(pp + 1, l); }
         }
     }
-    if (ns == 1) return;
+    if (ns + np == 1) return;
     // ---- the last workgroup of the unit merges (partials: write-through stores, device-coherent loads) ----
     wait_stores();
     __syncthreads();
@@ -407,67 +424,76 @@ __global__ __launch_bounds__(DENSE_WAVES * 64) void dense_kernel(const DenseArgs
     }
     __syncthreads();
     if (!s_last) return;
-    // thread: slices part, part + parts, ... of one head's channel pair; the first batch of loads before the weights
-    float* s_w = reinterpret_cast<float*>(smem);                    // [G][ns] normalised weights
-    float2* s_sum = reinterpret_cast<float2*>(s_w + ((G * ns + 3) & ~3));  // [parts][G * 64]
+    // thread: slices part, part + parts, ... of one head's channel pair; the first batch of loads before the weights.  Behind the
+    // unit's own slices come those of the rows in front (np, PAGED)
+    const int nt = PAGED ? ns + np : ns;
+    float* s_w = reinterpret_cast<float*>(smem);                    // [G][nt] normalised weights
+    float2* s_sum = reinterpret_cast<float2*>(s_w + ((G * nt + 3) & ~3));  // [parts][G * 64]
     const int items = G * (HATA_D / 2);
     const int parts = max(1, DENSE_WAVES * 64 / items);
-    auto address = [&](int i) {
-        return part0 + (i / (HATA_D / 2)) * head_stride + 2 + 2 * (i % (HATA_D / 2));
+    auto slice = [&](int g, int ch, int s) -> uint2 {  // two channels of slice s
+        if (PAGED && s >= ns)
+            return *reinterpret_cast<const uint2*>(pre + (int64_t)(s - ns) * np_step * a.pre_rows * (HATA_D + 2) + (np_row + g) * HATA_D + ch);
+        return ld_dev_u2(part0 + g * head_stride + 2 + ch + (int64_t)s * HATA_PSTRIDE);
     };
+    auto state = [&](int g, int s) -> uint2 {  // its maximum and sum
+        if (PAGED && s >= ns)
+            return *reinterpret_cast<const uint2*>(pre + ((int64_t)(s - ns) * np_step * (HATA_D + 2) + HATA_D) * a.pre_rows + 2 * (np_row + g));
+        return ld_dev_u2(part0 + g * head_stride + (int64_t)s * HATA_PSTRIDE);
+    };
+    constexpr int NML = PAGED ? 8 : 4;  // slices of a lane: DENSE_MAX_RUNS, and as many in front
     for (int i0 = 0; i0 < items; i0 += DENSE_WAVES * 64) {  // (more than once with more than 8 heads)
         const int item = min(i0 + (parts > 1 ? tid % items : tid), items - 1), part = parts > 1 ? tid / items : 0;
-        const float* pp = address(item);
+        const int ig = item / (HATA_D / 2), ich = 2 * (item % (HATA_D / 2));
         uint2 x[DENSE_BATCH];
         if (part < parts) {
 #pragma unroll
             for (int k = 0; k < DENSE_BATCH; ++k) {
                 const int s = part + k * parts;
-                x[k] = s < ns ? ld_dev_u2(pp + (int64_t)s * HATA_PSTRIDE) : make_uint2(0, 0);
+                x[k] = s < nt ? slice(ig, ich, s) : make_uint2(0, 0);
             }
         }
         if (i0 == 0) {
             for (int g = wave; g < G; g += DENSE_WAVES) {
-                const float* mp = part0 + g * head_stride;
-                uint2 ml[4];
+                uint2 ml[NML];
 #pragma unroll
-                for (int t = 0; t < 4; ++t)
-                    if (t * 64 < ns) ml[t] = ld_dev_u2(mp + (int64_t)min(lane + 64 * t, ns - 1) * HATA_PSTRIDE);
+                for (int t = 0; t < NML; ++t)
+                    if (t * 64 < nt) ml[t] = state(g, min(lane + 64 * t, nt - 1));
                 float M = HATA_NEG_INF;
 #pragma unroll
-                for (int t = 0; t < 4; ++t)
-                    if (lane + 64 * t < ns) M = fmaxf(M, __uint_as_float(ml[t].x));
+                for (int t = 0; t < NML; ++t)
+                    if (lane + 64 * t < nt) M = fmaxf(M, __uint_as_float(ml[t].x));
                 M = wave_max64(M);
-                float w[4], l = 0.f;
+                float w[NML], l = 0.f;
 #pragma unroll
-                for (int t = 0; t < 4; ++t) {
-                    w[t] = lane + 64 * t < ns && M != HATA_NEG_INF ? fast_exp2(__uint_as_float(ml[t].x) - M) : 0.f;
-                    if (lane + 64 * t < ns) l = fmaf(w[t], __uint_as_float(ml[t].y), l);
+                for (int t = 0; t < NML; ++t) {
+                    w[t] = lane + 64 * t < nt && M != HATA_NEG_INF ? fast_exp2(__uint_as_float(ml[t].x) - M) : 0.f;
+                    if (lane + 64 * t < nt) l = fmaf(w[t], __uint_as_float(ml[t].y), l);
                 }
                 l = wave_sum64(l);
                 const float inv = l > 0.f ? 1.f / l : 0.f;
 #pragma unroll
-                for (int t = 0; t < 4; ++t)
-                    if (lane + 64 * t < ns) s_w[g * ns + lane + 64 * t] = w[t] * inv;
+                for (int t = 0; t < NML; ++t)
+                    if (lane + 64 * t < nt) s_w[g * nt + lane + 64 * t] = w[t] * inv;
             }
             __syncthreads();
         }
         float2 sum = make_float2(0.f, 0.f);
         if (part < parts) {
-            const float* w = s_w + item / (HATA_D / 2) * ns;
+            const float* w = s_w + ig * nt;
             for (int s0 = part;;) {
 #pragma unroll
                 for (int k = 0; k < DENSE_BATCH; ++k) {
-                    const float f = w[min(s0 + k * parts, ns - 1)];  // (x is zero past the end)
+                    const float f = w[min(s0 + k * parts, nt - 1)];  // (x is zero past the end)
                     sum.x = fmaf(f, __uint_as_float(x[k].x), sum.x);
                     sum.y = fmaf(f, __uint_as_float(x[k].y), sum.y);
                 }
                 s0 += DENSE_BATCH * parts;
-                if (s0 >= ns) break;
+                if (s0 >= nt) break;
 #pragma unroll
                 for (int k = 0; k < DENSE_BATCH; ++k) {
                     const int s = s0 + k * parts;
-                    x[k] = s < ns ? ld_dev_u2(pp + (int64_t)s * HATA_PSTRIDE) : make_uint2(0, 0);
+                    x[k] = s < nt ? slice(ig, ich, s) : make_uint2(0, 0);
                 }
             }
         }
@@ -516,7 +542,7 @@ hipError_t prepare_dense() {  // (more than 64 KB of dynamic LDS has to be asked
 }
 
 hipError_t launch_dense(const hata_ctx* c, const void* q, const void* K, const void* V, const int32_t* seq_len, int B,
-                        float sm_scale, void* out, float* out_f32, hipStream_t s, const PageView* pages) {
+                        float sm_scale, void* out, float* out_f32, hipStream_t s, const PageView* pages, int pre_rows) {
     const hata_config& f = c->cfg;
     DenseArgs a;
     a.q = (const uint16_t*)q; a.K = (const uint16_t*)K; a.V = (const uint16_t*)V;
@@ -526,6 +552,9 @@ hipError_t launch_dense(const hata_ctx* c, const void* q, const void* K, const v
     a.Hq = f.Hq; a.Hkv = f.Hkv; a.G = c->G; a.L_cap = f.L_cap;
     a.B = B;
     a.pv = PageView{nullptr, 0, 0, 0};
+    a.info = pre_rows ? (const int4*)c->prefix_info : nullptr;
+    a.pre = c->prefix_part;
+    a.pre_rows = pre_rows;
     if (pages) {
         a.pv = *pages;
         a.L_cap = (int)std::min((int64_t)f.L_cap, (int64_t)pages->max_blocks << pages->shift);

@@ -55,6 +55,8 @@ struct hata_ctx {
     int cus;                 // compute units of the device that was current in hata_create
     int coop_opt_cap_paged[4];  // the same for the block-table variant of the kernel
     float* partials;       // [B_max*Hq, max(sparse_splits, n_chunks), d + 2], at least 256 * HATA_DENSE_ROUNDS * G rows
+    float* prefix_part;    // partial results of rows that groups of sequences share (prefix_part_floats)
+    int32_t* prefix_info;  // [B_max, 4] where a sequence finds its own among them
     void* wplanes;               // [Hkv, r/32, 8, 2, 64] 16-byte fragments: the two scaled fp16 planes of the hash weights (prefill key encode)
     const float* prepared_W_H;   // the weight tensor those planes were made from (nullptr: none)
     size_t control_bytes;  // bytes from chunk_info up to the partials: the control words, cleared at creation and after a give-up
@@ -91,7 +93,14 @@ hipError_t launch_encode_score(const hata_ctx* c, const void* q, const void* K, 
                                const int32_t* seq_len, const int32_t* k, int B, hipStream_t s);
 hipError_t prepare_dense();  // once per context
 hipError_t launch_dense(const hata_ctx* c, const void* q, const void* K, const void* V, const int32_t* seq_len, int B,
-                        float sm_scale, void* out, float* out_f32, hipStream_t s, const PageView* pages = nullptr);
+                        float sm_scale, void* out, float* out_f32, hipStream_t s, const PageView* pages = nullptr, int pre_rows = 0);
+// Rows that groups of sequences share, in front of launch_dense of the same call: partial results in prefix_part, *part_rows (which
+// launch_dense is then given as pre_rows) query rows each, and in prefix_info where a sequence finds its own
+#define HATA_PREFIX_GROUPS 1024  // groups beyond share nothing
+size_t prefix_part_floats(int B, int Hkv, int G);
+hipError_t prepare_prefix();  // once per context
+hipError_t launch_prefix(const hata_ctx* c, const void* q, const void* K, const void* V, const PageView& pages, const int32_t* seq_len, int B,
+                         const int32_t* group_start, const int32_t* shared_len, int n_groups, float sm_scale, int* part_rows, hipStream_t s);
 // What hata_plan_pages is given, and the L_cap of its context
 struct PagePlan {
     const int32_t *len_now, *len_next, *fork_from, *shared_blocks, *n_free;
