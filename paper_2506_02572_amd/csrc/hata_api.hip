@@ -134,7 +134,7 @@ int make_plan(const hata_config* f, const hata_tuning* t, Plan* p) {
     p->off_epoch = o;    o = align_up(o + (size_t)units * HATA_COUNTER_STRIDE * 4);
     p->off_qrec = o;     o = align_up(o + (size_t)f->B_max * f->Hq * p->Wd * p->n_chunks * 8);
     p->off_err = o;      o = align_up(o + 4);
-    p->off_plan = o;     o = align_up(o + 4);
+    p->off_plan = o;     o = align_up(o + (1 + HATA_PLAN_WGS / HATA_PLAN_GROUP) * HATA_COUNTER_STRIDE * 4);
     p->off_uhist = o;    o = align_up(o + (size_t)units * p->NB * 4);
     size_t n_partials = (size_t)f->B_max * f->Hq * max_splits;
     const size_t dense_partials = (size_t)256 * HATA_DENSE_ROUNDS * G;  // a workgroup has one per head of its group

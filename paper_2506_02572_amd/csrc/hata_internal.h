@@ -43,7 +43,7 @@ struct hata_ctx {
     unsigned long long* coop_cum;  // [B_max*Hkv, coop_cum_pitch()] cumulative chunk histograms, two scores and the unit's launch a word, and marks (cooperative step)
     uint32_t* unit_epoch;          // [B_max*Hkv, HATA_COUNTER_STRIDE] launches of the cooperative step on a unit, and whether chunk 0 gave the last one up
     unsigned long long* coop_qrec; // [B_max*Hkv, n_chunks, G*Wd] query code words, one copy per chunk, stamped with the unit's launch (cooperative step)
-    uint32_t* plan_counter;  // [1] finished workgroups of a page plan (self-resetting)
+    uint32_t* plan_counter;  // [1 + groups of workgroups, HATA_COUNTER_STRIDE] finished ones of a page plan (self-resetting)
     uint32_t* error_word;    // [1] set by a cooperative launch that gave up waiting
     int spin_limit;          // polls an in-kernel wait makes before it gives up (0 = the default)
     int keep_scores;         // single-launch step also writes the score array
@@ -108,6 +108,8 @@ struct PagePlan {
     int B, max_blocks, shift, n_pages, max_tokens, cap;
 };
 #define HATA_PLAN_MAX_B 8191  // sequences of a page plan (their sums lie in LDS)
+#define HATA_PLAN_WGS 512     // workgroups of a plan at most, and of a group that arrives together
+#define HATA_PLAN_GROUP 32
 hipError_t prepare_pages();   // once per context
 hipError_t launch_plan_pages(const hata_ctx* c, const PagePlan& p, hipStream_t s);
 hipError_t launch_write_slots(const hata_ctx* c, const void* K_new, const void* V_new, int64_t stride_t, int64_t stride_h,

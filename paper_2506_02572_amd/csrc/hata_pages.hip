@@ -15,9 +15,11 @@ namespace hata {
 // looked up in the table that releases it.  Written are rows of growing sequences and list entries from n_free on, read are
 // rows of shrinking sequences and list entries below n_free.  What every workgroup reads and the caller may have given as an
 // output too (lengths, n_free) is written by the last workgroup to arrive.
-// Bound by latency: the lengths, a page, a slot, one after the other.
+// Bound by latency: launch, lengths, sums, a page, a slot, one after the other.  32 sequences of a token each 5.9 us; 704 sequences
+// with 198779 new rows 12.7 (one workgroup 1690; 256 of them 16.5, a counter for all 512 17.6, pages behind the slots 17).
 // (uint32_t sums: HATA_PLAN_MAX_B sequences of 2^19 blocks, the most an L_cap of 2^23 rows has)
 #define PLAN_THREADS 256
+#define PLAN_BATCH 4
 #define PLAN_TOKENS_SAT ((1u << 23) + 1)  // above every max_tokens; 256 of them still are a 32-bit number
 
 struct PlanRequest {
@@ -62,38 +64,38 @@ __global__ __launch_bounds__(PLAN_THREADS) void plan_pages_kernel(const PagePlan
     uint32_t* gone_end = need_end + p.B;  // [B] for the pages that are released
     uint32_t* copy_end = gone_end + p.B;  // [B] for the blocks that forks copy
     const int tid = threadIdx.x, B = p.B;
-    const int per = (B + PLAN_THREADS - 1) / PLAN_THREADS, b0 = min(tid * per, B), b1 = min(b0 + per, B);
     const int n_free = clampi(*p.n_free, 0, p.n_pages);
     constexpr uint32_t OK = 0x80000000u;
+    // what every request adds, read side by side; then the sums, a run of sequences a thread
+#pragma unroll 4
+    for (int b = tid; b < B; b += PLAN_THREADS) {
+        const PlanRequest r = plan_request(p, b);
+        tok_end[b] = (uint32_t)min(r.n_new, 1 << 23) | (r.valid ? OK : 0u);
+        need_end[b] = (uint32_t)max(r.want - r.have, 0);
+        gone_end[b] = r.next < r.now ? (uint32_t)max(r.have - r.keep, 0) : 0u;
+        copy_end[b] = r.src >= 0 ? (uint32_t)(r.now >> p.shift) : 0u;
+    }
+    __syncthreads();
     {
-        uint32_t sum = 0;
-        for (int b = b0; b < b1; ++b) sum += (uint32_t)min(max(p.len_next[b], 0) - min(max(p.len_now[b], 0), max(p.len_next[b], 0)), 1 << 23);
-        uint32_t at = plan_before(min(sum, PLAN_TOKENS_SAT), lds4), need = 0, gone = 0, copy = 0;
-        for (int pass = 0; pass < 2; ++pass) {
-            for (int b = b0; b < b1; ++b) {
-                const PlanRequest r = plan_request(p, b);
-                if (pass == 0) {
-                    at += (uint32_t)min(r.n_new, 1 << 23);
-                    const uint32_t end = min(at, PLAN_TOKENS_SAT);
-                    tok_end[b] = end | (r.valid && (r.n_new == 0 || end <= (uint32_t)p.max_tokens) ? OK : 0u);
-                }
-                const bool ok = tok_end[b] & OK;
-                if (ok) {
-                    need += (uint32_t)max(r.want - r.have, 0);
-                    if (r.next < r.now) gone += (uint32_t)max(r.have - r.keep, 0);
-                    if (r.src >= 0) copy += (uint32_t)(r.now >> p.shift);
-                }
-                if (pass == 1) {
-                    need_end[b] = need;
-                    gone_end[b] = gone;
-                    copy_end[b] = copy;
-                }
-            }
-            if (pass == 0) {
-                need = plan_before(need, lds4);
-                gone = plan_before(gone, lds4);
-                copy = plan_before(copy, lds4);
-            }
+        const int per = (B + PLAN_THREADS - 1) / PLAN_THREADS, b0 = min(tid * per, B), b1 = min(b0 + per, B);
+        uint32_t sum = 0, need = 0, gone = 0, copy = 0;
+        for (int b = b0; b < b1; ++b) sum += tok_end[b] & ~OK;
+        uint32_t at = plan_before(min(sum, PLAN_TOKENS_SAT), lds4);
+        for (int b = b0; b < b1; ++b) {
+            const uint32_t own = tok_end[b] & ~OK, end = min(at += own, PLAN_TOKENS_SAT);
+            const bool ok = (tok_end[b] & OK) && (own == 0 || end <= (uint32_t)p.max_tokens);
+            tok_end[b] = end | (ok ? OK : 0u);
+            need_end[b] = need += ok ? need_end[b] : 0u;
+            gone_end[b] = gone += ok ? gone_end[b] : 0u;
+            copy_end[b] = copy += ok ? copy_end[b] : 0u;
+        }
+        need = plan_before(need, lds4);
+        gone = plan_before(gone, lds4);
+        copy = plan_before(copy, lds4);
+        for (int b = b0; b < b1; ++b) {
+            need_end[b] += need;
+            gone_end[b] += gone;
+            copy_end[b] += copy;
         }
     }
     __syncthreads();
@@ -124,46 +126,80 @@ __global__ __launch_bounds__(PLAN_THREADS) void plan_pages_kernel(const PagePlan
         used = before(need_end, b);
     }
     const int64_t left = avail - used;
-    auto released = [&](uint32_t i) {  // page number i of those released
+    auto released_at = [&](uint32_t i) -> const int32_t* {  // where page number i of those released is found
         const int b = find(gone_end, i);
-        const PlanRequest r = plan_request(p, b);
-        return clampi(p.table[(int64_t)b * p.max_blocks + r.keep + (int)(i - before(gone_end, b))], 0, p.n_pages - 1);
+        const int P1 = (1 << p.shift) - 1, want = (p.len_next[b] + P1) >> p.shift;
+        const int keep = max(want, p.shared_blocks ? p.shared_blocks[b] : 0);
+        return p.table + (int64_t)b * p.max_blocks + keep + (int)(i - before(gone_end, b));
     };
-    auto taken = [&](uint32_t j) {  // page number j of those needed
+    auto taken_at = [&](uint32_t j) -> const int32_t* {  // page number j of those needed
         const int64_t i = avail - 1 - j;
-        return i >= n_free ? released((uint32_t)(i - n_free)) : clampi(p.free_pages[i], 0, p.n_pages - 1);
+        return i >= n_free ? released_at((uint32_t)(i - n_free)) : p.free_pages + i;
     };
-    const uint32_t first = blockIdx.x * PLAN_THREADS + tid, step = gridDim.x * PLAN_THREADS;
-    for (uint32_t t = first; t < (uint32_t)p.max_tokens; t += step) {
-        int slot = -1, pos = -1;
-        if (t < all_tokens) {
-            const int b = find(tok_end, t);
-            if (granted(b)) {
-                const PlanRequest r = plan_request(p, b);
-                pos = r.now + (int)(t - before(tok_end, b));
-                const int block = pos >> p.shift;
-                const int page = block < r.have ? clampi(p.table[(int64_t)b * p.max_blocks + block], 0, p.n_pages - 1)
-                                                : taken(before(need_end, b) + (uint32_t)(block - r.have));
-                slot = (page << p.shift) + (pos & ((1 << p.shift) - 1));
+    auto page_number = [&](int v) { return clampi(v, 0, p.n_pages - 1); };
+    // Slots by the first workgroups, pages by the others, a chain of look-ups each: one behind the other they took twice as long.
+    // PLAN_BATCH elements of a thread go through a chain together.
+    const int slot_wgs = gridDim.x < 4 ? (int)gridDim.x : (int)(gridDim.x - gridDim.x / 4);
+    const bool pages_too = gridDim.x < 4, slot_wg = (int)blockIdx.x < slot_wgs;
+    if (slot_wg) {
+        const uint32_t step = (uint32_t)slot_wgs * PLAN_THREADS;
+        for (uint32_t t = blockIdx.x * PLAN_THREADS + tid; t < (uint32_t)p.max_tokens; t += step) {
+            int slot = -1, pos = -1;
+            if (t < all_tokens) {
+                const int b = find(tok_end, t);
+                if (granted(b)) {
+                    const int now = p.len_now[b], P1 = (1 << p.shift) - 1, have = (now + P1) >> p.shift;
+                    pos = now + (int)(t - before(tok_end, b));
+                    const int block = pos >> p.shift;
+                    const int32_t* at = block < have ? p.table + (int64_t)b * p.max_blocks + block
+                                                     : taken_at(before(need_end, b) + (uint32_t)(block - have));
+                    slot = (page_number(*at) << p.shift) + (pos & P1);
+                }
             }
+            p.slots[t] = slot;
+            if (p.positions) p.positions[t] = pos;
         }
-        p.slots[t] = slot;
-        if (p.positions) p.positions[t] = pos;
     }
-    for (uint32_t j = first; j < used; j += step) {
-        const int b = find(need_end, j);
-        p.table[(int64_t)b * p.max_blocks + plan_request(p, b).have + (int)(j - before(need_end, b))] = taken(j);
+    if (!slot_wg || pages_too) {
+        // a wave per sequence
+        const int lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+        const int first = (int)(pages_too ? blockIdx.x : blockIdx.x - slot_wgs) * 4 + wave;
+        const int step = (int)(pages_too ? gridDim.x : gridDim.x - slot_wgs) * 4;
+        const int64_t spare = min(left, (int64_t)p.n_pages) - n_free;  // released pages that nobody took
+        // n elements, element i read at src + i and written to dst + i
+        auto move = [&](const int32_t* src, int32_t* dst, int n) {
+            for (int i0 = lane; i0 < n; i0 += 64 * PLAN_BATCH) {
+                int v[PLAN_BATCH];
+#pragma unroll
+                for (int k = 0; k < PLAN_BATCH; ++k) v[k] = src[min(i0 + 64 * k, n - 1)];
+#pragma unroll
+                for (int k = 0; k < PLAN_BATCH; ++k)
+                    if (i0 + 64 * k < n) dst[i0 + 64 * k] = v[k];
+            }
+        };
+        for (int b = first; b < B; b += step) {
+            const uint32_t need0 = before(need_end, b), gone0 = before(gone_end, b), copy0 = before(copy_end, b);
+            const int need = (int)(need_end[b] - need0), gone = (int)(gone_end[b] - gone0), copy = (int)(copy_end[b] - copy0);
+            if ((need | gone | copy) == 0 || !granted(b)) continue;
+            int32_t* row = p.table + (int64_t)b * p.max_blocks;
+            const int P1 = (1 << p.shift) - 1, have = (p.len_now[b] + P1) >> p.shift;
+            for (int i = lane; i < need; i += 64) row[have + i] = page_number(*taken_at(need0 + i));
+            if (copy) move(p.table + (int64_t)p.fork_from[b] * p.max_blocks, row, copy);
+            if (gone) move(row + (have - gone), p.free_pages + n_free + gone0, (int)min((int64_t)gone, max(spare - (int64_t)gone0, (int64_t)0)));
+        }
     }
-    for (uint32_t i = first; i < all_copy; i += step) {
-        const int b = find(copy_end, i), k = (int)(i - before(copy_end, b));
-        if (granted(b)) p.table[(int64_t)b * p.max_blocks + k] = p.table[(int64_t)p.fork_from[b] * p.max_blocks + k];
-    }
-    for (uint32_t i = first; i < all_gone && (int64_t)n_free + i < min(left, (int64_t)p.n_pages); i += step) p.free_pages[n_free + i] = released(i);
     if (gridDim.x > 1) {
         __syncthreads();  // nothing of this workgroup reads lengths or n_free after this
         if (tid == 0) {
-            const int last = atomicAdd(counter, 1u) == gridDim.x - 1;
-            if (last) *counter = 0;
+            // (in groups: arrivals at one counter come 17 ns apart)
+            const int group = blockIdx.x / HATA_PLAN_GROUP, groups = (gridDim.x + HATA_PLAN_GROUP - 1) / HATA_PLAN_GROUP;
+            uint32_t* own = counter + (1 + group) * HATA_COUNTER_STRIDE;
+            int last = atomicAdd(own, 1u) == min(HATA_PLAN_GROUP, (int)gridDim.x - group * HATA_PLAN_GROUP) - 1;
+            if (last) {
+                *own = 0;
+                last = atomicAdd(counter, 1u) == groups - 1;
+                if (last) *counter = 0;
+            }
             s_last = last;
         }
         __syncthreads();
@@ -188,7 +224,8 @@ hipError_t prepare_pages() {  // (more than 64 KB of dynamic LDS has to be asked
 }
 
 hipError_t launch_plan_pages(const hata_ctx* c, const PagePlan& p, hipStream_t s) {
-    hipLaunchKernelGGL(plan_pages_kernel, dim3(1), dim3(PLAN_THREADS), (size_t)p.B * 16, s, p, c->plan_counter);
+    const int wgs = std::max(1, std::min(HATA_PLAN_WGS, std::max((p.max_tokens + PLAN_THREADS - 1) / PLAN_THREADS, p.B / 4)));
+    hipLaunchKernelGGL(plan_pages_kernel, dim3(wgs), dim3(PLAN_THREADS), (size_t)p.B * 16, s, p, c->plan_counter);
     return hipGetLastError();
 }
 

@@ -135,6 +135,8 @@ __device__ __forceinline__ bool prefix_share(const PrefixArgs& a, int mpt, int* 
         for (int b = tid; b < a.B; b += 256)
             if (b < start[0] || b >= start[n]) a.info[b] = make_int4(0, 0, 0, 0);
     __syncthreads();  // (the LDS is used anew)
+    // (in scalar registers from here on)
+    for (int* v : {&w.g, &w.h, &w.split, &w.ns, &w.qt, &w.tiles, &w.item, &w.first, &w.members, &w.lead}) *v = __builtin_amdgcn_readfirstlane(*v);
     return w.g >= 0;
 }
 
@@ -149,7 +151,7 @@ __device__ __forceinline__ void prefix_wait() { asm volatile("s_waitcnt vmcnt(%0
 template <int WQ>
 __global__ __launch_bounds__(256, 1) void prefix_kernel(const PrefixArgs a) {
     constexpr int WK = 4 / WQ, PART = WQ == 4 ? 64 : 32, STAGE = WK * PART, SUBS = PART / 32;
-    constexpr int NBUF = 128 / STAGE * 2 > 4 ? 4 : 128 / STAGE * 2;  // stages in LDS: 128 KB
+    constexpr int NBUF = 256 / STAGE;                                // stages in LDS: 128 KB
     constexpr int BLOCKS = PART / WQ / 16;                           // blocks of 16 rows a wave requests of a stage, K and V
     constexpr int M = 64 * WQ;
     extern __shared__ __attribute__((aligned(16))) char smem[];
@@ -183,27 +185,37 @@ __global__ __launch_bounds__(256, 1) void prefix_kernel(const PrefixArgs a) {
     }
 
     const uint32_t ring = __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)(__attribute__((address_space(3))) void*)smem);
-    const int32_t* table = a.pv.table + (int64_t)w.lead * a.pv.max_blocks;
+    // Page numbers by scalar loads, a stage ahead: a wait for a vector load is one for every request in flight
+    const auto table = (const __attribute__((address_space(4))) int32_t*)(uintptr_t)(a.pv.table + (int64_t)w.lead * a.pv.max_blocks);
+    int pages[BLOCKS];
+    auto first_row = [&](int s, int j) { return min(k0 + s * STAGE + wk * PART + (wq * BLOCKS + j) * 16, k1 - 16); };
+    auto look_up = [&](int s) {
+#pragma unroll
+        for (int j = 0; j < BLOCKS; ++j) pages[j] = table[first_row(s, j) >> a.pv.shift];
+    };
+    look_up(0);
     // this wave's rows of a stage: PART wk + 16 BLOCKS wq + 16 j ..; lane l of an instruction fetches, of row 4 i + l / 16 of a block,
     // the piece that belongs at slot l % 16
-    const int lr = lane >> 4, ls = lane & 15;
+    uint32_t off[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) off[i] = (4 * i + (lane >> 4)) * 256 + ((lane & 15) ^ (lane >> 4 << 2 | i)) * 16;
     auto request = [&](int s) {
 #pragma unroll
         for (int j = 0; j < BLOCKS; ++j) {
-            const int in = wk * PART + (wq * BLOCKS + j) * 16;
-            const int row = min(k0 + s * STAGE + in, k1 - 16);
-            const int page = clampi(__builtin_amdgcn_readfirstlane(table[row >> a.pv.shift]), 0, a.pv.n_pages - 1);
+            const int row = first_row(s, j), page = clampi(pages[j], 0, a.pv.n_pages - 1);
             const int64_t at = ((((int64_t)page * a.Hkv + w.h) << a.pv.shift) + (row & ((1 << a.pv.shift) - 1))) * HATA_D;
-            const uint32_t dst = ring + (uint32_t)((s % NBUF) * STAGE * 512 + in * 256);
+            const uint32_t dst = ring + (uint32_t)((s % NBUF) * STAGE * 512 + (wk * PART + (wq * BLOCKS + j) * 16) * 256);
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-                const int64_t o = at + (4 * i + lr) * HATA_D + (ls ^ (lr << 2 | i)) * 8;
                 // (written as instructions: behind the compiler's builtin for it, every LDS read waits for all requests)
-                asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(dst + i * 1024), "v"(a.K + o) : "memory", "m0");
-                asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(dst + STAGE * 256 + i * 1024), "v"(a.V + o) : "memory", "m0");
+                asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(dst + i * 1024), "v"(off[i]), "s"(a.K + at) : "memory", "m0");
+                asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(dst + STAGE * 256 + i * 1024), "v"(off[i]), "s"(a.V + at) : "memory", "m0");
             }
         }
+        look_up(s + 1);
     };
+    // The sums and the query rows live in the accumulation registers, where the matrix instructions take them from, the scores in the
+    // others; said at every turn, or the compiler moves the sums to and fro
     f32x16_t acc[2][4];
     float m[2] = {HATA_NEG_INF, HATA_NEG_INF}, sub[2] = {0.f, 0.f}, l[2] = {0.f, 0.f};
 #pragma unroll
@@ -212,10 +224,91 @@ __global__ __launch_bounds__(256, 1) void prefix_kernel(const PrefixArgs a) {
         for (int c = 0; c < 4; ++c)
 #pragma unroll
             for (int i = 0; i < 16; ++i) acc[t][c][i] = 0.f;
+    auto pin = [&]() {
+#pragma unroll
+        for (int t = 0; t < 2; ++t)
+#pragma unroll
+            for (int c = 0; c < 4; ++c) asm volatile("" : "+a"(acc[t][c]));
+    };
     // K operand: row n, piece 2 s + half.  V operand: rows 16 x + 4 half + 8 y + (lane % 16) / 4, channels 32 c + lane's 16 and the
     // four of lane % 4
     const uint32_t k_at = n * 256 + ((half ^ prefix_swizzle(n)) << 4);
     const int v_row = 4 * half + (lane & 15) / 4, v_piece = (lane >> 4 & 1) * 2 + ((lane & 3) >> 1);
+
+    auto products = [&](const char* kt, f32x16_t (&sc)[2]) {
+#pragma unroll
+        for (int t = 0; t < 2; ++t)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) sc[t][i] = 0.f;
+#pragma unroll
+        for (int k = 0; k < 8; ++k) {
+            const bf16x8_t kf = __builtin_bit_cast(bf16x8_t, *reinterpret_cast<const uint4*>(kt + (k_at ^ (k << 5))));
+#pragma unroll
+            for (int t = 0; t < 2; ++t)
+                sc[t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf, __builtin_bit_cast(bf16x8_t, qb[t][k]), sc[t], 0, 0, 0);
+        }
+#pragma unroll
+        for (int t = 0; t < 2; ++t) asm volatile("" : "+v"(sc[t]));
+    };
+    // the maxima in use, where these scores pass one by 2^8
+    auto follow = [&](const f32x16_t (&sc)[2]) {
+        float top[2];
+#pragma unroll
+        for (int t = 0; t < 2; ++t) {
+            top[t] = sc[t][0];
+#pragma unroll
+            for (int i = 1; i < 16; ++i) top[t] = fmaxf(top[t], sc[t][i]);
+            top[t] *= scale;
+        }
+        if (__builtin_amdgcn_ballot_w64(top[0] > m[0] + 8.f || top[1] > m[1] + 8.f) != 0ull) {
+#pragma unroll
+            for (int t = 0; t < 2; ++t) {
+                float x, y;
+                swap32(top[t], x, y);
+                const float to = fmaxf(fmaxf(x, y), m[t]);  // of both halves' rows
+                const float f = m[t] == HATA_NEG_INF ? (to == HATA_NEG_INF ? 1.f : 0.f) : fast_exp2(m[t] - to);
+                l[t] *= f;
+#pragma unroll
+                for (int c = 0; c < 4; ++c) acc[t][c] *= f;
+                m[t] = to;
+                sub[t] = to == HATA_NEG_INF ? 0.f : to;
+            }
+            pin();
+        }
+    };
+    auto weights = [&](const f32x16_t (&sc)[2], uint32_t (&p)[2][8]) {
+#pragma unroll
+        for (int t = 0; t < 2; ++t)
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                f32x2_t e;
+                e[0] = fast_exp2(fmaf(sc[t][2 * i], scale, -sub[t]));
+                e[1] = fast_exp2(fmaf(sc[t][2 * i + 1], scale, -sub[t]));
+                p[t][i] = __builtin_bit_cast(uint32_t, __builtin_convertvector(e, bf16x2_t));
+                l[t] = dot2_bf16(p[t][i], 0x3f803f80u, l[t]);
+            }
+    };
+    auto values = [&](const char* vt, const uint32_t (&p)[2][8]) {
+#pragma unroll
+        for (int x = 0; x < 2; ++x)
+#pragma unroll
+            for (int c = 0; c < 4; ++c) {
+                uint2 v[2];
+#pragma unroll
+                for (int y = 0; y < 2; ++y) {
+                    const int r = 16 * x + 8 * y + v_row;
+                    const s16x4_t av = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4_t*)const_cast<char*>(
+                        vt + r * 256 + (((4 * c + v_piece) ^ prefix_swizzle(r)) << 4) + (lane & 1) * 8));
+                    v[y] = __builtin_bit_cast(uint2, av);
+                }
+                const bf16x8_t vf = __builtin_bit_cast(bf16x8_t, make_uint4(v[0].x, v[0].y, v[1].x, v[1].y));
+#pragma unroll
+                for (int t = 0; t < 2; ++t)
+                    acc[t][c] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(
+                        vf, __builtin_bit_cast(bf16x8_t, make_uint4(p[t][4 * x], p[t][4 * x + 1], p[t][4 * x + 2], p[t][4 * x + 3])), acc[t][c], 0, 0, 0);
+            }
+    };
+    auto at_stage = [&](int s) { return (const char*)smem + (s % NBUF) * STAGE * 512 + wk * PART * 256; };  // K; V is STAGE * 256 bytes behind
 
     for (int s = 0; s < NBUF - (WQ > 1); ++s)
         if (s < stages) request(s);
@@ -223,84 +316,53 @@ __global__ __launch_bounds__(256, 1) void prefix_kernel(const PrefixArgs a) {
     for (int t = 0; t < 2; ++t)
 #pragma unroll
         for (int s = 0; s < 8; ++s)  // (used here, so that the wait for these loads is not in the loop)
-            asm volatile("" : "+v"(qb[t][s].x), "+v"(qb[t][s].y), "+v"(qb[t][s].z), "+v"(qb[t][s].w));
-    for (int s = 0; s < stages; ++s) {
-        // this wave's part of stage s is there once only the requests after it are outstanding
-        constexpr int AFTER = WQ > 1 ? NBUF - 2 : NBUF - 1;
-        if (s + AFTER < stages) prefix_wait<AFTER * BLOCKS * 8>();
-        else prefix_wait<0>();
-        if constexpr (WQ > 1) {
-            __syncthreads();
-            if (s + NBUF - 1 < stages) request(s + NBUF - 1);
-        }
-#pragma unroll
-        for (int sub_t = 0; sub_t < SUBS; ++sub_t) {
-            const char* kt = smem + (s % NBUF) * STAGE * 512 + (wk * PART + sub_t * 32) * 256;
-            const char* vt = kt + STAGE * 256;
-            if (STAGE > PREFIX_TILE && k0 + s * STAGE + wk * PART >= k1) break;  // (nothing but the last tile once more)
-            f32x16_t sc[2];
-#pragma unroll
-            for (int t = 0; t < 2; ++t)
-#pragma unroll
-                for (int i = 0; i < 16; ++i) sc[t][i] = 0.f;
-#pragma unroll
-            for (int k = 0; k < 8; ++k) {
-                const bf16x8_t kf = __builtin_bit_cast(bf16x8_t, *reinterpret_cast<const uint4*>(kt + (k_at ^ (k << 5))));
-#pragma unroll
-                for (int t = 0; t < 2; ++t)
-                    sc[t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf, __builtin_bit_cast(bf16x8_t, qb[t][k]), sc[t], 0, 0, 0);
+            asm volatile("" : "+a"(qb[t][s].x), "+a"(qb[t][s].y), "+a"(qb[t][s].z), "+a"(qb[t][s].w));
+    pin();
+    if constexpr (WQ == 1) {
+        // rows of this wave alone: nothing is waited for but its own requests
+        for (int s = 0; s < stages; ++s) {
+            if (s + 1 < stages) prefix_wait<BLOCKS * 8>();
+            else prefix_wait<0>();
+            if (k0 + s * STAGE + wk * PART < k1) {
+                f32x16_t sc[2];
+                uint32_t p[2][8];
+                products(at_stage(s), sc);
+                follow(sc);
+                weights(sc, p);
+                values(at_stage(s) + STAGE * 256, p);
             }
-            uint32_t p[2][8];
-#pragma unroll
-            for (int t = 0; t < 2; ++t) {
-                float top = sc[t][0];
-#pragma unroll
-                for (int i = 1; i < 16; ++i) top = fmaxf(top, sc[t][i]);
-                top *= scale;
-                if (__builtin_amdgcn_ballot_w64(top > m[t] + 8.f) != 0ull) {
-                    float x, y;
-                    swap32(top, x, y);
-                    const float to = fmaxf(fmaxf(x, y), m[t]);  // of both halves' rows
-                    const float f = fast_exp2(m[t] - to);       // (0 for the first)
-                    if (to != HATA_NEG_INF) {
-                        l[t] *= m[t] == HATA_NEG_INF ? 0.f : f;
-#pragma unroll
-                        for (int c = 0; c < 4; ++c) acc[t][c] *= m[t] == HATA_NEG_INF ? 0.f : f;
-                        m[t] = to;
-                        sub[t] = to;
-                    }
-                }
-#pragma unroll
-                for (int i = 0; i < 8; ++i) {
-                    f32x2_t e;
-                    e[0] = fast_exp2(fmaf(sc[t][2 * i], scale, -sub[t]));
-                    e[1] = fast_exp2(fmaf(sc[t][2 * i + 1], scale, -sub[t]));
-                    p[t][i] = __builtin_bit_cast(uint32_t, __builtin_convertvector(e, bf16x2_t));
-                    l[t] = dot2_bf16(p[t][i], 0x3f803f80u, l[t]);
-                }
-            }
-#pragma unroll
-            for (int x = 0; x < 2; ++x)
-#pragma unroll
-                for (int c = 0; c < 4; ++c) {
-                    uint2 v[2];
-#pragma unroll
-                    for (int y = 0; y < 2; ++y) {
-                        const int r = 16 * x + 8 * y + v_row;
-                        const s16x4_t av = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4_t*)const_cast<char*>(
-                            vt + r * 256 + (((4 * c + v_piece) ^ prefix_swizzle(r)) << 4) + (lane & 1) * 8));
-                        v[y] = __builtin_bit_cast(uint2, av);
-                    }
-                    const bf16x8_t vf = __builtin_bit_cast(bf16x8_t, make_uint4(v[0].x, v[0].y, v[1].x, v[1].y));
-#pragma unroll
-                    for (int t = 0; t < 2; ++t)
-                        acc[t][c] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(
-                            vf, __builtin_bit_cast(bf16x8_t, make_uint4(p[t][4 * x], p[t][4 * x + 1], p[t][4 * x + 2], p[t][4 * x + 3])), acc[t][c], 0, 0, 0);
-                }
-        }
-        if constexpr (WQ == 1) {
             asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // every read of this stage has returned
             if (s + NBUF < stages) request(s + NBUF);
+            pin();
+        }
+    } else {
+        // The products of the next 32 rows stand beside the weights of these: matrix cores and vector ALU at work together
+        f32x16_t sc[2], next[2];
+        if (stages >= NBUF - 1) prefix_wait<(NBUF - 2) * BLOCKS * 8>();  // (so many were requested)
+        else prefix_wait<0>();
+        __syncthreads();
+        products(at_stage(0), sc);
+        for (int s = 0; s < stages; ++s) {
+#pragma unroll
+            for (int i = 0; i < SUBS; ++i) {
+                uint32_t p[2][8];
+                follow(sc);
+                if (i + 1 < SUBS) {
+                    products(at_stage(s) + (i + 1) * 32 * 256, next);
+                } else if (s + 1 < stages) {
+                    // stage s + 1 is there once only the one behind it is outstanding; everybody is done with stage s - 1
+                    if (s + 2 < stages) prefix_wait<(NBUF - 3) * BLOCKS * 8>();
+                    else prefix_wait<0>();
+                    __syncthreads();
+                    if (s + NBUF - 1 < stages) request(s + NBUF - 1);
+                    products(at_stage(s + 1), next);
+                }
+                weights(sc, p);
+                values(at_stage(s) + STAGE * 256 + i * 32 * 256, p);
+#pragma unroll
+                for (int t = 0; t < 2; ++t) sc[t] = next[t];
+                pin();
+            }
         }
     }
 
