@@ -1,6 +1,8 @@
 // Pages of a paged cache: block tables and slot maps from request lengths, and packed rows written through a slot map.
 #include <algorithm>
+#include "hata_attn_core.h"
 #include "hata_device.h"
+#include "hata_encode_core.h"
 #include "hata_hash.h"
 #include "hata_internal.h"
 
@@ -234,6 +236,9 @@ hipError_t launch_plan_pages(const hata_ctx* c, const PagePlan& p, hipStream_t s
 // grid = (slices of COLS hash columns, Hkv, runs of WRITE_ROWS packed rows); the first slice copies the rows.  Codes in fp64
 // (hata_hash.h), four rows at a time.
 #define WRITE_ROWS 16
+// Rows up to which a call with codes goes this way: us, eight heads, r = 128, this way / by the matrix cores with prepared weights:
+// 64 rows 6.5 / 6.2, 128 6.8 / 7.2, 512 10.1 / 8.3, 1024 15.8 / 8.8; r = 256, 64 and 256 rows 6.3 / 6.7, 9.6 / 8.4
+#define HATA_WRITE_FEW 128
 struct WriteSlots {
     const uint16_t *K_new, *V_new;
     const int32_t* slots;
@@ -277,6 +282,239 @@ __global__ __launch_bounds__(256) void write_few_kernel(const WriteSlots a) {
     }
 }
 
+// Many rows: the projection on the matrix cores, as in encode_mfma_kernel (M = 32 hash columns of a wave, N = 32 rows; prepared
+// fp16 planes, or three bf16 planes split here), and the values next to zero once more in fp64.
+//
+// A sum of the matrix cores is within WRITE_ERROR |x| |w| of the exact one (Euclidean norms; at most 24 instructions, each off by a few units
+// in the last place of a partial sum, which |x| |w| bounds).  A sum that is not above that (one value in some 7000 of normally
+// distributed ones) is in doubt: it goes on a list, and once the workgroup is through its rows, sixteen lanes evaluate each of
+// them in fp64, where the products are exact.  (Evaluated where they were found, by a wave each, they cost a latency a stage.
+// 20711 rows, eight heads, r = 128, us: 46.0 that way, 38.7 with the list, 37.4 with none in doubt.)
+// fp16 planes: x loses up to 2^-24 below 2^-14 and saturates at 65504, the weights 2^-22 of their size or 2^-25; rows of which that
+// says nothing, because they are as large or as small as the numbers get, infinite or NaN, are evaluated in fp64 as a whole.
+//
+// Bound by the bytes it moves (512 read and 512 written a row), then by the products, which do not overlap with them on this
+// device: those 20711 rows 38.7 us, 4.5 TB/s, where a large copy reaches 4.8; 16384 rows of 32 heads, r = 256, 166 us, 3.4 TB/s.
+// Rounds of resident workgroups (write_rows_per_wg): 45.4 us with twice as many of half the rows.
+#define WRITE_ERROR 0x1p-16f
+#define WRITE_MAX_ROWS 1024  // of a workgroup
+#define WRITE_DOUBTS 512
+template <int R, bool F16>
+__global__ __launch_bounds__(R <= 128 ? 256 : 512, 2) void write_mfma_kernel(const WriteSlots a, const uint4* __restrict__ planes, int rows_per_wg) {
+    constexpr int COLW = R / 32, KP = R >= 128 ? 1 : 128 / R;  // waves by columns, by rows
+    constexpr int THREADS = 64 * COLW * KP, NT = R >= 128 ? 2 : 1, STAGE = 32 * NT * KP, WD = R / 32;
+    constexpr int ROWS_PER_IT = THREADS / 16, NIT = STAGE / ROWS_PER_IT;
+    __shared__ __attribute__((aligned(16))) uint16_t tile[STAGE * HATA_MFMA_PITCH];
+    __shared__ __attribute__((aligned(16))) uint32_t s_code[WRITE_MAX_ROWS * WD];
+    __shared__ float s_norm[STAGE];
+    __shared__ int s_row[WRITE_MAX_ROWS];
+    __shared__ uint32_t s_doubt[WRITE_DOUBTS];  // row of the workgroup * R + column
+    __shared__ int s_doubts, s_wholes;
+    __shared__ uint32_t s_whole[WRITE_MAX_ROWS / 32];  // rows of which every bit is in doubt
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int w = wave % COLW, part = wave / COLW, m = lane & 31, half = lane >> 5, h = blockIdx.y;
+    const int first = blockIdx.x * rows_per_wg, last = min(first + rows_per_wg, a.n);
+    const uint16_t* Kh = a.K_new + h * a.sh;
+    const uint16_t* Vh = a.V_new + h * a.sh;
+
+    const int lrow = tid >> 4, lsub = tid & 15;
+    uint4 pre[NIT], vpre[NIT];
+    int slot[NIT];
+    auto load_stage = [&](int t0) {
+#pragma unroll
+        for (int it = 0; it < NIT; ++it) {
+            const int t = t0 + it * ROWS_PER_IT + lrow;
+            slot[it] = a.slots[min(t, last - 1)];
+            if (t >= last) slot[it] = -1;
+        }
+#pragma unroll
+        for (int it = 0; it < NIT; ++it) {
+            const int64_t o = min(t0 + it * ROWS_PER_IT + lrow, last - 1) * a.st + lsub * 8;
+            pre[it] = load_once(Kh + o);
+            vpre[it] = load_once(Vh + o);
+        }
+    };
+    load_stage(first);
+    if (tid == 0) s_doubts = s_wholes = 0;
+    if (tid < WRITE_MAX_ROWS / 32) s_whole[tid] = 0;
+
+    // weight fragments, and the largest norm of this wave's columns (of the fp16 planes: scaled as they are)
+    bf16x8_t afrag[F16 ? 1 : 3][F16 ? 1 : 8];
+    f16x8_t afrag16[F16 ? 2 : 1][F16 ? 8 : 1];
+    float norm2 = 0.f, some_w = 0.f;
+    if constexpr (F16) {
+        const uint4* src = planes + ((int64_t)(h * COLW + w) * 8 * 2) * 64 + lane;
+#pragma unroll
+        for (int kk = 0; kk < 8; ++kk) {
+#pragma unroll
+            for (int p = 0; p < 2; ++p) afrag16[p][kk] = __builtin_bit_cast(f16x8_t, src[(kk * 2 + p) * 64]);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) norm2 = fmaf((float)afrag16[0][kk][e], (float)afrag16[0][kk][e], norm2);
+        }
+        some_w = norm2;  // (the largest weight of a tile is scaled to 2^13 or more)
+    } else {
+        const float* wp = a.W_H + (int64_t)h * HATA_D * R + w * 32 + m;
+#pragma unroll
+        for (int kk = 0; kk < 8; ++kk) {
+            uint32_t hi[4], mid[4], lo[4];
+#pragma unroll
+            for (int e2 = 0; e2 < 4; ++e2) {
+                const float w0 = wp[(int64_t)(kk * 16 + 8 * half + 2 * e2) * R], w1 = wp[(int64_t)(kk * 16 + 8 * half + 2 * e2 + 1) * R];
+                split_weight_pair(w0, w1, hi[e2], mid[e2], lo[e2]);
+                norm2 = fmaf(w0, w0, fmaf(w1, w1, norm2));
+                some_w = fmaxf(some_w, fmaxf(fabsf(w0), fabsf(w1)));
+            }
+            afrag[0][kk] = __builtin_bit_cast(bf16x8_t, make_uint4(hi[0], hi[1], hi[2], hi[3]));
+            afrag[1][kk] = __builtin_bit_cast(bf16x8_t, make_uint4(mid[0], mid[1], mid[2], mid[3]));
+            afrag[2][kk] = __builtin_bit_cast(bf16x8_t, make_uint4(lo[0], lo[1], lo[2], lo[3]));
+        }
+    }
+    norm2 += __shfl_xor(norm2, 32, 64);
+    // (the maximum drops NaN; of tiny weights, whose squares are lost, all rows are evaluated in fp64)
+    const bool doubt = __builtin_amdgcn_ballot_w64(!(norm2 < 0x1p120f)) != 0ull;
+    norm2 = wave_max64(norm2);
+    const bool no_w = !doubt && __builtin_amdgcn_ballot_w64(some_w != 0.f) == 0ull;
+    const float wn = no_w ? 0.f : doubt || norm2 < 0x1p-80f ? __builtin_huge_valf() : sqrtf(norm2);
+
+    // row t of the workgroup, hash column col, by the lanes of a row of sixteen; every one of them gets the answer
+    auto exact_bit = [&](int t, int col) {
+        const uint4 x = *reinterpret_cast<const uint4*>(Kh + (first + t) * a.st + lsub * 8);
+        const float* wc = a.W_H + ((int64_t)h * HATA_D + lsub * 8) * R + col;
+        float wv[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) wv[e] = wc[e * R];
+        const uint32_t xv[4] = {x.x, x.y, x.z, x.w};
+        double s = 0.0;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) s = fma((double)bf16_hi(xv[e]), (double)wv[2 * e + 1], fma((double)bf16_lo(xv[e]), (double)wv[2 * e], s));
+#pragma unroll
+        for (int o = 8; o >= 1; o >>= 1) s += __shfl_xor(s, o, 16);
+        return s >= 0.0;
+    };
+
+    for (int t0 = first; t0 < last; t0 += STAGE) {
+        __syncthreads();  // the previous stage has been consumed
+#pragma unroll
+        for (int it = 0; it < NIT; ++it) {
+            const int row = it * ROWS_PER_IT + lrow;
+            const uint4 x = pre[it];
+            *reinterpret_cast<uint4*>(&tile[row * HATA_MFMA_PITCH + lsub * 8]) = F16 ? __builtin_bit_cast(uint4, bf16x8_to_f16(x)) : x;
+            const float n2 = row_sum16(dot2_bf16(x.x, x.x, dot2_bf16(x.y, x.y, dot2_bf16(x.z, x.z, dot2_bf16(x.w, x.w, 0.f)))));
+            const float some = row_max16(((x.x | x.y | x.z | x.w) & 0x7fff7fffu) ? 1.f : 0.f);
+            int to = -1;
+            if (slot[it] >= 0 && slot[it] < a.rows) {
+                to = (int)slot_row(a, slot[it], h);
+                *reinterpret_cast<uint4*>(a.K + (int64_t)to * HATA_D + lsub * 8) = x;
+                *reinterpret_cast<uint4*>(a.V + (int64_t)to * HATA_D + lsub * 8) = vpre[it];
+            }
+            if (lsub == 0) {
+                // (a row of zeros projects to zero, in any arithmetic, and so does any row where the weights are zeros)
+                const bool in_range = n2 < (F16 ? 0x1p31f : 0x1p120f) && (n2 >= 0x1p-80f || some == 0.f);
+                s_norm[row] = in_range ? sqrtf(n2) : __builtin_huge_valf();
+                s_row[t0 - first + row] = to;
+            }
+        }
+        __syncthreads();
+        if (t0 + STAGE < last) load_stage(t0 + STAGE);  // overlaps the products below
+
+        f32x16_t acc[NT];
+#pragma unroll
+        for (int t = 0; t < NT; ++t)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) acc[t][i] = 0.f;
+        const int row0 = part * 32 * NT;
+        uint4 bfrag[NT];  // (a channel step ahead)
+#pragma unroll
+        for (int t = 0; t < NT; ++t) bfrag[t] = *reinterpret_cast<const uint4*>(&tile[(row0 + t * 32 + m) * HATA_MFMA_PITCH + 8 * half]);
+#pragma unroll
+        for (int kk = 0; kk < 8; ++kk)
+#pragma unroll
+            for (int t = 0; t < NT; ++t) {
+                if constexpr (F16) {
+#pragma unroll
+                    for (int p = 0; p < 2; ++p)
+                        acc[t] = __builtin_amdgcn_mfma_f32_32x32x16_f16(afrag16[p][kk], __builtin_bit_cast(f16x8_t, bfrag[t]), acc[t], 0, 0, 0);
+                } else {
+#pragma unroll
+                    for (int p = 0; p < 3; ++p)
+                        acc[t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(afrag[p][kk], __builtin_bit_cast(bf16x8_t, bfrag[t]), acc[t], 0, 0, 0);
+                }
+                if (kk + 1 < 8)
+                    bfrag[t] = *reinterpret_cast<const uint4*>(&tile[(row0 + t * 32 + m) * HATA_MFMA_PITCH + (kk + 1) * 16 + 8 * half]);
+            }
+        // this lane holds hash columns 8 (i / 4) + 4 half + i % 4 of row t * 32 + m
+#pragma unroll
+        for (int t = 0; t < NT; ++t) {
+            uint32_t word = sign_bits(acc[t]);
+            const int row = row0 + t * 32 + m;
+            const float xn = s_norm[row], near = F16 ? wn * fmaf(WRITE_ERROR, xn, 0x1p-20f) + 0x1p-21f * xn : WRITE_ERROR * wn * xn;
+            float least = fabsf(acc[t][0]);
+#pragma unroll
+            for (int i = 1; i < 16; ++i) least = fminf(least, fabsf(acc[t][i]));
+            const bool zeros = xn == 0.f || wn == 0.f;
+            const bool live = s_row[t0 - first + row] >= 0;
+            if (__builtin_amdgcn_ballot_w64(live && !zeros && !(least > near)) != 0ull) {
+                uint32_t todo = 0;
+#pragma unroll
+                for (int i = 0; i < 16; ++i) todo |= (!(fabsf(acc[t][i]) > near) ? 1u : 0u) << (8 * (i / 4) + i % 4);
+                if (zeros || !live) todo = 0;
+                const int r = t0 - first + row;
+                bool whole = todo != 0 && !(near < __builtin_huge_valf());
+                for (; todo && !whole; todo &= todo - 1) {
+                    const int at = atomicAdd(&s_doubts, 1);
+                    whole = at >= WRITE_DOUBTS;  // (no room)
+                    if (!whole) s_doubt[at] = (uint32_t)r * R + 32 * w + 4 * half + __ffs(todo) - 1;
+                }
+                if (whole) {
+                    atomicOr(&s_whole[r / 32], 1u << (r % 32));
+                    s_wholes = 1;
+                }
+            }
+            word <<= 4 * half;
+            word |= (uint32_t)__shfl_xor((int)word, 32, 64);
+            if (half == 0) s_code[(t0 - first + row) * WD + w] = word;
+        }
+    }
+    __syncthreads();
+    auto settle = [&](uint32_t item, bool own) {
+        const bool one = exact_bit((int)(item / R), (int)(item % R));
+        if (own && lsub == 0) {
+            uint32_t* word = &s_code[item / 32];
+            if (one) atomicOr(word, 1u << (item % 32));
+            else atomicAnd(word, ~(1u << (item % 32)));
+        }
+    };
+    const int doubts = min(s_doubts, WRITE_DOUBTS);
+    for (int i = tid / 16; i < (doubts + THREADS / 16 - 1) / (THREADS / 16) * (THREADS / 16); i += THREADS / 16)
+        settle(s_doubt[min(i, doubts - 1)], i < doubts);
+    for (int k = 0; k < (s_wholes ? WRITE_MAX_ROWS / 32 : 0); ++k)
+        for (uint32_t rows = s_whole[k]; rows; rows &= rows - 1)
+            for (int c = tid / 16; c < R; c += THREADS / 16) settle((uint32_t)(32 * k + __ffs(rows) - 1) * R + c, true);
+    __syncthreads();
+    // the code words, 16 bytes a thread where a code is as long
+    if constexpr (WD >= 4) {
+        for (int i = tid; i < (last - first) * (WD / 4); i += THREADS) {
+            const int to = s_row[i / (WD / 4)];
+            if (to >= 0) *reinterpret_cast<uint4*>(a.codes + (int64_t)to * WD + i % (WD / 4) * 4) = *reinterpret_cast<const uint4*>(&s_code[i * 4]);
+        }
+    } else {
+        for (int i = tid; i < (last - first) * WD; i += THREADS)
+            if (s_row[i / WD] >= 0) a.codes[(int64_t)s_row[i / WD] * WD + i % WD] = s_code[i];
+    }
+}
+
+// Rows of a workgroup: a round of as many workgroups as are resident (two of four waves on a compute unit, one of eight), or several
+// equal rounds
+static int write_rows_per_wg(int n, int Hkv, int r) {
+    const int64_t resident = (r <= 128 ? 2 : 1) * 256;
+    const int64_t stages = (n + 63) / 64;
+    int64_t rounds = 1, per;
+    do per = (stages * Hkv + rounds * resident - 1) / (rounds * resident), ++rounds;
+    while (per > WRITE_MAX_ROWS / 64);
+    while ((stages + per - 1) / per * Hkv > (rounds - 1) * resident && per < WRITE_MAX_ROWS / 64) ++per;  // (whole stages of every head)
+    return (int)per * 64;
+}
+
 hipError_t launch_write_slots(const hata_ctx* c, const void* K_new, const void* V_new, int64_t stride_t, int64_t stride_h,
                               const int32_t* slots, int n_tokens, void* K_pool, void* V_pool, uint32_t* codes, int shift, int n_pages,
                               const float* W_H, hipStream_t s) {
@@ -290,6 +528,23 @@ hipError_t launch_write_slots(const hata_ctx* c, const void* K_new, const void* 
         a.V_new += t0 * stride_t;
         a.slots += t0;
         a.n = std::min(most, n_tokens - t0);
+        if (codes && n_tokens > HATA_WRITE_FEW && (f.r == 32 || f.r == 64 || f.r == 128 || f.r == 256)) {
+            // the weight planes prepared for exactly this weight tensor, if any
+            const uint4* planes = (c->prepared_W_H == W_H && c->wplanes) ? (const uint4*)c->wplanes : nullptr;
+            const int per = write_rows_per_wg(a.n, f.Hkv, f.r);
+            const dim3 grid((a.n + per - 1) / per, f.Hkv);
+#define HATA_LAUNCH_WRITE(R_) \
+    hipLaunchKernelGGL((planes ? write_mfma_kernel<R_, true> : write_mfma_kernel<R_, false>), grid, dim3(R_ <= 128 ? 256 : 512), 0, s, a, planes, per)
+            if (f.r == 32) HATA_LAUNCH_WRITE(32);
+            else if (f.r == 64) HATA_LAUNCH_WRITE(64);
+            else if (f.r == 128) HATA_LAUNCH_WRITE(128);
+            else HATA_LAUNCH_WRITE(256);
+#undef HATA_LAUNCH_WRITE
+            const hipError_t e = hipGetLastError();
+            if (e != hipSuccess) return e;
+            if (n_tokens - t0 <= most) break;
+            continue;
+        }
         const int cols = f.r % 64 == 0 ? 64 : 32;
         hipLaunchKernelGGL((cols == 64 ? write_few_kernel<64> : write_few_kernel<32>),
                            dim3(codes ? f.r / cols : 1, f.Hkv, (a.n + WRITE_ROWS - 1) / WRITE_ROWS), dim3(256), 0, s, a);
