@@ -140,10 +140,12 @@ int make_plan(const hata_config* f, const hata_tuning* t, Plan* p) {
     const size_t dense_partials = (size_t)256 * HATA_DENSE_ROUNDS * G;  // a workgroup has one per head of its group
     if (n_partials < dense_partials) n_partials = dense_partials;
     p->dense_wgs_max = (int64_t)(n_partials / G);
+    const size_t own_partials = f->B_max > 1 ? (size_t)hata::dense_own_wgs(f->B_max, f->Hkv) * 8 * G : 0;  // (a wave has)
+    if (n_partials < own_partials) n_partials = own_partials;
     p->off_partials = o; o = align_up(o + n_partials * (128 + 2) * 4);
     p->off_wplanes = o;  o = align_up(o + (size_t)f->Hkv * 2 * 128 * f->r * 2);  // two fp16 planes
     p->off_pre = o;      o = align_up(o + hata::prefix_part_floats(f->B_max, f->Hkv, G) * 4);
-    p->off_pinfo = o;    o = align_up(o + (f->B_max > 1 ? (size_t)f->B_max * 16 : 0));
+    p->off_pinfo = o;    o = align_up(o + (f->B_max > 1 ? f->B_max * sizeof(hata::PrefixPlan) : 0));
     p->total = o;
     return HATA_OK;
 }
@@ -314,7 +316,7 @@ int hata_create_tuned(hata_ctx** ctx_out, const hata_config* cfg, const hata_tun
     c->coop_opts = 0;
     c->partials = (float*)(w + p.off_partials);
     c->prefix_part = (float*)(w + p.off_pre);
-    c->prefix_info = (int32_t*)(w + p.off_pinfo);
+    c->prefix_plan = (hata::PrefixPlan*)(w + p.off_pinfo);
     c->wplanes = (f_has_mfma_width(cfg->r)) ? (void*)(w + p.off_wplanes) : nullptr;
     c->prepared_W_H = nullptr;
     c->control_bytes = p.off_partials - p.off_cinfo;

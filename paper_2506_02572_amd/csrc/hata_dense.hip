@@ -19,6 +19,7 @@
 // workgroup with loads through registers and 64 partial results per unit took 36.8 and 48.7.  B = 4, 65536 rows,
 // groups of 8 (1.07 GB): 167 us, 6.4 TB/s (209).
 #include <algorithm>
+#include <type_traits>
 #include "hata_device.h"
 #include "hata_internal.h"
 #include "hata_attn_core.h"
@@ -46,9 +47,8 @@ struct DenseArgs {
     int64_t sb, sh, sn;
     float scale_log2;
     PageView pv;  // PAGED: the caches are pools of pages (sb, sh, sn are not used)
-    // PAGED: what the launch before has of rows that sequences share (prefix_kernel; null: nothing).  Of sequence b: rows that are done
-    // (whole tiles), the first partial result, their number | its query row << 16, the distance between them
-    const int4* info;
+    // DENSE_OWN: the sequences' runs and the shared rows' partial results, from the launch before
+    const PrefixPlan* plan;
     const float* pre;  // [..][pre_rows][HATA_D], then [pre_rows][2]
     int pre_rows;
 };
@@ -77,20 +77,19 @@ struct DenseShare { int b, h, L, split, ns, first; };  // (L: rows of its own, w
 // an even share of all tiles and a tile per wave up in steps of an eighth, at which the units' runs are no more than
 // the workgroups.  (Cut by the longest sequence there could be, 16 sequences of which one has 32768 rows and the others
 // 2048 took 167 us, this takes 50; 8 KV heads.)  Every wave of every workgroup computes the same; false: nothing left for this one.
-// info: of sequences that share rows, how many are done already (x); may be null.
-__device__ __forceinline__ bool dense_share(const int32_t* __restrict__ seq_len, const int4* __restrict__ info, int B, int Hkv, int L_cap, DenseShare& d) {
+__device__ __forceinline__ bool dense_share(const int32_t* __restrict__ seq_len, int B, int Hkv, int L_cap, DenseShare& d) {
     if (B == 1) {  // nothing to weigh up: which head this is does not wait for the length
         const int per = gridDim.x;
         d.b = 0;
         d.h = blockIdx.y;
         d.split = blockIdx.x;
         d.first = d.h * per;
-        d.L = clampi(seq_len[0], 0, L_cap) - (info ? info[0].x : 0);
+        d.L = clampi(seq_len[0], 0, L_cap);
         d.ns = clampi(((d.L + 15) / 16 + DENSE_WAVES - 1) / DENSE_WAVES, 1, per);
         return d.split < d.ns;
     }
     const int lane = threadIdx.x & 63, wg = blockIdx.x, wgs = gridDim.x;
-    auto length = [&](int b) { return b < B ? clampi(seq_len[b], 0, L_cap) - (info ? info[b].x : 0) : -1; };
+    auto length = [&](int b) { return b < B ? clampi(seq_len[b], 0, L_cap) : -1; };
     const int own = length(lane);  // the only round trip for up to 64 sequences
     auto of = [&](int b0) { return b0 == 0 ? own : length(b0 + lane); };
     // (a sequence without rows: one workgroup writes zeros)
@@ -131,11 +130,170 @@ __device__ __forceinline__ bool dense_share(const int32_t* __restrict__ seq_len,
     return false;
 }
 
+// ---- the end of a wave's run in the form DENSE_OWN ----
+// Partial results of the runs (written by other waves of this launch: device-coherent): [worker][G][HATA_D], and behind all of them
+// [worker][G][2], maximum and sum.
+//
+// Joins `nt` slices, 64 at a time: the states of all heads (lane: slice) and a first batch of channels are requested together, then come
+// the weights, then the rest.  KI: float4 of a lane, channels 4 (i % 32) .. of head i / 32, i = lane + 64 k (2 KI >= G heads);
+// M, L, sum: maximum, sum and channels so far.
+template <int KI, typename State, typename Slice>
+__device__ __forceinline__ void dense_own_join(int G, int nt, float* s_w, State state, Slice slice, float (&M)[2 * KI], float (&L)[2 * KI], float4 (&sum)[KI]) {
+    constexpr int U = KI == 8 ? 1 : 16 / KI;  // slices of a batch (registers)
+    const int lane = threadIdx.x & 63;
+    for (int s0 = 0; s0 < nt; s0 += 64) {
+        const int cnt = min(64, nt - s0);
+        uint2 st[2 * KI];
+#pragma unroll
+        for (int g = 0; g < 2 * KI; ++g) st[g] = state(min(g, G - 1), s0 + min(lane, cnt - 1));
+        float4 x[U][KI];
+        auto load = [&](int u0) {
+#pragma unroll
+            for (int u = 0; u < U; ++u)
+#pragma unroll
+                for (int k = 0; k < KI; ++k) x[u][k] = slice(min(lane + 64 * k, 32 * G - 1), s0 + min(u0 + u, cnt - 1));
+        };
+        load(0);
+        float f[2 * KI];
+#pragma unroll
+        for (int g = 0; g < 2 * KI; ++g) {
+            const float m = lane < cnt ? __uint_as_float(st[g].x) : HATA_NEG_INF, to = fmaxf(M[g], wave_max64(m));
+            const float w = m == HATA_NEG_INF ? 0.f : fast_exp2(m - to);
+            f[g] = M[g] == HATA_NEG_INF ? 1.f : fast_exp2(M[g] - to);  // (sums without a score are zero)
+            L[g] = fmaf(L[g], f[g], wave_sum64(lane < cnt ? w * __uint_as_float(st[g].y) : 0.f));
+            M[g] = to;
+            s_w[g * 64 + lane] = w;
+        }
+        __builtin_amdgcn_wave_barrier();
+#pragma unroll
+        for (int k = 0; k < KI; ++k) {
+            const float fk = lane < 32 ? f[2 * k] : f[2 * k + 1];
+            sum[k].x *= fk; sum[k].y *= fk; sum[k].z *= fk; sum[k].w *= fk;
+        }
+        for (int u0 = 0;;) {
+#pragma unroll
+            for (int u = 0; u < U; ++u)
+                if (u0 + u < cnt) {
+#pragma unroll
+                    for (int k = 0; k < KI; ++k) {
+                        const float w = s_w[(2 * k + lane / 32) * 64 + u0 + u];
+                        sum[k].x = fmaf(w, x[u][k].x, sum[k].x);
+                        sum[k].y = fmaf(w, x[u][k].y, sum[k].y);
+                        sum[k].z = fmaf(w, x[u][k].z, sum[k].z);
+                        sum[k].w = fmaf(w, x[u][k].w, sum[k].w);
+                    }
+                }
+            u0 += U;
+            if (u0 >= cnt) break;
+            load(u0);
+        }
+        __builtin_amdgcn_wave_barrier();
+    }
+}
+
+template <int VH, int NACC>
+__device__ __forceinline__ void dense_own_end(const DenseArgs& a, const DenseShare& d, char* ring, float m_run, float l_run, f32x4_t (&acc)[NACC],
+                                              const float* pre, int np, int np_row, int np_step, uint16_t* outp, float* outp32) {
+    const int lane = threadIdx.x & 63, n = lane & 15, kg = lane >> 4, G = a.G, ns = d.ns, nt = ns + np;
+    float* s_acc = reinterpret_cast<float*>(ring);  // [G][HATA_D + 4], of this wave alone
+    l_run = rows_sum4(l_run);
+    if constexpr (VH > 0) {
+#pragma unroll
+        for (int i = 0; i < 8 * VH; ++i) acc[i / 4][i % 4] = rows_sum4(acc[i / 4][i % 4]);
+        if (kg == 0) {
+#pragma unroll
+            for (int c = 0; c < 2 * VH; ++c)
+                *reinterpret_cast<float4*>(&s_acc[(n + c / 2) % VH * (HATA_D + 4) + 8 * n + 4 * (c & 1)]) = make_float4(acc[c][0], acc[c][1], acc[c][2], acc[c][3]);
+        }
+    } else if (n < G) {
+#pragma unroll
+        for (int c = 0; c < 8; ++c)  // acc[c][r] = O[head n][channel 16 c + 4 kg + r]
+            *reinterpret_cast<float4*>(&s_acc[n * (HATA_D + 4) + 16 * c + 4 * kg]) = make_float4(acc[c][0], acc[c][1], acc[c][2], acc[c][3]);
+    }
+    // (LDS serves a wave's accesses in order: what other lanes have written is there)
+    __builtin_amdgcn_wave_barrier();
+    float* part = a.partials + (int64_t)d.first * G * HATA_D;  // [ns][G][HATA_D]
+    float* states = a.partials + (int64_t)gridDim.x * DENSE_WAVES * G * HATA_D + (int64_t)d.first * G * 2;  // [ns][G][2]
+    if (ns > 1) {
+        float* p = part + (int64_t)d.split * G * HATA_D;
+        for (int i = lane; i < G * (HATA_D / 2); i += 64) {
+            const float2 v = *reinterpret_cast<const float2*>(&s_acc[i / (HATA_D / 2) * (HATA_D + 4) + i % (HATA_D / 2) * 2]);
+            st_dev(reinterpret_cast<unsigned long long*>(p + 2 * i), (unsigned long long)__float_as_uint(v.y) << 32 | __float_as_uint(v.x));
+        }
+        if (kg == 0 && n < G)
+            st_dev(reinterpret_cast<unsigned long long*>(states + (d.split * G + n) * 2),
+                   (unsigned long long)__float_as_uint(l_run) << 32 | __float_as_uint(m_run));
+        wait_stores();
+        int last = 0;
+        if (lane == 0) {
+            uint32_t* cnt = a.counter + ((int64_t)d.b * a.Hkv + d.h) * a.counter_stride;
+            last = atomicAdd(cnt, 1u) == (uint32_t)(ns - 1);
+            if (last) *cnt = 0;
+        }
+        if (!__builtin_amdgcn_readfirstlane(last)) return;
+    }
+    // (the only run of its unit begins with what it has, the last of several with the first of them)
+    const int own = ns > 1 ? ns : 0;
+    const int64_t pre_step = (int64_t)np_step * a.pre_rows * (HATA_D + 2);
+    auto state = [&](int g, int s) -> uint2 {
+        if (s < own) return ld_dev_u2(states + (s * G + g) * 2);
+        return *reinterpret_cast<const uint2*>(pre + (s - own) * pre_step + (int64_t)a.pre_rows * HATA_D + 2 * (np_row + g));
+    };
+    auto slice = [&](int i, int s) -> float4 {  // four channels
+        if (s < own) {
+            const float* p = part + (int64_t)s * G * HATA_D + 4 * i;
+            const uint2 x = ld_dev_u2(p), y = ld_dev_u2(p + 2);
+            return make_float4(__uint_as_float(x.x), __uint_as_float(x.y), __uint_as_float(y.x), __uint_as_float(y.y));
+        }
+        return *reinterpret_cast<const float4*>(pre + (s - own) * pre_step + np_row * HATA_D + 4 * i);
+    };
+    auto join = [&](auto ki) {
+        constexpr int KI = decltype(ki)::value;
+        float M[2 * KI], L[2 * KI];
+        float4 sum[KI];
+#pragma unroll
+        for (int g = 0; g < 2 * KI; ++g) {
+            const int from = VH ? min(g, VH - 1) : g;  // (the lane that has head g's state)
+            M[g] = own ? HATA_NEG_INF : __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(m_run), from));
+            L[g] = own ? 0.f : __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(l_run), from));
+        }
+#pragma unroll
+        for (int k = 0; k < KI; ++k) {
+            const int i = min(lane + 64 * k, 32 * G - 1);
+            sum[k] = own ? make_float4(0.f, 0.f, 0.f, 0.f) : *reinterpret_cast<const float4*>(&s_acc[i / 32 * (HATA_D + 4) + i % 32 * 4]);
+        }
+        __builtin_amdgcn_wave_barrier();
+        dense_own_join<KI>(G, own + np, s_acc, state, slice, M, L, sum);
+#pragma unroll
+        for (int k = 0; k < KI; ++k) {
+            const int i = lane + 64 * k;
+            const float l = lane < 32 ? L[2 * k] : L[2 * k + 1];
+            if (i < 32 * G) {
+                float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+                if (l != 0.f) o = make_float4(sum[k].x / l, sum[k].y / l, sum[k].z / l, sum[k].w / l);
+                *reinterpret_cast<uint2*>(outp + 4 * i) = make_uint2(f32_to_bf16(o.x) | f32_to_bf16(o.y) << 16, f32_to_bf16(o.z) | f32_to_bf16(o.w) << 16);
+                if (outp32) *reinterpret_cast<float4*>(outp32 + 4 * i) = o;
+            }
+        }
+    };
+    if (G <= 2) join(std::integral_constant<int, 1>());
+    else if (G <= 4) join(std::integral_constant<int, 2>());
+    else if (G <= 8) join(std::integral_constant<int, 4>());
+    else join(std::integral_constant<int, 8>());
+}
+
 enum DenseForm { DENSE_BF16X2, DENSE_FP32_ONE_HEAD, DENSE_FP32_TWO_HEADS, DENSE_FP32 };
-// PAGED: the rows lie in pools of pages.  A tile of 16 rows lies inside a page, so a wave looks up one page a tile, 64 tiles'
+// DENSE_PAGED: the rows lie in pools of pages.  A tile of 16 rows lies inside a page, so a wave looks up one page a tile, 64 tiles'
 // at a time (a lane each).
-template <DenseForm FORM, bool PAGED>
+// DENSE_OWN: the same, for the rows that sequences do not share (prefix_kernel has been at the others).  They are few for many
+// units, so what is dealt out are runs for single waves, not for workgroups: each has a unit, a run of tiles and partial results
+// of its own, meets no other wave, and the last one of a unit to arrive joins them and the shared rows'.  256 sequences with
+// some 250 rows behind shared ones, 8 KV heads, groups of 8: a workgroup per unit 171 us, ONE_OWN_US.
+enum DenseRows { DENSE_CONTIGUOUS, DENSE_PAGED, DENSE_OWN };
+template <DenseForm FORM, DenseRows ROWS>
 __global__ __launch_bounds__(DENSE_WAVES * 64) void dense_kernel(const DenseArgs a) {
+    constexpr bool PAGED = ROWS != DENSE_CONTIGUOUS, OWN = ROWS == DENSE_OWN;
+    constexpr int STEP = OWN ? 1 : DENSE_WAVES;  // between the tiles of a wave
     // ring[wave][DENSE_RING][DENSE_TILE_BYTES]; afterwards the waves' states, the merge weights and sums
     extern __shared__ __attribute__((aligned(16))) char smem[];
     __shared__ float s_m[DENSE_WAVES][16], s_l[DENSE_WAVES][16];
@@ -143,7 +301,37 @@ __global__ __launch_bounds__(DENSE_WAVES * 64) void dense_kernel(const DenseArgs
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int n = lane & 15, kg = lane >> 4;
     DenseShare d;
-    if (!dense_share(a.seq_len, PAGED ? a.info : nullptr, a.B, a.Hkv, a.L_cap, d)) return;
+    int row_first = 0;  // rows in front of this sequence's own, and the partial results of those
+    [[maybe_unused]] int np = 0, np_row = 0, np_step = 0;
+    [[maybe_unused]] const float* pre = nullptr;
+    if constexpr (OWN) {
+        const int worker = blockIdx.x * DENSE_WAVES + wave;
+        PrefixPlan x;
+        for (int b0 = 0;; b0 += 64) {
+            if (b0 >= a.B) return;  // nothing left for this wave
+            x = a.plan[min(b0 + lane, a.B - 1)];
+            const unsigned long long mine = __builtin_amdgcn_ballot_w64(b0 + lane < a.B && worker < x.start + x.runs * a.Hkv);
+            if (mine) {
+                const int l = __ffsll(mine) - 1;
+                d.b = b0 + l;
+                for (int* v : {&x.start, &x.runs, &x.rows, &x.first, &x.item, &x.splits, &x.row, &x.step}) *v = __builtin_amdgcn_readlane(*v, l);
+                break;
+            }
+        }
+        const int in = worker - x.start;
+        d.L = x.rows;
+        d.ns = x.runs;
+        d.h = in / x.runs;
+        d.split = in - d.h * x.runs;
+        d.first = worker - d.split;
+        row_first = x.first;
+        np = x.splits;
+        np_row = x.row;
+        np_step = x.step;
+        pre = a.pre + (x.item + (int64_t)d.h * np * np_step) * a.pre_rows * (HATA_D + 2);
+    } else if (!dense_share(a.seq_len, a.B, a.Hkv, a.L_cap, d)) {
+        return;
+    }
     const int split = d.split, ns = d.ns, h = d.h, b = d.b, L = d.L, G = a.G;
     const int64_t u = (int64_t)b * a.Hkv + h, hq0 = (int64_t)b * a.Hq + (int64_t)h * G;
     uint16_t* outp = a.out + hq0 * HATA_D;
@@ -154,19 +342,8 @@ __global__ __launch_bounds__(DENSE_WAVES * 64) void dense_kernel(const DenseArgs
 #pragma unroll
         for (int s = 0; s < 4; ++s) qb[s] = *reinterpret_cast<const uint4*>(q0 + 32 * s);
     }
-    // rows in front of this sequence's own, and the partial results of those
-    int row_first = 0, np = 0, np_row = 0, np_step = 0;
-    const float* pre = nullptr;
-    if (PAGED && a.info) {
-        const int4 x = a.info[b];
-        row_first = x.x;
-        np = x.z & 0xffff;
-        np_row = x.z >> 16;
-        np_step = x.w;
-        pre = a.pre + (x.y + (int64_t)h * np * np_step) * a.pre_rows * (HATA_D + 2);
-    }
     if (L == 0 && np == 0) {  // no row at all
-        for (int i = tid; i < G * HATA_D; i += DENSE_WAVES * 64) {
+        for (int i = OWN ? lane : tid; i < G * HATA_D; i += OWN ? 64 : DENSE_WAVES * 64) {
             outp[i] = 0;
             if (outp32) outp32[i] = 0.f;
         }
@@ -174,7 +351,7 @@ __global__ __launch_bounds__(DENSE_WAVES * 64) void dense_kernel(const DenseArgs
     }
     const int tiles = (L + 15) / 16;  // in even runs
     const int t_begin = (int)((int64_t)tiles * split / ns), t_end = (int)((int64_t)tiles * (split + 1) / ns);
-    const int mine = max(0, (t_end - t_begin - wave + DENSE_WAVES - 1) / DENSE_WAVES);  // tiles t_begin + wave + 8 j
+    const int t_wave = t_begin + (OWN ? 0 : wave), mine = max(0, (t_end - t_wave + STEP - 1) / STEP);  // tiles t_wave + STEP j
 
     const uint16_t* Kb = PAGED ? a.K : a.K + b * a.sb + h * a.sh;
     const uint16_t* Vb = PAGED ? a.V : a.V + b * a.sb + h * a.sh;
@@ -187,11 +364,11 @@ __global__ __launch_bounds__(DENSE_WAVES * 64) void dense_kernel(const DenseArgs
 #pragma unroll
     for (int i = 0; i < 4; ++i) off[i] = (4 * i + kg) * sn + (n ^ dense_swizzle(4 * i + kg)) * 8;
     auto request = [&](int j) {
-        const int row0 = (t_begin + wave + DENSE_WAVES * j) * 16;
+        const int row0 = (t_wave + STEP * j) * 16;
         int64_t at = row0 * sn;
         if constexpr (PAGED) {
             if (j % 64 == 0) {
-                const int n0 = row_first + min(row0 + lane * (16 * DENSE_WAVES), L - 1);
+                const int n0 = row_first + min(row0 + lane * (16 * STEP), L - 1);
                 page = clampi(a.pv.table[(int64_t)b * a.pv.max_blocks + (n0 >> a.pv.shift)], 0, a.pv.n_pages - 1);
             }
             const int p = __builtin_amdgcn_readlane(page, j % 64);
@@ -239,7 +416,7 @@ __global__ __launch_bounds__(DENSE_WAVES * 64) void dense_kernel(const DenseArgs
     auto compute = [&](int j) {
         const char* t = ring + (j % DENSE_RING) * DENSE_TILE_BYTES;
         const int after = mine - 1 - j;
-        const int left = min(L - (t_begin + wave + DENSE_WAVES * j) * 16, 16);
+        const int left = min(L - (t_wave + STEP * j) * 16, 16);
         wait_tile<4>(after);
         // (fp32 forms: four sums of 32 channels instead of one of 128, for the same reason as above)
         f32x4_t sacc, part[4];
@@ -366,6 +543,10 @@ __global__ __launch_bounds__(DENSE_WAVES * 64) void dense_kernel(const DenseArgs
     }
     for (int j = 0; j < mine; ++j) compute(j);
 
+    if constexpr (OWN) {
+        dense_own_end<VH>(a, d, ring, m_run, l_run, acc, pre, np, np_row, np_step, outp, outp32);
+        return;
+    }
     // ---- the eight states of the workgroup ----
     __syncthreads();  // the ring is no longer read
     float* s_acc = reinterpret_cast<float*>(smem);  // [DENSE_WAVES][G][HATA_D + 4]
@@ -402,7 +583,7 @@ __global__ __launch_bounds__(DENSE_WAVES * 64) void dense_kernel(const DenseArgs
             av = fmaf(f, s_acc[(w * G + g) * (HATA_D + 4) + ch], av);
             l = fmaf(f, s_l[w][g], l);
         }
-        if (ns + np == 1) {
+        if (ns == 1) {
             const float o = l > 0.f ? av / l : 0.f;
             outp[i] = (uint16_t)f32_to_bf16(o);
             if (outp32) outp32[i] = o;
@@ -412,7 +593,7 @@ __global__ __launch_bounds__(DENSE_WAVES * 64) void dense_kernel(const DenseArgs
             if (ch == 0) { st_dev(pp, M); st_dev(pp + 1, l); }
         }
     }
-    if (ns + np == 1) return;
+    if (ns == 1) return;
     // ---- the last workgroup of the unit merges (partials: write-through stores, device-coherent loads) ----
     wait_stores();
     __syncthreads();
@@ -424,76 +605,67 @@ __global__ __launch_bounds__(DENSE_WAVES * 64) void dense_kernel(const DenseArgs
     }
     __syncthreads();
     if (!s_last) return;
-    // thread: slices part, part + parts, ... of one head's channel pair; the first batch of loads before the weights.  Behind the
-    // unit's own slices come those of the rows in front (np, PAGED)
-    const int nt = PAGED ? ns + np : ns;
-    float* s_w = reinterpret_cast<float*>(smem);                    // [G][nt] normalised weights
-    float2* s_sum = reinterpret_cast<float2*>(s_w + ((G * nt + 3) & ~3));  // [parts][G * 64]
+    // thread: slices part, part + parts, ... of one head's channel pair; the first batch of loads before the weights
+    float* s_w = reinterpret_cast<float*>(smem);                    // [G][ns] normalised weights
+    float2* s_sum = reinterpret_cast<float2*>(s_w + ((G * ns + 3) & ~3));  // [parts][G * 64]
     const int items = G * (HATA_D / 2);
     const int parts = max(1, DENSE_WAVES * 64 / items);
-    auto slice = [&](int g, int ch, int s) -> uint2 {  // two channels of slice s
-        if (PAGED && s >= ns)
-            return *reinterpret_cast<const uint2*>(pre + (int64_t)(s - ns) * np_step * a.pre_rows * (HATA_D + 2) + (np_row + g) * HATA_D + ch);
-        return ld_dev_u2(part0 + g * head_stride + 2 + ch + (int64_t)s * HATA_PSTRIDE);
+    auto address = [&](int i) {
+        return part0 + (i / (HATA_D / 2)) * head_stride + 2 + 2 * (i % (HATA_D / 2));
     };
-    auto state = [&](int g, int s) -> uint2 {  // its maximum and sum
-        if (PAGED && s >= ns)
-            return *reinterpret_cast<const uint2*>(pre + ((int64_t)(s - ns) * np_step * (HATA_D + 2) + HATA_D) * a.pre_rows + 2 * (np_row + g));
-        return ld_dev_u2(part0 + g * head_stride + (int64_t)s * HATA_PSTRIDE);
-    };
-    constexpr int NML = PAGED ? 8 : 4;  // slices of a lane: DENSE_MAX_RUNS, and as many in front
     for (int i0 = 0; i0 < items; i0 += DENSE_WAVES * 64) {  // (more than once with more than 8 heads)
         const int item = min(i0 + (parts > 1 ? tid % items : tid), items - 1), part = parts > 1 ? tid / items : 0;
-        const int ig = item / (HATA_D / 2), ich = 2 * (item % (HATA_D / 2));
+        const float* pp = address(item);
         uint2 x[DENSE_BATCH];
         if (part < parts) {
 #pragma unroll
             for (int k = 0; k < DENSE_BATCH; ++k) {
                 const int s = part + k * parts;
-                x[k] = s < nt ? slice(ig, ich, s) : make_uint2(0, 0);
+                x[k] = s < ns ? ld_dev_u2(pp + (int64_t)s * HATA_PSTRIDE) : make_uint2(0, 0);
             }
         }
         if (i0 == 0) {
             for (int g = wave; g < G; g += DENSE_WAVES) {
-                uint2 ml[NML];
+                const float* mp = part0 + g * head_stride;
+                uint2 ml[4];
 #pragma unroll
-                for (int t = 0; t < NML; ++t)
-                    if (t * 64 < nt) ml[t] = state(g, min(lane + 64 * t, nt - 1));
+                for (int t = 0; t < 4; ++t)
+                    if (t * 64 < ns) ml[t] = ld_dev_u2(mp + (int64_t)min(lane + 64 * t, ns - 1) * HATA_PSTRIDE);
                 float M = HATA_NEG_INF;
 #pragma unroll
-                for (int t = 0; t < NML; ++t)
-                    if (lane + 64 * t < nt) M = fmaxf(M, __uint_as_float(ml[t].x));
+                for (int t = 0; t < 4; ++t)
+                    if (lane + 64 * t < ns) M = fmaxf(M, __uint_as_float(ml[t].x));
                 M = wave_max64(M);
-                float w[NML], l = 0.f;
+                float w[4], l = 0.f;
 #pragma unroll
-                for (int t = 0; t < NML; ++t) {
-                    w[t] = lane + 64 * t < nt && M != HATA_NEG_INF ? fast_exp2(__uint_as_float(ml[t].x) - M) : 0.f;
-                    if (lane + 64 * t < nt) l = fmaf(w[t], __uint_as_float(ml[t].y), l);
+                for (int t = 0; t < 4; ++t) {
+                    w[t] = lane + 64 * t < ns && M != HATA_NEG_INF ? fast_exp2(__uint_as_float(ml[t].x) - M) : 0.f;
+                    if (lane + 64 * t < ns) l = fmaf(w[t], __uint_as_float(ml[t].y), l);
                 }
                 l = wave_sum64(l);
                 const float inv = l > 0.f ? 1.f / l : 0.f;
 #pragma unroll
-                for (int t = 0; t < NML; ++t)
-                    if (lane + 64 * t < nt) s_w[g * nt + lane + 64 * t] = w[t] * inv;
+                for (int t = 0; t < 4; ++t)
+                    if (lane + 64 * t < ns) s_w[g * ns + lane + 64 * t] = w[t] * inv;
             }
             __syncthreads();
         }
         float2 sum = make_float2(0.f, 0.f);
         if (part < parts) {
-            const float* w = s_w + ig * nt;
+            const float* w = s_w + item / (HATA_D / 2) * ns;
             for (int s0 = part;;) {
 #pragma unroll
                 for (int k = 0; k < DENSE_BATCH; ++k) {
-                    const float f = w[min(s0 + k * parts, nt - 1)];  // (x is zero past the end)
+                    const float f = w[min(s0 + k * parts, ns - 1)];  // (x is zero past the end)
                     sum.x = fmaf(f, __uint_as_float(x[k].x), sum.x);
                     sum.y = fmaf(f, __uint_as_float(x[k].y), sum.y);
                 }
                 s0 += DENSE_BATCH * parts;
-                if (s0 >= nt) break;
+                if (s0 >= ns) break;
 #pragma unroll
                 for (int k = 0; k < DENSE_BATCH; ++k) {
                     const int s = s0 + k * parts;
-                    x[k] = s < nt ? slice(ig, ich, s) : make_uint2(0, 0);
+                    x[k] = s < ns ? ld_dev_u2(pp + (int64_t)s * HATA_PSTRIDE) : make_uint2(0, 0);
                 }
             }
         }
@@ -531,15 +703,17 @@ static int dense_splits(int64_t units, int L_cap) {
 }
 
 hipError_t prepare_dense() {  // (more than 64 KB of dynamic LDS has to be asked for)
-    for (const void* fn : {(const void*)dense_kernel<DENSE_BF16X2, false>, (const void*)dense_kernel<DENSE_FP32, false>,
-                           (const void*)dense_kernel<DENSE_FP32_ONE_HEAD, false>, (const void*)dense_kernel<DENSE_FP32_TWO_HEADS, false>,
-                           (const void*)dense_kernel<DENSE_BF16X2, true>, (const void*)dense_kernel<DENSE_FP32, true>,
-                           (const void*)dense_kernel<DENSE_FP32_ONE_HEAD, true>, (const void*)dense_kernel<DENSE_FP32_TWO_HEADS, true>}) {
+#define HATA_DENSE_ROWS(F_) (const void*)dense_kernel<F_, DENSE_CONTIGUOUS>, (const void*)dense_kernel<F_, DENSE_PAGED>, (const void*)dense_kernel<F_, DENSE_OWN>
+    for (const void* fn : {HATA_DENSE_ROWS(DENSE_BF16X2), HATA_DENSE_ROWS(DENSE_FP32), HATA_DENSE_ROWS(DENSE_FP32_ONE_HEAD),
+                           HATA_DENSE_ROWS(DENSE_FP32_TWO_HEADS)}) {
         const hipError_t e = hipFuncSetAttribute(fn, hipFuncAttributeMaxDynamicSharedMemorySize, (int)dense_lds());
         if (e != hipSuccess) return e;
     }
+#undef HATA_DENSE_ROWS
     return hipSuccess;
 }
+
+int dense_own_wgs(int B, int Hkv) { return std::max(256, (B * Hkv + DENSE_WAVES - 1) / DENSE_WAVES); }
 
 hipError_t launch_dense(const hata_ctx* c, const void* q, const void* K, const void* V, const int32_t* seq_len, int B,
                         float sm_scale, void* out, float* out_f32, hipStream_t s, const PageView* pages, int pre_rows) {
@@ -552,7 +726,7 @@ hipError_t launch_dense(const hata_ctx* c, const void* q, const void* K, const v
     a.Hq = f.Hq; a.Hkv = f.Hkv; a.G = c->G; a.L_cap = f.L_cap;
     a.B = B;
     a.pv = PageView{nullptr, 0, 0, 0};
-    a.info = pre_rows ? (const int4*)c->prefix_info : nullptr;
+    a.plan = c->prefix_plan;
     a.pre = c->prefix_part;
     a.pre_rows = pre_rows;
     if (pages) {
@@ -564,8 +738,8 @@ hipError_t launch_dense(const hata_ctx* c, const void* q, const void* K, const v
     const int64_t spare = splits == 1 && B > 1 ? std::max((int64_t)0, std::min((int64_t)256, c->dense_wgs_max - units)) : 0;
     a.sb = f.kv_stride_b; a.sh = f.kv_stride_h; a.sn = f.kv_stride_n;
     a.scale_log2 = sm_scale * 1.4426950408889634f;
-    const dim3 grid = B == 1 ? dim3((unsigned)splits, f.Hkv) : dim3((unsigned)(units * splits + spare));
-#define HATA_DENSE_FORM(F_) (pages ? dense_kernel<F_, true> : dense_kernel<F_, false>)
+    const dim3 grid = pre_rows ? dim3((unsigned)dense_own_wgs(B, f.Hkv)) : B == 1 ? dim3((unsigned)splits, f.Hkv) : dim3((unsigned)(units * splits + spare));
+#define HATA_DENSE_FORM(F_) (pre_rows ? dense_kernel<F_, DENSE_OWN> : pages ? dense_kernel<F_, DENSE_PAGED> : dense_kernel<F_, DENSE_CONTIGUOUS>)
     const auto fn = c->HT >= 4 ? HATA_DENSE_FORM(DENSE_BF16X2) : c->G == 1 ? HATA_DENSE_FORM(DENSE_FP32_ONE_HEAD)
                     : c->G == 2 ? HATA_DENSE_FORM(DENSE_FP32_TWO_HEADS) : HATA_DENSE_FORM(DENSE_FP32);
 #undef HATA_DENSE_FORM

@@ -13,6 +13,15 @@
 // dense attention: at most this many rounds of one workgroup per CU, with a partial result each
 #define HATA_DENSE_ROUNDS 4
 
+namespace hata {
+// Of a sequence in a call with groups that share rows: its rows behind the shared ones, in `runs` runs a KV head for a wave each (waves
+// start .. start + runs * Hkv - 1 of the launch), and the partial results of the shared rows: `splits` a KV head from item on, `step`
+// apart, its query rows from `row` on
+struct PrefixPlan {
+    int start, runs, rows, first, item, splits, row, step;
+};
+}  // namespace hata
+
 struct hata_ctx {
     hata_config cfg;
     int G;            // query heads per KV head
@@ -56,7 +65,7 @@ struct hata_ctx {
     int coop_opt_cap_paged[4];  // the same for the block-table variant of the kernel
     float* partials;       // [B_max*Hq, max(sparse_splits, n_chunks), d + 2], at least 256 * HATA_DENSE_ROUNDS * G rows
     float* prefix_part;    // partial results of rows that groups of sequences share (prefix_part_floats)
-    int32_t* prefix_info;  // [B_max, 4] where a sequence finds its own among them
+    hata::PrefixPlan* prefix_plan;  // [B_max] what is left to the sequences themselves, and where they find their own among those
     void* wplanes;               // [Hkv, r/32, 8, 2, 64] 16-byte fragments: the two scaled fp16 planes of the hash weights (prefill key encode)
     const float* prepared_W_H;   // the weight tensor those planes were made from (nullptr: none)
     size_t control_bytes;  // bytes from chunk_info up to the partials: the control words, cleared at creation and after a give-up
@@ -95,9 +104,10 @@ hipError_t prepare_dense();  // once per context
 hipError_t launch_dense(const hata_ctx* c, const void* q, const void* K, const void* V, const int32_t* seq_len, int B,
                         float sm_scale, void* out, float* out_f32, hipStream_t s, const PageView* pages = nullptr, int pre_rows = 0);
 // Rows that groups of sequences share, in front of launch_dense of the same call: partial results in prefix_part, *part_rows (which
-// launch_dense is then given as pre_rows) query rows each, and in prefix_info where a sequence finds its own
+// launch_dense is then given as pre_rows) query rows each, and prefix_plan
 #define HATA_PREFIX_GROUPS 1024  // groups beyond share nothing
 size_t prefix_part_floats(int B, int Hkv, int G);
+int dense_own_wgs(int B, int Hkv);  // workgroups of the launch behind
 hipError_t prepare_prefix();  // once per context
 hipError_t launch_prefix(const hata_ctx* c, const void* q, const void* K, const void* V, const PageView& pages, const int32_t* seq_len, int B,
                          const int32_t* group_start, const int32_t* shared_len, int n_groups, float sm_scale, int* part_rows, hipStream_t s);

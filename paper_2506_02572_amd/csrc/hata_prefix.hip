@@ -8,7 +8,9 @@
 //     192 registers) and goes over 32 rows at a time on v_mfma_f32_32x32x16_bf16: S^T = K Q^T, O^T += V^T P^T.  In S^T a lane has 16
 //     rows of ONE query row, which are what the second product wants from it as P: nothing crosses lanes.
 //   - WQ waves share what they read (rows come into LDS by direct loads, 64 of K and of V a stage), 4 / WQ go over different rows.
-//   - The maximum is followed loosely: a wave scales its sums only where a score passes the one in use by 2^8.
+//   - The maximum is followed loosely: a wave scales its sums (1500 cycles, as much as the products of 32 rows) only where a score
+//     passes the one in use by 2^40.  Sums and weights are floating-point numbers, nothing is lost by it as long as no value is as
+//     large as 2^70 (2^127 less the weight and 2^17 rows).
 //   - Weights are rounded to bf16 (to nearest: half a step, 2^-8 relative; their sum is of the rounded ones), which halves the second
 //     product against two terms, and the matrix cores are what bounds groups of more than some 200 query rows a KV head.
 #include <algorithm>
@@ -23,15 +25,16 @@ typedef __attribute__((ext_vector_type(2))) float f32x2_t;
 
 #define PREFIX_TILE 64       // rows that runs are cut by; what is left of the common rows is read by every sequence itself
 #define PREFIX_MAX_SPLITS 256
+#define PREFIX_LOOSE 40.f
 #define PREFIX_LDS (4 * 64 * (HATA_D + 4) * 4)  // the waves' sums at the end; before, the ring of stages
 
 struct PrefixArgs {
     const uint16_t *q, *K, *V;
     const int32_t *seq_len, *group_start, *shared_len;
-    int4* info;
+    PrefixPlan* plan;
     float* part;
     PageView pv;
-    int B, Hq, Hkv, G, L_cap, n_groups;
+    int B, Hq, Hkv, G, L_cap, n_groups, own_waves;  // own_waves: of the launch behind
     float scale_log2;
 };
 
@@ -39,110 +42,192 @@ struct PrefixArgs {
 //
 // Every workgroup works it out for itself: the groups' members, the rows they have in common, and the shortest run (in tiles) at
 // which the launch's workgroups suffice, one per (group, KV head, tile of query rows, run).  The tiles of query rows of a run are
-// neighbours on one XCD, whose L2 then serves all but the first of them.
+// neighbours on one XCD, whose L2 then serves all but the first of them.  The last workgroup writes the plan that the launch behind
+// goes by.  (A workgroup more than there are compute units would have to wait for one.)  It has nothing else to do, unless runs
+// would be longer by more than an eighth for that.
 struct PrefixShare { int g, h, split, ns, qt, tiles, item, first, members, lead; };
+struct PrefixGroups { int *start, *least, *count, *lead; };  // in LDS: first member [n + 1]; tiles in common, members that have rows, the first of them [n]
 
-__device__ __forceinline__ bool prefix_share(const PrefixArgs& a, int mpt, int* lds, PrefixShare& w) {
-    const int n = a.n_groups, tid = threadIdx.x, lane = tid & 63;
-    int* start = lds;            // [n + 1] first member
-    int* least = start + n + 1;  // [n] rows of the shortest member that has rows; afterwards tiles in common
-    int* count = least + n;      // [n] members that have rows
-    int* lead = count + n;       // [n] the first of them
+__device__ __forceinline__ PrefixGroups prefix_groups(const PrefixArgs& a, int* lds) {
+    const int n = a.n_groups, tid = threadIdx.x;
+    int* start = lds;
+    int* least = start + n + 1;
+    int* count = least + n;
+    int* lead = count + n;
+    int* shared = lead + n;
+    const int own = a.seq_len[min(tid, a.B - 1)];  // (on its way with the groups')
     for (int i = tid; i <= n; i += 256) {
         start[i] = clampi(a.group_start[i], 0, a.B);
-        if (i < n) { least[i] = 0x7fffffff; count[i] = 0; lead[i] = 0x7fffffff; }
+        if (i < n) { least[i] = 0x7fffffff; count[i] = 0; lead[i] = 0x7fffffff; shared[i] = a.shared_len[i]; }
     }
     __syncthreads();
-    for (int o = 1; o <= n; o <<= 1) {  // ascending, whatever the caller gave
-        int v[HATA_PREFIX_GROUPS / 256 + 1];
-#pragma unroll
-        for (int k = 0; k < HATA_PREFIX_GROUPS / 256 + 1; ++k) {
-            const int i = tid + 256 * k;
-            v[k] = i <= n ? max(start[i], i >= o ? start[i - o] : 0) : 0;
-        }
-        __syncthreads();
-#pragma unroll
-        for (int k = 0; k < HATA_PREFIX_GROUPS / 256 + 1; ++k)
-            if (tid + 256 * k <= n) start[tid + 256 * k] = v[k];
+    int falls = 0;
+    for (int i = tid; i < n; i += 256) falls |= start[i] > start[i + 1];
+    if (__syncthreads_or(falls)) {  // ascending, whatever the caller gave
+        if (tid == 0)
+            for (int i = 1; i <= n; ++i) start[i] = max(start[i], start[i - 1]);
         __syncthreads();
     }
-    auto group_of = [&](int b) {  // -1: none
-        if (b < start[0] || b >= start[n]) return -1;
-        int lo = 0, c = n;  // the last group that begins at b or before
-        while (c > 1) {
-            const int half = c / 2;
-            if (start[lo + half] <= b) { lo += half; c -= half; }
-            else c = half;
+    for (int b0 = 0; b0 < a.B; b0 += 256) {
+        const int b = b0 + tid, L = b < a.B ? clampi(b0 ? a.seq_len[b] : own, 0, a.L_cap) : 0;
+        int g = -1;
+        if (L > 0 && b >= start[0] && b < start[n]) {
+            int c = n;  // the last group that begins at b or before
+            g = 0;
+            while (c > 1) {
+                const int h = c / 2;
+                if (start[g + h] <= b) { g += h; c -= h; }
+                else c = h;
+            }
         }
-        return lo;
-    };
-    for (int b = start[0] + tid; b < start[n]; b += 256) {
-        const int L = clampi(a.seq_len[b], 0, a.L_cap), g = group_of(b);
-        if (L > 0) {
+        const unsigned long long some = __builtin_amdgcn_ballot_w64(g >= 0);
+        if (!some) continue;
+        const int l0 = __ffsll(some) - 1, g0 = __builtin_amdgcn_readlane(g, l0);
+        if (__builtin_amdgcn_ballot_w64(g >= 0 && g != g0) == 0ull) {  // a wave of one group (lengths are below 2^24)
+            const int low = (int)-wave_max64(g >= 0 ? -(float)L : HATA_NEG_INF);
+            if ((tid & 63) == l0) {
+                atomicMin(&least[g], low);
+                atomicAdd(&count[g], __popcll(some));
+                atomicMin(&lead[g], b);
+            }
+        } else if (g >= 0) {
             atomicMin(&least[g], L);
             atomicAdd(&count[g], 1);
             atomicMin(&lead[g], b);
         }
     }
     __syncthreads();
-    for (int g = tid; g < n; g += 256) least[g] = count[g] >= 2 ? max(min(a.shared_len[g], least[g]), 0) / PREFIX_TILE : 0;
+    for (int g = tid; g < n; g += 256) least[g] = count[g] >= 2 ? max(min(shared[g], least[g]), 0) / PREFIX_TILE : 0;
     __syncthreads();
-    auto qtiles = [&](int g) { return (start[g + 1] - start[g] + mpt - 1) / mpt; };
-    auto splits = [&](int g, int run) { return min((least[g] + run - 1) / run, PREFIX_MAX_SPLITS); };
-    int64_t all = 0;
-    int longest = 1;
+    return PrefixGroups{start, least, count, lead};
+}
+
+// The run length, and through `each` the groups of every 64 (lane: group g, its tiles of query rows, its runs, its first item)
+template <typename Each>
+__device__ __forceinline__ void prefix_items(const PrefixArgs& a, const PrefixGroups& s, int mpt, int wgs, Each each) {
+    const int n = a.n_groups, lane = threadIdx.x & 63;
+    auto qtiles = [&](int g) { return g < n ? (s.start[g + 1] - s.start[g] + mpt - 1) / mpt : 0; };
+    auto tiles = [&](int g) { return g < n ? s.least[g] : 0; };
+    const int qt0 = qtiles(lane), tiles0 = tiles(lane);  // (all there is, mostly)
+    float all = wave_sum64((float)qt0 * tiles0), longest = wave_max64((float)tiles0);
+    for (int g0 = 64; g0 < n; g0 += 64) {
+        all += wave_sum64((float)qtiles(g0 + lane) * tiles(g0 + lane));
+        longest = fmaxf(longest, wave_max64((float)tiles(g0 + lane)));
+    }
+    auto splits = [](int t, int run) { return min((t + run - 1) / run, PREFIX_MAX_SPLITS); };
+    int run = max(1, (int)ceilf(all * (float)a.Hkv / (float)wgs)), with_last = 0;
+    for (;; run += max(1, run >> 4)) {
+        uint32_t items = (uint32_t)__builtin_amdgcn_readlane((int)wave_incl_scan((uint32_t)(qt0 * splits(tiles0, run))), 63);
+        for (int g0 = 64; g0 < n; g0 += 64)
+            items += (uint32_t)__builtin_amdgcn_readlane((int)wave_incl_scan((uint32_t)(qtiles(g0 + lane) * splits(tiles(g0 + lane), run))), 63);
+        items *= (uint32_t)a.Hkv;
+        if (items == (uint32_t)wgs && !with_last) with_last = run;  // (the workgroup with the plan would have an item too)
+        if (items < (uint32_t)wgs || run >= (int)longest) break;
+    }
+    if (with_last && 8 * run > 9 * with_last) run = with_last;
+    uint32_t base = 0;
     for (int g0 = 0; g0 < n; g0 += 64) {
-        const int g = g0 + lane;
-        all += (int64_t)wave_sum64(g < n ? (float)qtiles(g) * least[g] : 0.f);
-        longest = max(longest, (int)wave_max64(g < n ? (float)least[g] : 0.f));
+        const int g = g0 + lane, qt = g0 ? qtiles(g) : qt0, ns = splits(g0 ? tiles(g) : tiles0, run);
+        const uint32_t upto = wave_incl_scan((uint32_t)(a.Hkv * qt * ns));
+        if (each(g, qt, ns, (int)(base + upto) - a.Hkv * qt * ns)) return;
+        base += (uint32_t)__builtin_amdgcn_readlane((int)upto, 63);
     }
-    const int wgs = gridDim.x;
-    int run = (int)max((int64_t)1, (all * a.Hkv + wgs - 1) / wgs);
-    for (;; run += max(1, run >> 3)) {
-        uint32_t items = 0;
-        for (int g0 = 0; g0 < n; g0 += 64) {
-            const int g = g0 + lane;
-            items += (uint32_t)__builtin_amdgcn_readlane((int)wave_incl_scan(g < n ? (uint32_t)(qtiles(g) * splits(g, run)) : 0u), 63);
-        }
-        if (items * (uint32_t)a.Hkv <= (uint32_t)wgs || run >= longest) break;
-    }
-    // this workgroup's item, and for the first workgroup where every sequence finds its group's partial results
+}
+
+__device__ __forceinline__ bool prefix_share(const PrefixArgs& a, int mpt, int* lds, PrefixShare& w) {
     const int item = (int)((blockIdx.x % 8) * (gridDim.x / 8) + blockIdx.x / 8);
-    int base = 0;
+    const PrefixGroups s = prefix_groups(a, lds);
     w.g = -1;
-    for (int g = 0; g < n; ++g) {
-        const int qt = qtiles(g), ns = splits(g, run), items = a.Hkv * qt * ns;
-        if (blockIdx.x == 0) {
-            for (int b = start[g] + tid; b < start[g + 1]; b += 256) {
-                const int i = b - start[g];
-                const bool some = ns > 0 && clampi(a.seq_len[b], 0, a.L_cap) > 0;
-                a.info[b] = some ? make_int4(least[g] * PREFIX_TILE, base + i / mpt, ns | (i % mpt * a.G) << 16, qt) : make_int4(0, 0, 0, 0);
+    prefix_items(a, s, mpt, gridDim.x, [&](int g, int qt, int ns, int base) {
+        const unsigned long long here = __builtin_amdgcn_ballot_w64(item >= base && item < base + a.Hkv * qt * ns);
+        if (!here) return false;
+        const int l = __ffsll(here) - 1;
+        w.g = __builtin_amdgcn_readlane(g, l);
+        qt = __builtin_amdgcn_readlane(qt, l);
+        ns = __builtin_amdgcn_readlane(ns, l);
+        const int in = item - __builtin_amdgcn_readlane(base, l);
+        w.ns = ns;
+        w.item = item;
+        w.qt = in % qt;
+        w.split = in / qt % ns;
+        w.h = in / (qt * ns);
+        w.tiles = __builtin_amdgcn_readfirstlane(s.least[w.g]);
+        w.lead = __builtin_amdgcn_readfirstlane(s.lead[w.g]);
+        const int start = __builtin_amdgcn_readfirstlane(s.start[w.g]);
+        w.first = start + w.qt * mpt;
+        w.members = min(mpt, __builtin_amdgcn_readfirstlane(s.start[w.g + 1]) - w.first);
+        return true;
+    });
+    __syncthreads();  // (the LDS is used anew)
+    return w.g >= 0;
+}
+
+// The plan for the rows that are left to the sequences: where they begin, and runs of them for the waves of the launch behind -- the
+// shortest run length (at least PREFIX_OWN_RUN tiles of 16 rows) at which its waves suffice.
+#define PREFIX_OWN_RUN 4
+#define PREFIX_OWN_RUNS 256  // of a unit
+__device__ __forceinline__ void prefix_plan(const PrefixArgs& a, int mpt, int* lds) {
+    const int n = a.n_groups, tid = threadIdx.x, lane = tid & 63;
+    const PrefixGroups s = prefix_groups(a, lds);
+    int* rows = lds + 5 * n + 1;  // [B] behind the shared ones
+    for (int b = tid; b < a.B; b += 256) {
+        const int L = clampi(a.seq_len[b], 0, a.L_cap);
+        rows[b] = L;
+        if (L == 0 || b < s.start[0] || b >= s.start[n]) a.plan[b] = PrefixPlan{0, 0, L, 0, 0, 0, 0, 1};
+    }
+    __syncthreads();
+    prefix_items(a, s, mpt, gridDim.x, [&](int g, int qt, int ns, int base) {
+        // (a wave's lanes have a group each; the four waves share its members)
+        for (unsigned long long left = __builtin_amdgcn_ballot_w64(g < n); left; left &= left - 1) {
+            const int l = __ffsll(left) - 1, gl = __builtin_amdgcn_readlane(g, l);
+            const int qtl = __builtin_amdgcn_readlane(qt, l), nsl = __builtin_amdgcn_readlane(ns, l), at = __builtin_amdgcn_readlane(base, l);
+            const int start = s.start[gl], first = s.least[gl] * PREFIX_TILE;
+            for (int b = start + tid; b < s.start[gl + 1]; b += 256) {
+                const int i = b - start, L = rows[b];
+                if (L == 0) continue;
+                rows[b] = L - first;
+                a.plan[b] = PrefixPlan{0, 0, L - first, first, at + i / mpt, nsl, i % mpt * a.G, max(qtl, 1)};
             }
         }
-        if (item >= base && item < base + items) {
-            const int in = item - base;
-            w.g = g; w.ns = ns; w.tiles = least[g]; w.item = item;
-            w.qt = in % qt;
-            w.split = in / qt % ns;
-            w.h = in / (qt * ns);
-            w.first = start[g] + w.qt * mpt;
-            w.members = min(mpt, start[g + 1] - w.first);
-            w.lead = lead[g];
-        }
-        base += items;
+        return false;
+    });
+    __syncthreads();
+    auto tiles = [&](int b) { return b < a.B ? (max(rows[b], 1) + 15) / 16 : 0; };
+    float all = 0.f, longest = 0.f;
+    for (int b0 = 0; b0 < a.B; b0 += 64) {
+        all += wave_sum64((float)tiles(b0 + lane));
+        longest = fmaxf(longest, wave_max64((float)tiles(b0 + lane)));
     }
-    if (blockIdx.x == 0)
-        for (int b = tid; b < a.B; b += 256)
-            if (b < start[0] || b >= start[n]) a.info[b] = make_int4(0, 0, 0, 0);
+    int run = max(PREFIX_OWN_RUN, (int)ceilf(all * (float)a.Hkv / (float)a.own_waves));
+    auto runs = [&](int b) { return (uint32_t)min((tiles(b) + run - 1) / run, PREFIX_OWN_RUNS); };
+    for (;; run += max(1, run >> 4)) {
+        uint32_t w = 0;
+        for (int b0 = 0; b0 < a.B; b0 += 64) w += (uint32_t)__builtin_amdgcn_readlane((int)wave_incl_scan(runs(b0 + lane)), 63);
+        if (w * (uint32_t)a.Hkv <= (uint32_t)a.own_waves || run >= (int)longest) break;
+    }
+    uint32_t start = 0;
+    for (int b0 = 0; b0 < a.B; b0 += 64) {
+        const int b = b0 + lane;
+        const uint32_t r = runs(b), upto = wave_incl_scan(r);
+        if (tid < 64 && b < a.B) {
+            a.plan[b].start = (int)((start + upto - r) * a.Hkv);
+            a.plan[b].runs = (int)r;
+        }
+        start += (uint32_t)__builtin_amdgcn_readlane((int)upto, 63);
+    }
     __syncthreads();  // (the LDS is used anew)
-    // (in scalar registers from here on)
-    for (int* v : {&w.g, &w.h, &w.split, &w.ns, &w.qt, &w.tiles, &w.item, &w.first, &w.members, &w.lead}) *v = __builtin_amdgcn_readfirstlane(*v);
-    return w.g >= 0;
 }
 
 // 16-byte piece c of row r of a stage is at slot c ^ prefix_swizzle(r): 16 rows of one piece, and four rows of four pieces, are in
 // 16 different slots, so that neither product's reads have bank conflicts
 __device__ __forceinline__ int prefix_swizzle(int r) { return (r & 3) << 2 | (r >> 2 & 3); }
+
+// (fmaxf alone costs an instruction more for each operand, to quiet a NaN that is dropped anyway)
+__device__ __forceinline__ float max3(float a, float b, float c) {
+    float r;
+    asm("v_max3_f32 %0, %1, %2, %3" : "=v"(r) : "v"(a), "v"(b), "v"(c));
+    return r;
+}
 
 template <int N>
 __device__ __forceinline__ void prefix_wait() { asm volatile("s_waitcnt vmcnt(%0)" ::"n"(N) : "memory"); }
@@ -157,6 +242,7 @@ __global__ __launch_bounds__(256, 1) void prefix_kernel(const PrefixArgs a) {
     extern __shared__ __attribute__((aligned(16))) char smem[];
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int wq = wave % WQ, wk = wave / WQ, n = lane & 31, half = lane >> 5;
+    if (blockIdx.x == gridDim.x - 1) prefix_plan(a, M / a.G, reinterpret_cast<int*>(smem));
     PrefixShare w;
     if (!prefix_share(a, M / a.G, reinterpret_cast<int*>(smem), w)) return;
     const int G = a.G, rows = w.members * G;
@@ -250,9 +336,7 @@ __global__ __launch_bounds__(256, 1) void prefix_kernel(const PrefixArgs a) {
 #pragma unroll
         for (int t = 0; t < 2; ++t) asm volatile("" : "+v"(sc[t]));
     };
-    // the maxima in use, where these scores pass one by 2^8
-    auto follow = [&](const f32x16_t (&sc)[2]) {
-        float top[2];
+    auto highest = [&](const f32x16_t (&sc)[2], float (&top)[2]) {
 #pragma unroll
         for (int t = 0; t < 2; ++t) {
             top[t] = sc[t][0];
@@ -260,7 +344,10 @@ __global__ __launch_bounds__(256, 1) void prefix_kernel(const PrefixArgs a) {
             for (int i = 1; i < 16; ++i) top[t] = fmaxf(top[t], sc[t][i]);
             top[t] *= scale;
         }
-        if (__builtin_amdgcn_ballot_w64(top[0] > m[0] + 8.f || top[1] > m[1] + 8.f) != 0ull) {
+    };
+    // the maxima in use, where the highest scores pass one by far
+    auto follow = [&](const float (&top)[2]) {
+        if (__builtin_amdgcn_ballot_w64(top[0] > m[0] + PREFIX_LOOSE || top[1] > m[1] + PREFIX_LOOSE) != 0ull) {
 #pragma unroll
             for (int t = 0; t < 2; ++t) {
                 float x, y;
@@ -326,8 +413,10 @@ __global__ __launch_bounds__(256, 1) void prefix_kernel(const PrefixArgs a) {
             if (k0 + s * STAGE + wk * PART < k1) {
                 f32x16_t sc[2];
                 uint32_t p[2][8];
+                float top[2];
                 products(at_stage(s), sc);
-                follow(sc);
+                highest(sc, top);
+                follow(top);
                 weights(sc, p);
                 values(at_stage(s) + STAGE * 256, p);
             }
@@ -336,29 +425,92 @@ __global__ __launch_bounds__(256, 1) void prefix_kernel(const PrefixArgs a) {
             pin();
         }
     } else {
-        // The products of the next 32 rows stand beside the weights of these: matrix cores and vector ALU at work together
+        // The products of the next 32 rows stand beside the weights of these, and their maxima beside these rows' second product:
+        // matrix cores and vector ALU at work together, in one straight piece of code (what is computed behind the last rows is
+        // of stale LDS and not used)
         f32x16_t sc[2], next[2];
+        float top[2];
         if (stages >= NBUF - 1) prefix_wait<(NBUF - 2) * BLOCKS * 8>();  // (so many were requested)
         else prefix_wait<0>();
         __syncthreads();
         products(at_stage(0), sc);
+        highest(sc, top);
         for (int s = 0; s < stages; ++s) {
 #pragma unroll
             for (int i = 0; i < SUBS; ++i) {
                 uint32_t p[2][8];
-                follow(sc);
-                if (i + 1 < SUBS) {
-                    products(at_stage(s) + (i + 1) * 32 * 256, next);
-                } else if (s + 1 < stages) {
+                follow(top);
+                if (i + 1 == SUBS && s + 1 < stages) {
                     // stage s + 1 is there once only the one behind it is outstanding; everybody is done with stage s - 1
                     if (s + 2 < stages) prefix_wait<(NBUF - 3) * BLOCKS * 8>();
                     else prefix_wait<0>();
                     __syncthreads();
                     if (s + NBUF - 1 < stages) request(s + NBUF - 1);
-                    products(at_stage(s + 1), next);
                 }
-                weights(sc, p);
-                values(at_stage(s) + STAGE * 256 + i * 32 * 256, p);
+                // (left to itself the compiler puts the matrix instructions one behind the other)
+                const char* kt = i + 1 < SUBS ? at_stage(s) + (i + 1) * 32 * 256 : at_stage(s + 1);
+                const char* vt = at_stage(s) + STAGE * 256 + i * 32 * 256;
+                auto k_piece = [&](int k) { return __builtin_bit_cast(bf16x8_t, *reinterpret_cast<const uint4*>(kt + (k_at ^ (k << 5)))); };
+                bf16x8_t kf[3] = {k_piece(0), k_piece(1), k_piece(2)};
+#pragma unroll
+                for (int t = 0; t < 2; ++t)
+#pragma unroll
+                    for (int j = 0; j < 16; ++j) next[t][j] = 0.f;
+                f32x2_t e[3];  // two weights on their way: arguments, then exponentials
+                auto argument = [&](int j) {
+                    e[j % 3][0] = fmaf(sc[j / 8][2 * (j % 8)], scale, -sub[j / 8]);
+                    e[j % 3][1] = fmaf(sc[j / 8][2 * (j % 8) + 1], scale, -sub[j / 8]);
+                };
+                auto power = [&](int j) { e[j % 3][0] = fast_exp2(e[j % 3][0]); e[j % 3][1] = fast_exp2(e[j % 3][1]); };
+                auto round = [&](int j) {
+                    p[j / 8][j % 8] = __builtin_bit_cast(uint32_t, __builtin_convertvector(e[j % 3], bf16x2_t));
+                    l[j / 8] = dot2_bf16(p[j / 8][j % 8], 0x3f803f80u, l[j / 8]);
+                };
+                argument(0);
+                power(0);
+                argument(1);
+                __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+                for (int j = 0; j < 16; ++j) {
+                    next[j % 2] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf[j / 2 % 3], __builtin_bit_cast(bf16x8_t, qb[j % 2][j / 2]), next[j % 2], 0, 0, 0);
+                    if (j % 2 == 1 && j / 2 + 3 < 8) kf[j / 2 % 3] = k_piece(j / 2 + 3);
+                    if (j + 1 < 16) power(j + 1);
+                    if (j + 2 < 16) argument(j + 2);
+                    round(j);
+                    __builtin_amdgcn_sched_barrier(0);
+                }
+                auto v_piece_at = [&](int j) {  // channels 32 (j % 4) of rows 16 (j / 4) ..
+                    uint2 v[2];
+#pragma unroll
+                    for (int y = 0; y < 2; ++y) {
+                        const int r = 16 * (j / 4) + 8 * y + v_row;
+                        v[y] = __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4_t*)const_cast<char*>(
+                            vt + r * 256 + (((4 * (j % 4) + v_piece) ^ prefix_swizzle(r)) << 4) + (lane & 1) * 8)));
+                    }
+                    return __builtin_bit_cast(bf16x8_t, make_uint4(v[0].x, v[0].y, v[1].x, v[1].y));
+                };
+                bf16x8_t vf[3] = {v_piece_at(0), v_piece_at(1), v_piece_at(2)};
+                __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+                for (int j = 0; j < 16; ++j) {
+                    const int t = j % 2, x = j / 8, c = j / 2 % 4;
+                    acc[t][c] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(
+                        vf[j / 2 % 3], __builtin_bit_cast(bf16x8_t, make_uint4(p[t][4 * x], p[t][4 * x + 1], p[t][4 * x + 2], p[t][4 * x + 3])), acc[t][c], 0, 0, 0);
+                    if (j % 2 == 1 && j / 2 + 3 < 8) vf[j / 2 % 3] = v_piece_at(j / 2 + 3);
+                    if (j == 1) {
+                        asm volatile("" : "+v"(next[0]));
+                        top[0] = fmaxf(next[0][0], next[0][1]);
+                    }
+                    if (j == 8) {
+                        asm volatile("" : "+v"(next[1]));
+                        top[1] = fmaxf(next[1][0], next[1][1]);
+                    }
+                    if (j >= 1 && j < 8) top[0] = max3(top[0], next[0][2 * j], next[0][2 * j + 1]);
+                    if (j >= 9) top[1] = max3(top[1], next[1][2 * (j - 8)], next[1][2 * (j - 8) + 1]);
+                    __builtin_amdgcn_sched_barrier(0);
+                }
+                top[0] *= scale;
+                top[1] *= scale;
 #pragma unroll
                 for (int t = 0; t < 2; ++t) sc[t] = next[t];
                 pin();
@@ -374,36 +526,60 @@ __global__ __launch_bounds__(256, 1) void prefix_kernel(const PrefixArgs a) {
     for (int t = 0; t < 2; ++t) {
         float x, y;
         swap32(l[t], x, y);
-        if (half == 0) { s_m[wave][32 * t + n] = m[t]; s_l[wave][32 * t + n] = x + y; }
+        l[t] = x + y;
+        if (half == 0) { s_m[wave][32 * t + n] = m[t]; s_l[wave][32 * t + n] = l[t]; }
+    }
+    float top[2] = {m[0], m[1]}, total[2] = {l[0], l[1]};
+    if constexpr (WK > 1) {
+        __syncthreads();
+#pragma unroll
+        for (int t = 0; t < 2; ++t) {
+#pragma unroll
+            for (int k = 0; k < WK; ++k) top[t] = fmaxf(top[t], s_m[wq + k * WQ][32 * t + n]);
+            total[t] = 0.f;
+#pragma unroll
+            for (int k = 0; k < WK; ++k) {
+                const float mk = s_m[wq + k * WQ][32 * t + n];
+                total[t] = fmaf(mk == HATA_NEG_INF ? 1.f : fast_exp2(mk - top[t]), s_l[wq + k * WQ][32 * t + n], total[t]);
+            }
+            const float f = m[t] == HATA_NEG_INF ? 1.f : fast_exp2(m[t] - top[t]);  // (sums without a score are zero)
+#pragma unroll
+            for (int c = 0; c < 4; ++c) acc[t][c] *= f;
+        }
+    }
+#pragma unroll
+    for (int t = 0; t < 2; ++t)
 #pragma unroll
         for (int c = 0; c < 4; ++c)
 #pragma unroll
             for (int i = 0; i < 4; ++i)  // acc[t][c][4 i + j]: channel 32 c + 8 i + 4 half + j of query row 32 t + n
                 *reinterpret_cast<float4*>(&s_acc[(wave * 64 + 32 * t + n) * (HATA_D + 4) + 32 * c + 8 * i + 4 * half]) =
                     make_float4(acc[t][c][4 * i], acc[t][c][4 * i + 1], acc[t][c][4 * i + 2], acc[t][c][4 * i + 3]);
-    }
     __syncthreads();
     float* out = a.part + (int64_t)w.item * (M * (HATA_D + 2));
-    for (int i = tid; i < rows * (HATA_D / 4); i += 256) {
-        const int r = i / (HATA_D / 4), c4 = i % (HATA_D / 4) * 4, w0 = r / 64, r0 = r % 64;
-        float top = s_m[w0][r0], sum = 0.f;
+    if (wk == 0 && half == 0) {
 #pragma unroll
-        for (int k = 1; k < WK; ++k) top = fmaxf(top, s_m[w0 + k * WQ][r0]);
-        float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+        for (int t = 0; t < 2; ++t)
+            if (64 * wq + 32 * t + n < rows)
+                *reinterpret_cast<float2*>(out + M * HATA_D + 2 * (64 * wq + 32 * t + n)) = make_float2(top[t], total[t]);
+    }
+    // eight rows a turn, four turns together
+    const int r8 = tid / 32, c4 = tid % 32 * 4;
+    for (int i0 = 0; i0 < rows; i0 += 32) {
+        float4 o[4];
 #pragma unroll
-        for (int k = 0; k < WK; ++k) {
-            const int wv = w0 + k * WQ;
-            const float f = s_m[wv][r0] == HATA_NEG_INF ? 0.f : fast_exp2(s_m[wv][r0] - top);
-            const float4 v = *reinterpret_cast<const float4*>(&s_acc[(wv * 64 + r0) * (HATA_D + 4) + c4]);
-            // (a wave whose scores were all -inf may hold NaN there, of infinite values; it counts if no other score does)
-            if (f != 0.f || top == HATA_NEG_INF) {
-                const float g = top == HATA_NEG_INF ? 1.f : f;
-                o.x = fmaf(g, v.x, o.x); o.y = fmaf(g, v.y, o.y); o.z = fmaf(g, v.z, o.z); o.w = fmaf(g, v.w, o.w);
-                sum = fmaf(g, s_l[wv][r0], sum);
+        for (int j = 0; j < 4; ++j) {
+            const int r = i0 + 8 * j + r8;  // (rows up to M lie in LDS)
+            o[j] = *reinterpret_cast<const float4*>(&s_acc[(r / 64 * 64 + r % 64) * (HATA_D + 4) + c4]);
+#pragma unroll
+            for (int k = 1; k < WK; ++k) {
+                const float4 v = *reinterpret_cast<const float4*>(&s_acc[((r / 64 + k * WQ) * 64 + r % 64) * (HATA_D + 4) + c4]);
+                o[j].x += v.x; o[j].y += v.y; o[j].z += v.z; o[j].w += v.w;
             }
         }
-        *reinterpret_cast<float4*>(out + r * HATA_D + c4) = o;
-        if (c4 == 0) *reinterpret_cast<float2*>(out + M * HATA_D + 2 * r) = make_float2(top, sum);
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+            if (i0 + 8 * j + r8 < rows) *reinterpret_cast<float4*>(out + (i0 + 8 * j + r8) * HATA_D + c4) = o[j];
     }
 }
 
@@ -443,7 +619,8 @@ hipError_t launch_prefix(const hata_ctx* c, const void* q, const void* K, const 
     PrefixArgs a;
     a.q = (const uint16_t*)q; a.K = (const uint16_t*)K; a.V = (const uint16_t*)V;
     a.seq_len = seq_len; a.group_start = group_start; a.shared_len = shared_len;
-    a.info = (int4*)c->prefix_info;
+    a.plan = c->prefix_plan;
+    a.own_waves = dense_own_wgs(B, f.Hkv) * 8;
     a.part = c->prefix_part;
     a.pv = pages;
     a.B = B; a.Hq = f.Hq; a.Hkv = f.Hkv; a.G = c->G;

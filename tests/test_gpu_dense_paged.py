@@ -108,15 +108,16 @@ class World:
         return self.out, self.out32
 
     def check(self, groups=True, ref=None, **kw):
-        """fp32 output: the weights of shared rows are rounded to bf16 (half a step: 2^-8 relative), the others to two terms
-        (2^-15) or not at all; logits of fp32 sums: |q.k| summed is below 2^9 here, 2^-24 of it for each of some ten roundings,
-        below 2^-11 at most, an e-fold of that in the weights; the bf16 output is that, rounded."""
+        """fp32 output o = sum p v / sum p: the weights p of shared rows are rounded to bf16, p (1 + d) with |d| <= 2^-8 (half a
+        step), in both sums, which moves o by sum p d (v - o) / sum p, at most 2^-8 (sum p |v| + |o|) / sum p; the others are taken in
+        two terms (2^-15) or as they are; logits of fp32 sums: |q.k| summed is below 2^9 here, 2^-24 of it for each of some ten
+        roundings, below 2^-11 at most, an e-fold of that in the weights; the bf16 output is that, rounded."""
         import torch
         out, out32 = self.run(groups, **kw)
         torch.cuda.synchronize()
         want, size = ref if ref is not None else self.exact()
-        weight = (2.0 ** -8 if groups and self.shared else 0.0) + 2.0 ** -11
-        err = (out32.double() - want).abs() - weight * size
+        rounded = 2.0 ** -8 if groups and self.shared else 0.0
+        err = (out32.double() - want).abs() - rounded * (size + want.abs()) - 2.0 ** -11 * size
         assert bool((err <= 1e-30).all()), f"off by {float((out32.double() - want).abs().max()):.3e} (bound passed by {float(err.max()):.3e})"
         assert torch.equal(out.view(torch.bfloat16), out32.to(torch.bfloat16))
         return want, size
@@ -248,7 +249,7 @@ def test_infinite_values_of_other_rows(hata):
     out, out32 = w.run()
     torch.cuda.synchronize()
     err = (out32[0].double() - ref[0][0]).abs()
-    assert bool((err <= (2.0 ** -8 + 2.0 ** -11) * ref[1][0]).all())
+    assert bool((err <= 2.0 ** -8 * (ref[1][0] + ref[0][0].abs()) + 2.0 ** -11 * ref[1][0]).all())
     assert bool(out32[1:].isnan().any())
 
 
