@@ -47,7 +47,8 @@ struct DenseArgs {
     int64_t sb, sh, sn;
     float scale_log2;
     PageView pv;  // PAGED: the caches are pools of pages (sb, sh, sn are not used)
-    // DENSE_OWN: the sequences' runs and the shared rows' partial results, from the launch before
+    int team;  // DENSE_OWN: waves that have a run together
+    // the sequences' runs and the shared rows' partial results, from the launch before
     const PrefixPlan* plan;
     const float* pre;  // [..][pre_rows][HATA_D], then [pre_rows][2]
     int pre_rows;
@@ -130,28 +131,28 @@ __device__ __forceinline__ bool dense_share(const int32_t* __restrict__ seq_len,
     return false;
 }
 
-// ---- the end of a wave's run in the form DENSE_OWN ----
-// Partial results of the runs (written by other waves of this launch: device-coherent): [worker][G][HATA_D], and behind all of them
-// [worker][G][2], maximum and sum.
+// ---- the end of a team's run in the form DENSE_OWN ----
+// Partial results of the runs (written by other teams of this launch: device-coherent): [team][G][HATA_D], and behind all of them
+// [team][G][2], maximum and sum.
 //
-// Joins `nt` slices, 64 at a time: the states of all heads (lane: slice) and a first batch of channels are requested together, then come
-// the weights, then the rest.  KI: float4 of a lane, channels 4 (i % 32) .. of head i / 32, i = lane + 64 k (2 KI >= G heads);
-// M, L, sum: maximum, sum and channels so far.
+// Joins `nt` slices, 64 at a time: the states of this wave's heads (lane: slice) and a first batch of channels are requested together,
+// then come the weights, then the rest.  KI: float4 of a lane, channels 4 (i % 32) .. of head g0 + i / 32, i = lane + 64 k;
+// M, L, sum: maximum, sum and channels so far.  (s_w: this wave's)
 template <int KI, typename State, typename Slice>
-__device__ __forceinline__ void dense_own_join(int G, int nt, float* s_w, State state, Slice slice, float (&M)[2 * KI], float (&L)[2 * KI], float4 (&sum)[KI]) {
+__device__ __forceinline__ void dense_own_join(int g0, int G, int nt, float* s_w, State state, Slice slice, float (&M)[2 * KI], float (&L)[2 * KI], float4 (&sum)[KI]) {
     constexpr int U = KI == 8 ? 1 : 16 / KI;  // slices of a batch (registers)
     const int lane = threadIdx.x & 63;
     for (int s0 = 0; s0 < nt; s0 += 64) {
         const int cnt = min(64, nt - s0);
         uint2 st[2 * KI];
 #pragma unroll
-        for (int g = 0; g < 2 * KI; ++g) st[g] = state(min(g, G - 1), s0 + min(lane, cnt - 1));
+        for (int g = 0; g < 2 * KI; ++g) st[g] = state(min(g0 + g, G - 1), s0 + min(lane, cnt - 1));
         float4 x[U][KI];
         auto load = [&](int u0) {
 #pragma unroll
             for (int u = 0; u < U; ++u)
 #pragma unroll
-                for (int k = 0; k < KI; ++k) x[u][k] = slice(min(lane + 64 * k, 32 * G - 1), s0 + min(u0 + u, cnt - 1));
+                for (int k = 0; k < KI; ++k) x[u][k] = slice(min(32 * g0 + lane + 64 * k, 32 * G - 1), s0 + min(u0 + u, cnt - 1));
         };
         load(0);
         float f[2 * KI];
@@ -192,54 +193,41 @@ __device__ __forceinline__ void dense_own_join(int G, int nt, float* s_w, State 
 }
 
 template <int VH, int NACC>
-__device__ __forceinline__ void dense_own_end(const DenseArgs& a, const DenseShare& d, char* ring, float m_run, float l_run, f32x4_t (&acc)[NACC],
-                                              const float* pre, int np, int np_row, int np_step, uint16_t* outp, float* outp32) {
-    const int lane = threadIdx.x & 63, n = lane & 15, kg = lane >> 4, G = a.G, ns = d.ns, nt = ns + np;
-    float* s_acc = reinterpret_cast<float*>(ring);  // [G][HATA_D + 4], of this wave alone
+__device__ __forceinline__ void dense_own_end(const DenseArgs& a, const DenseShare& d, char* smem, float (&s_m)[DENSE_WAVES][16], float (&s_l)[DENSE_WAVES][16],
+                                              float m_run, float l_run, f32x4_t (&acc)[NACC], const float* pre, int np, int np_row, int np_step,
+                                              bool idle, uint16_t* outp, float* outp32) {
+    __shared__ int s_last[DENSE_WAVES];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), n = lane & 15, kg = lane >> 4;
+    const int G = a.G, ns = d.ns, in_team = wave % a.team, first_wave = wave - in_team;
+    // a wave's ring: its state [G][HATA_D + 4], behind that the weights of a join
+    auto state_of = [&](int w) { return reinterpret_cast<float*>(smem + w * (DENSE_RING * DENSE_TILE_BYTES)); };
+    float* s_acc = state_of(wave);
     l_run = rows_sum4(l_run);
     if constexpr (VH > 0) {
 #pragma unroll
         for (int i = 0; i < 8 * VH; ++i) acc[i / 4][i % 4] = rows_sum4(acc[i / 4][i % 4]);
         if (kg == 0) {
+            if (n < VH) { s_m[wave][n] = m_run; s_l[wave][n] = l_run; }
 #pragma unroll
             for (int c = 0; c < 2 * VH; ++c)
                 *reinterpret_cast<float4*>(&s_acc[(n + c / 2) % VH * (HATA_D + 4) + 8 * n + 4 * (c & 1)]) = make_float4(acc[c][0], acc[c][1], acc[c][2], acc[c][3]);
         }
     } else if (n < G) {
+        if (kg == 0) { s_m[wave][n] = m_run; s_l[wave][n] = l_run; }
 #pragma unroll
         for (int c = 0; c < 8; ++c)  // acc[c][r] = O[head n][channel 16 c + 4 kg + r]
             *reinterpret_cast<float4*>(&s_acc[n * (HATA_D + 4) + 16 * c + 4 * kg]) = make_float4(acc[c][0], acc[c][1], acc[c][2], acc[c][3]);
     }
-    // (LDS serves a wave's accesses in order: what other lanes have written is there)
-    __builtin_amdgcn_wave_barrier();
+    if (a.team > 1) __syncthreads();
+    else __builtin_amdgcn_wave_barrier();  // (LDS serves a wave's accesses in order)
     float* part = a.partials + (int64_t)d.first * G * HATA_D;  // [ns][G][HATA_D]
     float* states = a.partials + (int64_t)gridDim.x * DENSE_WAVES * G * HATA_D + (int64_t)d.first * G * 2;  // [ns][G][2]
-    if (ns > 1) {
-        float* p = part + (int64_t)d.split * G * HATA_D;
-        for (int i = lane; i < G * (HATA_D / 2); i += 64) {
-            const float2 v = *reinterpret_cast<const float2*>(&s_acc[i / (HATA_D / 2) * (HATA_D + 4) + i % (HATA_D / 2) * 2]);
-            st_dev(reinterpret_cast<unsigned long long*>(p + 2 * i), (unsigned long long)__float_as_uint(v.y) << 32 | __float_as_uint(v.x));
-        }
-        if (kg == 0 && n < G)
-            st_dev(reinterpret_cast<unsigned long long*>(states + (d.split * G + n) * 2),
-                   (unsigned long long)__float_as_uint(l_run) << 32 | __float_as_uint(m_run));
-        wait_stores();
-        int last = 0;
-        if (lane == 0) {
-            uint32_t* cnt = a.counter + ((int64_t)d.b * a.Hkv + d.h) * a.counter_stride;
-            last = atomicAdd(cnt, 1u) == (uint32_t)(ns - 1);
-            if (last) *cnt = 0;
-        }
-        if (!__builtin_amdgcn_readfirstlane(last)) return;
-    }
-    // (the only run of its unit begins with what it has, the last of several with the first of them)
-    const int own = ns > 1 ? ns : 0;
     const int64_t pre_step = (int64_t)np_step * a.pre_rows * (HATA_D + 2);
-    auto state = [&](int g, int s) -> uint2 {
+    auto state = [&](int own, int g, int s) -> uint2 {
         if (s < own) return ld_dev_u2(states + (s * G + g) * 2);
         return *reinterpret_cast<const uint2*>(pre + (s - own) * pre_step + (int64_t)a.pre_rows * HATA_D + 2 * (np_row + g));
     };
-    auto slice = [&](int i, int s) -> float4 {  // four channels
+    auto slice = [&](int own, int i, int s) -> float4 {  // four channels
         if (s < own) {
             const float* p = part + (int64_t)s * G * HATA_D + 4 * i;
             const uint2 x = ld_dev_u2(p), y = ld_dev_u2(p + 2);
@@ -247,26 +235,79 @@ __device__ __forceinline__ void dense_own_end(const DenseArgs& a, const DenseSha
         }
         return *reinterpret_cast<const float4*>(pre + (s - own) * pre_step + np_row * HATA_D + 4 * i);
     };
-    auto join = [&](auto ki) {
+    auto finish = [&](auto ki) {
         constexpr int KI = decltype(ki)::value;
+        const int g0 = 2 * KI * in_team;  // this wave's heads
+        const bool none = idle || g0 >= G;
         float M[2 * KI], L[2 * KI];
         float4 sum[KI];
+        // the team's waves
 #pragma unroll
-        for (int g = 0; g < 2 * KI; ++g) {
-            const int from = VH ? min(g, VH - 1) : g;  // (the lane that has head g's state)
-            M[g] = own ? HATA_NEG_INF : __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(m_run), from));
-            L[g] = own ? 0.f : __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(l_run), from));
+        for (int j = 0; j < 2 * KI; ++j) {
+            const int g = min(g0 + j, G - 1);
+            M[j] = s_m[first_wave][g];
+            for (int w = 1; w < a.team; ++w) M[j] = fmaxf(M[j], s_m[first_wave + w][g]);
+            L[j] = 0.f;
+            for (int w = 0; w < a.team; ++w) {
+                const float m = s_m[first_wave + w][g];
+                L[j] = fmaf(m == HATA_NEG_INF ? 1.f : fast_exp2(m - M[j]), s_l[first_wave + w][g], L[j]);  // (sums without a score are zero)
+            }
         }
 #pragma unroll
         for (int k = 0; k < KI; ++k) {
-            const int i = min(lane + 64 * k, 32 * G - 1);
-            sum[k] = own ? make_float4(0.f, 0.f, 0.f, 0.f) : *reinterpret_cast<const float4*>(&s_acc[i / 32 * (HATA_D + 4) + i % 32 * 4]);
+            const int i = min(32 * g0 + lane + 64 * k, 32 * G - 1), at = i / 32 * (HATA_D + 4) + i % 32 * 4;
+            const float top = lane < 32 ? M[2 * k] : M[2 * k + 1];
+            sum[k] = make_float4(0.f, 0.f, 0.f, 0.f);
+            for (int w = 0; w < a.team; ++w) {
+                const float m = s_m[first_wave + w][i / 32], f = m == HATA_NEG_INF ? 1.f : fast_exp2(m - top);
+                const float4 v = *reinterpret_cast<const float4*>(&state_of(first_wave + w)[at]);
+                sum[k].x = fmaf(f, v.x, sum[k].x); sum[k].y = fmaf(f, v.y, sum[k].y);
+                sum[k].z = fmaf(f, v.z, sum[k].z); sum[k].w = fmaf(f, v.w, sum[k].w);
+            }
         }
-        __builtin_amdgcn_wave_barrier();
-        dense_own_join<KI>(G, own + np, s_acc, state, slice, M, L, sum);
+        int own = 0;
+        if (!none && ns > 1) {
+#pragma unroll
+            for (int k = 0; k < KI; ++k) {
+                const int i = 32 * g0 + lane + 64 * k;
+                if (i < 32 * G) {
+                    unsigned long long* p = reinterpret_cast<unsigned long long*>(part + (int64_t)d.split * G * HATA_D + 4 * i);
+                    st_dev(p, (unsigned long long)__float_as_uint(sum[k].y) << 32 | __float_as_uint(sum[k].x));
+                    st_dev(p + 1, (unsigned long long)__float_as_uint(sum[k].w) << 32 | __float_as_uint(sum[k].z));
+                }
+            }
+#pragma unroll
+            for (int j = 0; j < 2 * KI; ++j)
+                if (lane == j && g0 + j < G)
+                    st_dev(reinterpret_cast<unsigned long long*>(states + (d.split * G + g0 + j) * 2),
+                           (unsigned long long)__float_as_uint(L[j]) << 32 | __float_as_uint(M[j]));
+            wait_stores();
+        }
+        if (a.team > 1) __syncthreads();
+        if (in_team == 0 && lane == 0) {
+            int last = 1;
+            if (!idle && ns > 1) {
+                uint32_t* cnt = a.counter + ((int64_t)d.b * a.Hkv + d.h) * a.counter_stride;
+                last = atomicAdd(cnt, 1u) == (uint32_t)(ns - 1);
+                if (last) *cnt = 0;
+            }
+            s_last[wave] = last;
+        }
+        if (a.team > 1) __syncthreads();
+        else __builtin_amdgcn_wave_barrier();
+        if (none || !s_last[first_wave]) return;
+        if (ns > 1) {  // (the only run of its unit goes on with what it has)
+            own = ns;
+#pragma unroll
+            for (int j = 0; j < 2 * KI; ++j) { M[j] = HATA_NEG_INF; L[j] = 0.f; }
+#pragma unroll
+            for (int k = 0; k < KI; ++k) sum[k] = make_float4(0.f, 0.f, 0.f, 0.f);
+        }
+        dense_own_join<KI>(g0, G, own + np, s_acc + 16 * (HATA_D + 4), [&](int g, int s) { return state(own, g, s); },
+                           [&](int i, int s) { return slice(own, i, s); }, M, L, sum);
 #pragma unroll
         for (int k = 0; k < KI; ++k) {
-            const int i = lane + 64 * k;
+            const int i = 32 * g0 + lane + 64 * k;
             const float l = lane < 32 ? L[2 * k] : L[2 * k + 1];
             if (i < 32 * G) {
                 float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
@@ -276,24 +317,24 @@ __device__ __forceinline__ void dense_own_end(const DenseArgs& a, const DenseSha
             }
         }
     };
-    if (G <= 2) join(std::integral_constant<int, 1>());
-    else if (G <= 4) join(std::integral_constant<int, 2>());
-    else if (G <= 8) join(std::integral_constant<int, 4>());
-    else join(std::integral_constant<int, 8>());
+    const int need = (G + 2 * a.team - 1) / (2 * a.team);
+    if (need <= 1) finish(std::integral_constant<int, 1>());
+    else if (need <= 2) finish(std::integral_constant<int, 2>());
+    else if (need <= 4) finish(std::integral_constant<int, 4>());
+    else finish(std::integral_constant<int, 8>());
 }
 
 enum DenseForm { DENSE_BF16X2, DENSE_FP32_ONE_HEAD, DENSE_FP32_TWO_HEADS, DENSE_FP32 };
 // DENSE_PAGED: the rows lie in pools of pages.  A tile of 16 rows lies inside a page, so a wave looks up one page a tile, 64 tiles'
 // at a time (a lane each).
 // DENSE_OWN: the same, for the rows that sequences do not share (prefix_kernel has been at the others).  They are few for many
-// units, so what is dealt out are runs for single waves, not for workgroups: each has a unit, a run of tiles and partial results
-// of its own, meets no other wave, and the last one of a unit to arrive joins them and the shared rows'.  256 sequences with
-// some 250 rows behind shared ones, 8 KV heads, groups of 8: a workgroup per unit 171 us, ONE_OWN_US.
+// units, so what is dealt out are runs for teams of `team` waves of a workgroup (1, 2, 4 or 8), by the plan of the launch before;
+// the last team of a unit to arrive joins its runs and the shared rows' partial results.
 enum DenseRows { DENSE_CONTIGUOUS, DENSE_PAGED, DENSE_OWN };
 template <DenseForm FORM, DenseRows ROWS>
 __global__ __launch_bounds__(DENSE_WAVES * 64) void dense_kernel(const DenseArgs a) {
     constexpr bool PAGED = ROWS != DENSE_CONTIGUOUS, OWN = ROWS == DENSE_OWN;
-    constexpr int STEP = OWN ? 1 : DENSE_WAVES;  // between the tiles of a wave
+    const int step = OWN ? a.team : DENSE_WAVES;  // between the tiles of a wave
     // ring[wave][DENSE_RING][DENSE_TILE_BYTES]; afterwards the waves' states, the merge weights and sums
     extern __shared__ __attribute__((aligned(16))) char smem[];
     __shared__ float s_m[DENSE_WAVES][16], s_l[DENSE_WAVES][16];
@@ -304,31 +345,32 @@ __global__ __launch_bounds__(DENSE_WAVES * 64) void dense_kernel(const DenseArgs
     int row_first = 0;  // rows in front of this sequence's own, and the partial results of those
     [[maybe_unused]] int np = 0, np_row = 0, np_step = 0;
     [[maybe_unused]] const float* pre = nullptr;
+    [[maybe_unused]] bool idle = false;
     if constexpr (OWN) {
-        const int worker = blockIdx.x * DENSE_WAVES + wave;
-        PrefixPlan x;
-        for (int b0 = 0;; b0 += 64) {
-            if (b0 >= a.B) return;  // nothing left for this wave
-            x = a.plan[min(b0 + lane, a.B - 1)];
+        const int worker = (blockIdx.x * DENSE_WAVES + wave) / a.team;
+        d = DenseShare{-1, 0, 0, 0, 1, 0};
+        for (int b0 = 0; b0 < a.B && d.b < 0; b0 += 64) {
+            PrefixPlan x = a.plan[min(b0 + lane, a.B - 1)];
             const unsigned long long mine = __builtin_amdgcn_ballot_w64(b0 + lane < a.B && worker < x.start + x.runs * a.Hkv);
             if (mine) {
                 const int l = __ffsll(mine) - 1;
-                d.b = b0 + l;
                 for (int* v : {&x.start, &x.runs, &x.rows, &x.first, &x.item, &x.splits, &x.row, &x.step}) *v = __builtin_amdgcn_readlane(*v, l);
-                break;
+                const int in = worker - x.start;
+                d.b = b0 + l;
+                d.L = x.rows;
+                d.ns = x.runs;
+                d.h = in / x.runs;
+                d.split = in - d.h * x.runs;
+                d.first = worker - d.split;
+                row_first = x.first;
+                np = x.splits;
+                np_row = x.row;
+                np_step = x.step;
+                pre = a.pre + (x.item + (int64_t)d.h * np * np_step) * a.pre_rows * (HATA_D + 2);
             }
         }
-        const int in = worker - x.start;
-        d.L = x.rows;
-        d.ns = x.runs;
-        d.h = in / x.runs;
-        d.split = in - d.h * x.runs;
-        d.first = worker - d.split;
-        row_first = x.first;
-        np = x.splits;
-        np_row = x.row;
-        np_step = x.step;
-        pre = a.pre + (x.item + (int64_t)d.h * np * np_step) * a.pre_rows * (HATA_D + 2);
+        idle = d.b < 0;  // nothing left for this team (it still comes to the barriers)
+        if (idle) d.b = 0;
     } else if (!dense_share(a.seq_len, a.B, a.Hkv, a.L_cap, d)) {
         return;
     }
@@ -343,15 +385,16 @@ __global__ __launch_bounds__(DENSE_WAVES * 64) void dense_kernel(const DenseArgs
         for (int s = 0; s < 4; ++s) qb[s] = *reinterpret_cast<const uint4*>(q0 + 32 * s);
     }
     if (L == 0 && np == 0) {  // no row at all
-        for (int i = OWN ? lane : tid; i < G * HATA_D; i += OWN ? 64 : DENSE_WAVES * 64) {
+        for (int i = OWN ? lane : tid; i < (idle ? 0 : G * HATA_D); i += OWN ? 64 : DENSE_WAVES * 64) {
             outp[i] = 0;
             if (outp32) outp32[i] = 0.f;
         }
-        return;
+        if (!OWN) return;
+        idle = true;
     }
     const int tiles = (L + 15) / 16;  // in even runs
     const int t_begin = (int)((int64_t)tiles * split / ns), t_end = (int)((int64_t)tiles * (split + 1) / ns);
-    const int t_wave = t_begin + (OWN ? 0 : wave), mine = max(0, (t_end - t_wave + STEP - 1) / STEP);  // tiles t_wave + STEP j
+    const int t_wave = t_begin + (OWN ? wave % step : wave), mine = max(0, (t_end - t_wave + step - 1) / step);  // tiles t_wave + step j
 
     const uint16_t* Kb = PAGED ? a.K : a.K + b * a.sb + h * a.sh;
     const uint16_t* Vb = PAGED ? a.V : a.V + b * a.sb + h * a.sh;
@@ -364,11 +407,11 @@ __global__ __launch_bounds__(DENSE_WAVES * 64) void dense_kernel(const DenseArgs
 #pragma unroll
     for (int i = 0; i < 4; ++i) off[i] = (4 * i + kg) * sn + (n ^ dense_swizzle(4 * i + kg)) * 8;
     auto request = [&](int j) {
-        const int row0 = (t_wave + STEP * j) * 16;
+        const int row0 = (t_wave + step * j) * 16;
         int64_t at = row0 * sn;
         if constexpr (PAGED) {
             if (j % 64 == 0) {
-                const int n0 = row_first + min(row0 + lane * (16 * STEP), L - 1);
+                const int n0 = row_first + min(row0 + lane * (16 * step), L - 1);
                 page = clampi(a.pv.table[(int64_t)b * a.pv.max_blocks + (n0 >> a.pv.shift)], 0, a.pv.n_pages - 1);
             }
             const int p = __builtin_amdgcn_readlane(page, j % 64);
@@ -416,7 +459,7 @@ __global__ __launch_bounds__(DENSE_WAVES * 64) void dense_kernel(const DenseArgs
     auto compute = [&](int j) {
         const char* t = ring + (j % DENSE_RING) * DENSE_TILE_BYTES;
         const int after = mine - 1 - j;
-        const int left = min(L - (t_wave + STEP * j) * 16, 16);
+        const int left = min(L - (t_wave + step * j) * 16, 16);
         wait_tile<4>(after);
         // (fp32 forms: four sums of 32 channels instead of one of 128, for the same reason as above)
         f32x4_t sacc, part[4];
@@ -544,7 +587,7 @@ __global__ __launch_bounds__(DENSE_WAVES * 64) void dense_kernel(const DenseArgs
     for (int j = 0; j < mine; ++j) compute(j);
 
     if constexpr (OWN) {
-        dense_own_end<VH>(a, d, ring, m_run, l_run, acc, pre, np, np_row, np_step, outp, outp32);
+        dense_own_end<VH>(a, d, smem, s_m, s_l, m_run, l_run, acc, pre, np, np_row, np_step, idle, outp, outp32);
         return;
     }
     // ---- the eight states of the workgroup ----
@@ -713,6 +756,12 @@ hipError_t prepare_dense() {  // (more than 64 KB of dynamic LDS has to be asked
     return hipSuccess;
 }
 
+// Waves of a team: as many units as fit on the compute units at once that way
+int dense_own_team(int B, int Hkv) {
+    int team = DENSE_WAVES;
+    while (team > 1 && B * Hkv * team > 256 * DENSE_WAVES) team /= 2;
+    return team;
+}
 int dense_own_wgs(int B, int Hkv) { return std::max(256, (B * Hkv + DENSE_WAVES - 1) / DENSE_WAVES); }
 
 hipError_t launch_dense(const hata_ctx* c, const void* q, const void* K, const void* V, const int32_t* seq_len, int B,
@@ -727,6 +776,7 @@ hipError_t launch_dense(const hata_ctx* c, const void* q, const void* K, const v
     a.B = B;
     a.pv = PageView{nullptr, 0, 0, 0};
     a.plan = c->prefix_plan;
+    a.team = dense_own_team(B, f.Hkv);
     a.pre = c->prefix_part;
     a.pre_rows = pre_rows;
     if (pages) {

@@ -14,7 +14,7 @@
 #define HATA_DENSE_ROUNDS 4
 
 namespace hata {
-// Of a sequence in a call with groups that share rows: its rows behind the shared ones, in `runs` runs a KV head for a wave each (waves
+// Of a sequence in a call with groups that share rows: its rows behind the shared ones, in `runs` runs a KV head for a team each (teams
 // start .. start + runs * Hkv - 1 of the launch), and the partial results of the shared rows: `splits` a KV head from item on, `step`
 // apart, its query rows from `row` on
 struct PrefixPlan {
@@ -107,7 +107,8 @@ hipError_t launch_dense(const hata_ctx* c, const void* q, const void* K, const v
 // launch_dense is then given as pre_rows) query rows each, and prefix_plan
 #define HATA_PREFIX_GROUPS 1024  // groups beyond share nothing
 size_t prefix_part_floats(int B, int Hkv, int G);
-int dense_own_wgs(int B, int Hkv);  // workgroups of the launch behind
+int dense_own_wgs(int B, int Hkv);  // workgroups of the launch behind, and waves of its teams
+int dense_own_team(int B, int Hkv);
 hipError_t prepare_prefix();  // once per context
 hipError_t launch_prefix(const hata_ctx* c, const void* q, const void* K, const void* V, const PageView& pages, const int32_t* seq_len, int B,
                          const int32_t* group_start, const int32_t* shared_len, int n_groups, float sm_scale, int* part_rows, hipStream_t s);

@@ -34,7 +34,7 @@ struct PrefixArgs {
     PrefixPlan* plan;
     float* part;
     PageView pv;
-    int B, Hq, Hkv, G, L_cap, n_groups, own_waves;  // own_waves: of the launch behind
+    int B, Hq, Hkv, G, L_cap, n_groups, own_teams, own_run;  // of the launch behind: teams, and the fewest tiles of a run
     float scale_log2;
 };
 
@@ -162,9 +162,9 @@ __device__ __forceinline__ bool prefix_share(const PrefixArgs& a, int mpt, int* 
     return w.g >= 0;
 }
 
-// The plan for the rows that are left to the sequences: where they begin, and runs of them for the waves of the launch behind -- the
-// shortest run length (at least PREFIX_OWN_RUN tiles of 16 rows) at which its waves suffice.
-#define PREFIX_OWN_RUN 4
+// The plan for the rows that are left to the sequences: where they begin, and runs of them for the teams of the launch behind -- the
+// shortest run length (at least PREFIX_OWN_RUN tiles of 16 rows a wave) at which its teams suffice.
+#define PREFIX_OWN_RUN 2
 #define PREFIX_OWN_RUNS 256  // of a unit
 __device__ __forceinline__ void prefix_plan(const PrefixArgs& a, int mpt, int* lds) {
     const int n = a.n_groups, tid = threadIdx.x, lane = tid & 63;
@@ -198,12 +198,12 @@ __device__ __forceinline__ void prefix_plan(const PrefixArgs& a, int mpt, int* l
         all += wave_sum64((float)tiles(b0 + lane));
         longest = fmaxf(longest, wave_max64((float)tiles(b0 + lane)));
     }
-    int run = max(PREFIX_OWN_RUN, (int)ceilf(all * (float)a.Hkv / (float)a.own_waves));
+    int run = max(a.own_run, (int)ceilf(all * (float)a.Hkv / (float)a.own_teams));
     auto runs = [&](int b) { return (uint32_t)min((tiles(b) + run - 1) / run, PREFIX_OWN_RUNS); };
     for (;; run += max(1, run >> 4)) {
         uint32_t w = 0;
         for (int b0 = 0; b0 < a.B; b0 += 64) w += (uint32_t)__builtin_amdgcn_readlane((int)wave_incl_scan(runs(b0 + lane)), 63);
-        if (w * (uint32_t)a.Hkv <= (uint32_t)a.own_waves || run >= (int)longest) break;
+        if (w * (uint32_t)a.Hkv <= (uint32_t)a.own_teams || run >= (int)longest) break;
     }
     uint32_t start = 0;
     for (int b0 = 0; b0 < a.B; b0 += 64) {
@@ -285,6 +285,10 @@ __global__ __launch_bounds__(256, 1) void prefix_kernel(const PrefixArgs a) {
     uint32_t off[4];
 #pragma unroll
     for (int i = 0; i < 4; ++i) off[i] = (4 * i + (lane >> 4)) * 256 + ((lane & 15) ^ (lane >> 4 << 2 | i)) * 16;
+    // (written as instructions: behind the compiler's builtin for it, every LDS read waits for all requests)
+    auto fetch = [&](uint32_t dst, uint32_t o, const uint16_t* p) {
+        asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(dst), "v"(o), "s"(p) : "memory", "m0");
+    };
     auto request = [&](int s) {
 #pragma unroll
         for (int j = 0; j < BLOCKS; ++j) {
@@ -293,9 +297,8 @@ __global__ __launch_bounds__(256, 1) void prefix_kernel(const PrefixArgs a) {
             const uint32_t dst = ring + (uint32_t)((s % NBUF) * STAGE * 512 + (wk * PART + (wq * BLOCKS + j) * 16) * 256);
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-                // (written as instructions: behind the compiler's builtin for it, every LDS read waits for all requests)
-                asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(dst + i * 1024), "v"(off[i]), "s"(a.K + at) : "memory", "m0");
-                asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(dst + STAGE * 256 + i * 1024), "v"(off[i]), "s"(a.V + at) : "memory", "m0");
+                fetch(dst + i * 1024, off[i], a.K + at);
+                fetch(dst + STAGE * 256 + i * 1024, off[i], a.V + at);
             }
         }
         look_up(s + 1);
@@ -397,8 +400,9 @@ __global__ __launch_bounds__(256, 1) void prefix_kernel(const PrefixArgs a) {
     };
     auto at_stage = [&](int s) { return (const char*)smem + (s % NBUF) * STAGE * 512 + wk * PART * 256; };  // K; V is STAGE * 256 bytes behind
 
+    // (with several query waves a stage behind the last one is the last rows once more: as many requests are outstanding everywhere)
     for (int s = 0; s < NBUF - (WQ > 1); ++s)
-        if (s < stages) request(s);
+        if (WQ > 1 || s < stages) request(s);
 #pragma unroll
     for (int t = 0; t < 2; ++t)
 #pragma unroll
@@ -430,8 +434,7 @@ __global__ __launch_bounds__(256, 1) void prefix_kernel(const PrefixArgs a) {
         // of stale LDS and not used)
         f32x16_t sc[2], next[2];
         float top[2];
-        if (stages >= NBUF - 1) prefix_wait<(NBUF - 2) * BLOCKS * 8>();  // (so many were requested)
-        else prefix_wait<0>();
+        prefix_wait<(NBUF - 2) * 8>();
         __syncthreads();
         products(at_stage(0), sc);
         highest(sc, top);
@@ -440,12 +443,21 @@ __global__ __launch_bounds__(256, 1) void prefix_kernel(const PrefixArgs a) {
             for (int i = 0; i < SUBS; ++i) {
                 uint32_t p[2][8];
                 follow(top);
-                if (i + 1 == SUBS && s + 1 < stages) {
-                    // stage s + 1 is there once only the one behind it is outstanding; everybody is done with stage s - 1
-                    if (s + 2 < stages) prefix_wait<(NBUF - 3) * BLOCKS * 8>();
-                    else prefix_wait<0>();
+                // stage s + 1 is there once only the one behind it is outstanding; everybody is done with stage s - 1, whose place
+                // the requests of this turn fill
+                static_assert(BLOCKS == 1, "eight requests a stage");
+                const bool turn = i + 1 == SUBS;
+                uint32_t dst = 0;
+                const uint16_t *k_from = nullptr, *v_from = nullptr;
+                if (turn) {
+                    prefix_wait<(NBUF - 3) * 8>();
                     __syncthreads();
-                    if (s + NBUF - 1 < stages) request(s + NBUF - 1);
+                    const int row = first_row(s + NBUF - 1, 0), page = clampi(pages[0], 0, a.pv.n_pages - 1);
+                    const int64_t at = ((((int64_t)page * a.Hkv + w.h) << a.pv.shift) + (row & ((1 << a.pv.shift) - 1))) * HATA_D;
+                    dst = ring + (uint32_t)(((s + NBUF - 1) % NBUF) * STAGE * 512 + (wk * PART + wq * 16) * 256);
+                    k_from = a.K + at;
+                    v_from = a.V + at;
+                    look_up(s + NBUF);
                 }
                 // (left to itself the compiler puts the matrix instructions one behind the other)
                 const char* kt = i + 1 < SUBS ? at_stage(s) + (i + 1) * 32 * 256 : at_stage(s + 1);
@@ -477,6 +489,7 @@ __global__ __launch_bounds__(256, 1) void prefix_kernel(const PrefixArgs a) {
                     if (j + 1 < 16) power(j + 1);
                     if (j + 2 < 16) argument(j + 2);
                     round(j);
+                    if (turn && j % 2 == 0) fetch(dst + (j / 4) * 1024 + (j / 2 % 2) * STAGE * 256, off[j / 4], j / 2 % 2 ? v_from : k_from);
                     __builtin_amdgcn_sched_barrier(0);
                 }
                 auto v_piece_at = [&](int j) {  // channels 32 (j % 4) of rows 16 (j / 4) ..
@@ -519,6 +532,7 @@ __global__ __launch_bounds__(256, 1) void prefix_kernel(const PrefixArgs a) {
     }
 
     // ---- the waves' sums, joined where they have the same query rows ----
+    prefix_wait<0>();
     __syncthreads();  // the ring is no longer read
     float* s_acc = reinterpret_cast<float*>(smem);  // [wave][64][HATA_D + 4]
     __shared__ float s_m[4][64], s_l[4][64];
@@ -620,7 +634,9 @@ hipError_t launch_prefix(const hata_ctx* c, const void* q, const void* K, const 
     a.q = (const uint16_t*)q; a.K = (const uint16_t*)K; a.V = (const uint16_t*)V;
     a.seq_len = seq_len; a.group_start = group_start; a.shared_len = shared_len;
     a.plan = c->prefix_plan;
-    a.own_waves = dense_own_wgs(B, f.Hkv) * 8;
+    const int team = dense_own_team(B, f.Hkv);
+    a.own_teams = dense_own_wgs(B, f.Hkv) * 8 / team;
+    a.own_run = PREFIX_OWN_RUN * team;
     a.part = c->prefix_part;
     a.pv = pages;
     a.B = B; a.Hq = f.Hq; a.Hkv = f.Hkv; a.G = c->G;
