@@ -241,28 +241,51 @@ __device__ __forceinline__ void dense_own_end(const DenseArgs& a, const DenseSha
         const bool none = idle || g0 >= G;
         float M[2 * KI], L[2 * KI];
         float4 sum[KI];
-        // the team's waves
+        // the team's waves (all of their LDS reads together)
+        auto member = [&](int w) { return first_wave + min(w, a.team - 1); };
+        if (KI > 4 || a.team == 1) {  // (more than eight heads a wave: it is alone)
 #pragma unroll
-        for (int j = 0; j < 2 * KI; ++j) {
-            const int g = min(g0 + j, G - 1);
-            M[j] = s_m[first_wave][g];
-            for (int w = 1; w < a.team; ++w) M[j] = fmaxf(M[j], s_m[first_wave + w][g]);
-            L[j] = 0.f;
-            for (int w = 0; w < a.team; ++w) {
-                const float m = s_m[first_wave + w][g];
-                L[j] = fmaf(m == HATA_NEG_INF ? 1.f : fast_exp2(m - M[j]), s_l[first_wave + w][g], L[j]);  // (sums without a score are zero)
+            for (int j = 0; j < 2 * KI; ++j) {
+                M[j] = s_m[wave][min(g0 + j, G - 1)];
+                L[j] = s_l[wave][min(g0 + j, G - 1)];
             }
-        }
 #pragma unroll
-        for (int k = 0; k < KI; ++k) {
-            const int i = min(32 * g0 + lane + 64 * k, 32 * G - 1), at = i / 32 * (HATA_D + 4) + i % 32 * 4;
-            const float top = lane < 32 ? M[2 * k] : M[2 * k + 1];
-            sum[k] = make_float4(0.f, 0.f, 0.f, 0.f);
-            for (int w = 0; w < a.team; ++w) {
-                const float m = s_m[first_wave + w][i / 32], f = m == HATA_NEG_INF ? 1.f : fast_exp2(m - top);
-                const float4 v = *reinterpret_cast<const float4*>(&state_of(first_wave + w)[at]);
-                sum[k].x = fmaf(f, v.x, sum[k].x); sum[k].y = fmaf(f, v.y, sum[k].y);
-                sum[k].z = fmaf(f, v.z, sum[k].z); sum[k].w = fmaf(f, v.w, sum[k].w);
+            for (int k = 0; k < KI; ++k) {
+                const int i = min(32 * g0 + lane + 64 * k, 32 * G - 1);
+                sum[k] = *reinterpret_cast<const float4*>(&s_acc[i / 32 * (HATA_D + 4) + i % 32 * 4]);
+            }
+        } else {
+            float f[2 * KI][DENSE_WAVES];
+#pragma unroll
+            for (int j = 0; j < 2 * KI; ++j) {
+                const int g = min(g0 + j, G - 1);
+                float l[DENSE_WAVES];
+#pragma unroll
+                for (int w = 0; w < DENSE_WAVES; ++w) { f[j][w] = s_m[member(w)][g]; l[w] = s_l[member(w)][g]; }
+                M[j] = f[j][0];
+#pragma unroll
+                for (int w = 1; w < DENSE_WAVES; ++w) M[j] = fmaxf(M[j], f[j][w]);
+                L[j] = 0.f;
+#pragma unroll
+                for (int w = 0; w < DENSE_WAVES; ++w) {
+                    f[j][w] = f[j][w] == HATA_NEG_INF ? 1.f : fast_exp2(f[j][w] - M[j]);  // (sums without a score are zero)
+                    if (w < a.team) L[j] = fmaf(f[j][w], l[w], L[j]);
+                }
+            }
+#pragma unroll
+            for (int k = 0; k < KI; ++k) {
+                const int i = min(32 * g0 + lane + 64 * k, 32 * G - 1), at = i / 32 * (HATA_D + 4) + i % 32 * 4;
+                float4 v[DENSE_WAVES];
+#pragma unroll
+                for (int w = 0; w < DENSE_WAVES; ++w) v[w] = *reinterpret_cast<const float4*>(&state_of(member(w))[at]);
+                sum[k] = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+                for (int w = 0; w < DENSE_WAVES; ++w)
+                    if (w < a.team) {
+                        const float x = lane < 32 ? f[2 * k][w] : f[2 * k + 1][w];
+                        sum[k].x = fmaf(x, v[w].x, sum[k].x); sum[k].y = fmaf(x, v[w].y, sum[k].y);
+                        sum[k].z = fmaf(x, v[w].z, sum[k].z); sum[k].w = fmaf(x, v[w].w, sum[k].w);
+                    }
             }
         }
         int own = 0;
@@ -577,6 +600,16 @@ __global__ __launch_bounds__(DENSE_WAVES * 64) void dense_kernel(const DenseArgs
                                                                  __builtin_bit_cast(bf16x8_t, pb), acc[c], 0, 0, 0);
         }
     };
+    // the shared rows' partial results, which other compute units have written, on their way into this one's L2: a word of each line
+    [[maybe_unused]] float ahead[4];
+    if constexpr (OWN) {
+        const int lines = idle ? 0 : np * G * (HATA_D / 32);
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            const int i = min((k * step + wave % step) * 64 + lane, lines - 1), per = G * (HATA_D / 32);
+            ahead[k] = lines ? pre[(int64_t)(i / per) * np_step * a.pre_rows * (HATA_D + 2) + np_row * HATA_D + i % per * 32] : 0.f;
+        }
+    }
     for (int j = 0; j < min(mine, DENSE_RING); ++j) request(j);
 #pragma unroll
     for (int s = 0; s < 4; ++s) {
@@ -587,6 +620,7 @@ __global__ __launch_bounds__(DENSE_WAVES * 64) void dense_kernel(const DenseArgs
     for (int j = 0; j < mine; ++j) compute(j);
 
     if constexpr (OWN) {
+        asm volatile("" ::"v"(ahead[0]), "v"(ahead[1]), "v"(ahead[2]), "v"(ahead[3]));
         dense_own_end<VH>(a, d, smem, s_m, s_l, m_run, l_run, acc, pre, np, np_row, np_step, idle, outp, outp32);
         return;
     }

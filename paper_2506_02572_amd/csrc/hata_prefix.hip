@@ -8,9 +8,9 @@
 //     192 registers) and goes over 32 rows at a time on v_mfma_f32_32x32x16_bf16: S^T = K Q^T, O^T += V^T P^T.  In S^T a lane has 16
 //     rows of ONE query row, which are what the second product wants from it as P: nothing crosses lanes.
 //   - WQ waves share what they read (rows come into LDS by direct loads, 64 of K and of V a stage), 4 / WQ go over different rows.
-//   - The maximum is followed loosely: a wave scales its sums (1500 cycles, as much as the products of 32 rows) only where a score
-//     passes the one in use by 2^40.  Sums and weights are floating-point numbers, nothing is lost by it as long as no value is as
-//     large as 2^70 (2^127 less the weight and 2^17 rows).
+//   - The maximum is followed loosely: scaling a wave's sums takes 1500 cycles, as much as the products of 32 rows, so the reference
+//     m_i is set PREFIX_LOOSE (binary) orders above the highest score when one passes it.  Weights are at most 1 all the same, and as
+//     floating-point numbers keep their precision; what is lost are weights 2^-70 of the largest, and values below 2^-70.
 //   - Weights are rounded to bf16 (to nearest: half a step, 2^-8 relative; their sum is of the rounded ones), which halves the second
 //     product against two terms, and the matrix cores are what bounds groups of more than some 200 query rows a KV head.
 #include <algorithm>
@@ -25,7 +25,7 @@ typedef __attribute__((ext_vector_type(2))) float f32x2_t;
 
 #define PREFIX_TILE 64       // rows that runs are cut by; what is left of the common rows is read by every sequence itself
 #define PREFIX_MAX_SPLITS 256
-#define PREFIX_LOOSE 40.f
+#define PREFIX_LOOSE 56.f
 #define PREFIX_LDS (4 * 64 * (HATA_D + 4) * 4)  // the waves' sums at the end; before, the ring of stages
 
 struct PrefixArgs {
@@ -194,16 +194,19 @@ __device__ __forceinline__ void prefix_plan(const PrefixArgs& a, int mpt, int* l
     __syncthreads();
     auto tiles = [&](int b) { return b < a.B ? (max(rows[b], 1) + 15) / 16 : 0; };
     float all = 0.f, longest = 0.f;
-    for (int b0 = 0; b0 < a.B; b0 += 64) {
-        all += wave_sum64((float)tiles(b0 + lane));
-        longest = fmaxf(longest, wave_max64((float)tiles(b0 + lane)));
+    for (int b = lane; b < a.B; b += 64) {
+        all += (float)tiles(b);
+        longest = fmaxf(longest, (float)tiles(b));
     }
+    all = wave_sum64(all);
+    longest = wave_max64(longest);
     int run = max(a.own_run, (int)ceilf(all * (float)a.Hkv / (float)a.own_teams));
+    if (a.B * a.Hkv >= a.own_teams) run = max(run, (int)longest);  // (one a unit)
     auto runs = [&](int b) { return (uint32_t)min((tiles(b) + run - 1) / run, PREFIX_OWN_RUNS); };
     for (;; run += max(1, run >> 4)) {
-        uint32_t w = 0;
-        for (int b0 = 0; b0 < a.B; b0 += 64) w += (uint32_t)__builtin_amdgcn_readlane((int)wave_incl_scan(runs(b0 + lane)), 63);
-        if (w * (uint32_t)a.Hkv <= (uint32_t)a.own_teams || run >= (int)longest) break;
+        float n = 0.f;  // (below 2^24)
+        for (int b = lane; b < a.B; b += 64) n += (float)runs(b);
+        if (wave_sum64(n) * (float)a.Hkv <= (float)a.own_teams || run >= (int)longest) break;
     }
     uint32_t start = 0;
     for (int b0 = 0; b0 < a.B; b0 += 64) {
@@ -348,14 +351,14 @@ __global__ __launch_bounds__(256, 1) void prefix_kernel(const PrefixArgs a) {
             top[t] *= scale;
         }
     };
-    // the maxima in use, where the highest scores pass one by far
+    // the references, where the highest scores pass one
     auto follow = [&](const float (&top)[2]) {
-        if (__builtin_amdgcn_ballot_w64(top[0] > m[0] + PREFIX_LOOSE || top[1] > m[1] + PREFIX_LOOSE) != 0ull) {
+        if (__builtin_amdgcn_ballot_w64(top[0] > m[0] || top[1] > m[1]) != 0ull) {
 #pragma unroll
             for (int t = 0; t < 2; ++t) {
                 float x, y;
                 swap32(top[t], x, y);
-                const float to = fmaxf(fmaxf(x, y), m[t]);  // of both halves' rows
+                const float high = fmaxf(x, y), to = high > m[t] ? high + PREFIX_LOOSE : m[t];  // (both halves' rows)
                 const float f = m[t] == HATA_NEG_INF ? (to == HATA_NEG_INF ? 1.f : 0.f) : fast_exp2(m[t] - to);
                 l[t] *= f;
 #pragma unroll
@@ -400,15 +403,17 @@ __global__ __launch_bounds__(256, 1) void prefix_kernel(const PrefixArgs a) {
     };
     auto at_stage = [&](int s) { return (const char*)smem + (s % NBUF) * STAGE * 512 + wk * PART * 256; };  // K; V is STAGE * 256 bytes behind
 
-    // (with several query waves a stage behind the last one is the last rows once more: as many requests are outstanding everywhere)
-    for (int s = 0; s < NBUF - (WQ > 1); ++s)
-        if (WQ > 1 || s < stages) request(s);
+    // (the wait for the query rows is one for every request so far: the first stage's only)
+    request(0);
 #pragma unroll
     for (int t = 0; t < 2; ++t)
 #pragma unroll
         for (int s = 0; s < 8; ++s)  // (used here, so that the wait for these loads is not in the loop)
             asm volatile("" : "+a"(qb[t][s].x), "+a"(qb[t][s].y), "+a"(qb[t][s].z), "+a"(qb[t][s].w));
     pin();
+    // (with several query waves a stage behind the last one is the last rows once more: as many requests are outstanding everywhere)
+    for (int s = 1; s < NBUF - (WQ > 1); ++s)
+        if (WQ > 1 || s < stages) request(s);
     if constexpr (WQ == 1) {
         // rows of this wave alone: nothing is waited for but its own requests
         for (int s = 0; s < stages; ++s) {
