@@ -693,14 +693,14 @@ int hata_dense_decode_paged(hata_ctx* ctx, const void* q, const void* K_pool, co
     if (rc != HATA_OK) return rc;
     if (!q || !K_pool || !V_pool || !seq_len || !out) return HATA_EINVAL;
     if (n_groups < 0 || n_groups > B || (n_groups > 0 && (!group_start || !shared_len))) return HATA_EINVAL;
-    if (!aligned(q, 16) || !aligned(K_pool, 16) || !aligned(V_pool, 16) || !aligned(out, 2) || !aligned(out_f32, 4) ||
+    if (!aligned(q, 16) || !aligned(K_pool, 16) || !aligned(V_pool, 16) || !aligned(out, 8) || !aligned(out_f32, 16) ||
         !aligned(block_table, 4) || !aligned(seq_len, 4) || !aligned(group_start, 4) || !aligned(shared_len, 4))
         return HATA_EINVAL;
     hata::PageView pv;
     rc = make_page_view(ctx, block_table, max_blocks, page_rows, n_pages, &pv);
     if (rc != HATA_OK) return rc;
     int pre_rows = 0;
-    if (n_groups > 0 && B > 1) {
+    if (n_groups > 0 && B > 1 && B <= HATA_PREFIX_MAX_B) {
         const hipError_t e = hata::launch_prefix(ctx, q, K_pool, V_pool, pv, seq_len, B, group_start, shared_len,
                                                  n_groups < HATA_PREFIX_GROUPS ? n_groups : HATA_PREFIX_GROUPS, sm_scale, &pre_rows,
                                                  (hipStream_t)stream);

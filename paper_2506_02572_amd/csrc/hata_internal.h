@@ -105,7 +105,8 @@ hipError_t launch_dense(const hata_ctx* c, const void* q, const void* K, const v
                         float sm_scale, void* out, float* out_f32, hipStream_t s, const PageView* pages = nullptr, int pre_rows = 0);
 // Rows that groups of sequences share, in front of launch_dense of the same call: partial results in prefix_part, *part_rows (which
 // launch_dense is then given as pre_rows) query rows each, and prefix_plan
-#define HATA_PREFIX_GROUPS 1024  // groups beyond share nothing
+#define HATA_PREFIX_GROUPS 1024  // groups beyond share nothing, and neither do batches of more sequences (what a workgroup has LDS for)
+#define HATA_PREFIX_MAX_B 16384
 size_t prefix_part_floats(int B, int Hkv, int G);
 int dense_own_wgs(int B, int Hkv);  // workgroups of the launch behind, and waves of its teams
 int dense_own_team(int B, int Hkv);

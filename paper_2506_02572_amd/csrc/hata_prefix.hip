@@ -1,7 +1,7 @@
 // Decode attention over rows that a group of sequences has in common (Eq. 1 of the paper, block tables): read once for all of
 // them.  For the query rows i of a group's members (member by member, the G heads of a KV head side by side) and a run of the
 // common rows,
-//   m_i = max_n s_in,  l_i = sum_n 2^(s_in - m_i),  o_i = sum_n 2^(s_in - m_i) V_n,   s_in = scale log2(e) q_i . K_n,
+//   l_i = sum_n 2^(s_in - m_i),  o_i = sum_n 2^(s_in - m_i) V_n,   s_in = scale log2(e) q_i . K_n,  m_i >= max_n s_in,
 // which dense_kernel joins with the sequences' own rows.
 //
 //   - A workgroup of four waves has a tile of 64 WQ query rows and a run of rows.  A wave holds 64 query rows (operands and sums:
@@ -170,6 +170,7 @@ __device__ __forceinline__ void prefix_plan(const PrefixArgs& a, int mpt, int* l
     const int n = a.n_groups, tid = threadIdx.x, lane = tid & 63;
     const PrefixGroups s = prefix_groups(a, lds);
     int* rows = lds + 5 * n + 1;  // [B] behind the shared ones
+    static_assert((5 * HATA_PREFIX_GROUPS + 1 + HATA_PREFIX_MAX_B) * 4 <= PREFIX_LDS, "room for the plan");
     for (int b = tid; b < a.B; b += 256) {
         const int L = clampi(a.seq_len[b], 0, a.L_cap);
         rows[b] = L;
@@ -614,6 +615,7 @@ static int64_t prefix_wgs(int B, int Hkv, int G, int n_groups, int waves) {
 
 size_t prefix_part_floats(int B, int Hkv, int G) {
     if (B < 2) return 0;
+    B = std::min(B, HATA_PREFIX_MAX_B);
     size_t most = 0;
     for (int waves = 1; waves <= 4; waves *= 2) {
         // the most groups that go by so many waves

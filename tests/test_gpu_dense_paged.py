@@ -316,6 +316,6 @@ def test_refusals(hata):
     for bad in ({"h": None}, {"q": None}, {"K": None}, {"V": None}, {"table": None}, {"max_blocks": 0}, {"P": 8}, {"P": 24},
                 {"n_pages": 0}, {"n_pages": 1 << 27}, {"max_blocks": 1 << 27}, {"seq": None}, {"B": 0}, {"B": 5}, {"n": -1},
                 {"n": 5, "gs": p, "sl": p}, {"n": 1, "sl": p}, {"n": 1, "gs": p}, {"out": None}, {"q": p + 8}, {"K": p + 2},
-                {"V": p + 8}, {"out": p + 1}, {"out32": p + 2}, {"seq": p + 1}, {"n": 1, "gs": p + 2, "sl": p}, {"table": p + 2}):
+                {"V": p + 8}, {"out": p + 4}, {"out32": p + 8}, {"seq": p + 1}, {"n": 1, "gs": p + 2, "sl": p}, {"table": p + 2}):
         assert call(**bad) == -1, bad
     ctx.close()
