@@ -73,6 +73,8 @@ class World:
         page, row = torch.from_numpy(self.table[b, n // self.P].astype(np.int64)).cuda(), torch.from_numpy(n % self.P).cuda()
         return pool[page, :, row].double()  # [n, Hkv, D]
 
+    scale = SCALE
+
     def exact(self):
         """The outputs, and per output the sum of weight times absolute value: what a relative error of the weights costs."""
         import torch
@@ -84,7 +86,7 @@ class World:
                 continue
             K, V = self.rows(self.K, b), self.rows(self.V, b)
             for h in range(self.Hkv):
-                p = torch.softmax(self.q[b, h * G:(h + 1) * G].double() @ K[:, h].T * SCALE, dim=1)
+                p = torch.softmax(self.q[b, h * G:(h + 1) * G].double() @ K[:, h].T * self.scale, dim=1)
                 out[b, h * G:(h + 1) * G] = p @ V[:, h]
                 size[b, h * G:(h + 1) * G] = p @ V[:, h].abs()
         return out, size
@@ -103,7 +105,7 @@ class World:
             self.out32.fill_(float("nan"))
             torch.cuda.synchronize()
         self.ctx.hata_dense_decode_paged(self.q, self.K, self.V, t, self.width, self.P, self.n_pages, lens, self.B,
-                                         starts if n else None, shared if n else None, n, SCALE, self.out, self.out32,
+                                         starts if n else None, shared if n else None, n, self.scale, self.out, self.out32,
                                          stream=stream)
         return self.out, self.out32
 
@@ -262,6 +264,106 @@ def test_large_logits(hata):
         for b in range(w.B):
             w.K[int(w.table[b, row // 16]), :, row % 16] = 30.0
         w.check()
+
+
+@pytest.mark.parametrize("scale", [-SCALE, 0.0, 1e-30, 2.0])
+def test_scales(hata, scale):
+    w = World([2100 + i for i in range(20)], [(20, 2048)], Hq=8, Hkv=2, P=16, seed=5, outliers=False)
+    w.scale = scale
+    w.check()
+
+
+@pytest.mark.parametrize("exponent", [-60, 60, 125])
+def test_values_of_every_size(hata, exponent):
+    """Values near the largest and smallest that the sums can hold: no weight is above 1, so nothing overflows on the way."""
+    w = World([900 + i for i in range(20)], [(20, 832)], Hq=8, Hkv=2, P=16, seed=6, outliers=False)
+    w.V.copy_((w.V.double() * 2.0 ** exponent / 4).to(w.V.dtype))
+    w.check()
+
+
+def test_one_kv_head_many_splits(hata):
+    World([140000 + i for i in range(3)], [(3, 139968)], Hq=16, Hkv=1, P=32, seed=7).check()
+
+
+def test_context_larger_than_the_batch(hata):
+    w = World([700 + i for i in range(9)], [(5, 640), (4, 688)], Hq=8, Hkv=2, P=16, seed=8)
+    w.ctx.close()
+    w.ctx = hata.Context(300, 8, 2, D, 32, 4096, 64)
+    w.check()
+    w.check(groups=False)
+
+
+def test_more_groups_than_are_looked_at(hata):
+    """Pairs that share, 1100 of them: those behind the 1024th read their rows twice."""
+    World([80 + i % 7 for i in range(2200)], [(2, 64)] * 1100, Hq=2, Hkv=1, P=16, seed=9, outliers=False).check()
+
+
+def test_large_batches(hata):
+    """Every sequence has the same rows and query: the answer of one, of all of them."""
+    import torch
+    one = World([100], Hq=2, Hkv=1, P=16, seed=10, outliers=False)
+    want, _ = one.check()
+    for B in (5000, 16384, 20000):
+        ctx = hata.Context(B, 2, 1, D, 32, 112, 64)
+        i32 = lambda a: torch.tensor(a, dtype=torch.int32, device="cuda")
+        q = one.q.expand(B, 2, D).contiguous()
+        table = torch.from_numpy(one.table).cuda().expand(B, one.width).contiguous()
+        out = torch.full((B, 2, D), float("nan"), dtype=torch.bfloat16, device="cuda")
+        for groups in (0, 1, 2):
+            ctx.hata_dense_decode_paged(q, one.K, one.V, table, one.width, 16, one.n_pages, i32([100] * B), B, i32([0, B // 3, B]),
+                                        i32([64, 96]), groups, SCALE, out)
+            torch.cuda.synchronize()
+            assert bool(((out.double() - want).abs() <= 2.0 ** -6 * want.abs().max()).all()), (B, groups)
+        ctx.close()
+
+
+def test_pools_beyond_four_gigabytes(hata):
+    """Pages at the far end of pools of 4.6 GB each: row offsets that pass 32 bits."""
+    import torch
+    w = World([520 + i for i in range(6)] + [333], [(6, 512)], Hq=16, Hkv=8, P=32, seed=11)
+    far = 70000 - w.n_pages
+    for name in ("K", "V"):
+        pool = torch.empty((70000, w.Hkv, w.P, D), dtype=torch.bfloat16, device="cuda")
+        pool[far:] = getattr(w, name)
+        setattr(w, name, pool)
+    w.table = np.where((w.table >= 0) & (w.table < w.n_pages), w.table + far, w.table).astype(np.int32)
+    w.n_pages = 70000
+    ref = w.check()
+    w.check(groups=False, ref=ref)
+    # rows written there through a slot map
+    T = 300
+    x = torch.randn((T, 2, w.Hkv, D), device="cuda").to(torch.bfloat16)
+    slots = torch.arange(70000 * w.P - T, 70000 * w.P, dtype=torch.int32, device="cuda")
+    codes = torch.zeros((70000, w.Hkv, w.P, 1), dtype=torch.int32, device="cuda")
+    W = torch.randn((w.Hkv, D, 32), device="cuda")
+    for n in (T, 100):  # both forms
+        w.K[-T // w.P - 1:].zero_()
+        codes.zero_()
+        w.ctx.hata_write_slots(x[-n:, 0], x[-n:, 1], 2 * w.Hkv * D, D, slots[-n:], n, w.K, w.V, codes, w.P, w.n_pages, W)
+        torch.cuda.synchronize()
+        rows = w.K.transpose(1, 2)[-T // w.P - 1:].reshape(-1, w.Hkv, D)[-n:]
+        assert torch.equal(rows, x[-n:, 0])
+        bits = torch.einsum("thd,hdr->thr", x[-n:, 0].double(), W.double()) >= 0
+        words = (bits.long() << torch.arange(32, device="cuda")).sum(2)
+        got = codes.transpose(1, 2)[-T // w.P - 1:].reshape(-1, w.Hkv)[-n:].long() & 0xFFFFFFFF
+        assert torch.equal(got, words)
+
+
+def test_two_contexts_at_once(hata):
+    import torch
+    ws = [World([3000 + 7 * i for i in range(24)], [(24, 2992)], Hq=8, Hkv=2, P=16, seed=s) for s in (20, 21)]
+    refs = [w.exact() for w in ws]
+    streams = [torch.cuda.Stream() for _ in ws]
+    for w in ws:
+        w.run()
+    torch.cuda.synchronize()
+    for _ in range(10):
+        for w, s in zip(ws, streams):
+            w.run(stream=s, fill=False)
+    torch.cuda.synchronize()
+    for w, ref in zip(ws, refs):
+        err = (w.out32.double() - ref[0]).abs() - 2.0 ** -8 * (ref[1] + ref[0].abs()) - 2.0 ** -11 * ref[1]
+        assert bool((err <= 0).all())
 
 
 def test_twice_the_same_and_captured(hata):
