@@ -43,8 +43,8 @@ struct PrefixArgs {
 // Every workgroup works it out for itself: the groups' members, the rows they have in common, and the shortest run (in tiles) at
 // which the launch's workgroups suffice, one per (group, KV head, tile of query rows, run).  The tiles of query rows of a run are
 // neighbours on one XCD, whose L2 then serves all but the first of them.  The last workgroup writes the plan that the launch behind
-// goes by.  (A workgroup more than there are compute units would have to wait for one.)  It has nothing else to do, unless runs
-// would be longer by more than an eighth for that.
+// goes by.  (A workgroup more than there are compute units would have to wait for one.)  It has nothing else to do, unless the
+// others' runs would be longer for that by more than the plan takes (5 us; a tile of rows takes 0.6 us for 64 query rows).
 struct PrefixShare { int g, h, split, ns, qt, tiles, item, first, members, lead; };
 struct PrefixGroups { int *start, *least, *count, *lead; };  // in LDS: first member [n + 1]; tiles in common, members that have rows, the first of them [n]
 
@@ -124,7 +124,7 @@ __device__ __forceinline__ void prefix_items(const PrefixArgs& a, const PrefixGr
         if (items == (uint32_t)wgs && !with_last) with_last = run;  // (the workgroup with the plan would have an item too)
         if (items < (uint32_t)wgs || run >= (int)longest) break;
     }
-    if (with_last && 8 * run > 9 * with_last) run = with_last;
+    if (with_last && (run - with_last) * mpt * a.G > 8 * 64) run = with_last;
     uint32_t base = 0;
     for (int g0 = 0; g0 < n; g0 += 64) {
         const int g = g0 + lane, qt = g0 ? qtiles(g) : qt0, ns = splits(g0 ? tiles(g) : tiles0, run);
@@ -289,10 +289,14 @@ __global__ __launch_bounds__(256, 1) void prefix_kernel(const PrefixArgs a) {
     uint32_t off[4];
 #pragma unroll
     for (int i = 0; i < 4; ++i) off[i] = (4 * i + (lane >> 4)) * 256 + ((lane & 15) ^ (lane >> 4 << 2 | i)) * 16;
-    // (written as instructions: behind the compiler's builtin for it, every LDS read waits for all requests.  nt: 12 sequences behind
-    // 131072 rows 119 -> 108 us, 32 behind 32768 68 -> 63, and no loss where several tiles of query rows read the same)
+    // (written as instructions: behind the compiler's builtin for it, every LDS read waits for all requests.  nt where the rows are read
+    // by one tile of query rows, mostly: 12 sequences behind 131072 rows 119 -> 108 us, 32 behind 32768 68 -> 63; with eight tiles
+    // it is the same, and slower where the caches hold the rows already)
     auto fetch = [&](uint32_t dst, uint32_t o, const uint16_t* p) {
-        asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2 nt" ::"s"(dst), "v"(o), "s"(p) : "memory", "m0");
+        if constexpr (WQ <= 2)
+            asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2 nt" ::"s"(dst), "v"(o), "s"(p) : "memory", "m0");
+        else
+            asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(dst), "v"(o), "s"(p) : "memory", "m0");
     };
     auto request = [&](int s) {
 #pragma unroll
