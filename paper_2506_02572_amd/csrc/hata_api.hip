@@ -140,7 +140,7 @@ int make_plan(const hata_config* f, const hata_tuning* t, Plan* p) {
     const size_t dense_partials = (size_t)256 * HATA_DENSE_ROUNDS * G;  // a workgroup has one per head of its group
     if (n_partials < dense_partials) n_partials = dense_partials;
     p->dense_wgs_max = (int64_t)(n_partials / G);
-    const size_t own_partials = f->B_max > 1 ? (size_t)hata::dense_own_wgs(f->B_max, f->Hkv) * 8 * G : 0;  // (a wave has)
+    const size_t own_partials = f->B_max > 1 ? (size_t)hata::dense_own_wgs(f->B_max, f->Hkv, true) * 8 * G : 0;  // (a wave has)
     if (n_partials < own_partials) n_partials = own_partials;
     p->off_partials = o; o = align_up(o + n_partials * (128 + 2) * 4);
     p->off_wplanes = o;  o = align_up(o + (size_t)f->Hkv * 2 * 128 * f->r * 2);  // two fp16 planes

@@ -33,6 +33,7 @@ namespace hata {
 #define DENSE_TILE_BYTES 8192  // 16 rows of K, 16 rows of V
 #define DENSE_RUN 4            // tiles (of a wave) summed in a row where the weights stay fp32
 #define DENSE_MAX_RUNS 256     // of a unit (four partial results per lane in the merge)
+#define DENSE_OWN_SPARE 256    // workgroups more than fit at once, for sequences much longer than the others (DENSE_OWN)
 #define DENSE_BATCH 16         // partial results in flight per thread in the merge
 
 struct DenseArgs {
@@ -352,7 +353,10 @@ enum DenseForm { DENSE_BF16X2, DENSE_FP32_ONE_HEAD, DENSE_FP32_TWO_HEADS, DENSE_
 // at a time (a lane each).
 // DENSE_OWN: the same, for the rows that sequences do not share (prefix_kernel has been at the others).  They are few for many
 // units, so what is dealt out are runs for teams of `team` waves of a workgroup (1, 2, 4 or 8), by the plan of the launch before;
-// the last team of a unit to arrive joins its runs and the shared rows' partial results.
+// the last team of a unit to arrive joins its runs and the shared rows' partial results.  Eight KV heads, us of this launch:
+// 256 sequences of 1 to 500 rows, groups of eight heads, 77 with a wave for a unit (51 where all have 250: the long ones end
+// late), 171 with a workgroup for each, 135 with as many tiles for every wave, of one unit or several; 32 sequences of up to
+// 1024 rows, groups of four, 25 with teams of eight, 31 of four, 32 of two.
 enum DenseRows { DENSE_CONTIGUOUS, DENSE_PAGED, DENSE_OWN };
 template <DenseForm FORM, DenseRows ROWS>
 __global__ __launch_bounds__(DENSE_WAVES * 64) void dense_kernel(const DenseArgs a) {
@@ -393,6 +397,10 @@ __global__ __launch_bounds__(DENSE_WAVES * 64) void dense_kernel(const DenseArgs
             }
         }
         idle = d.b < 0;  // nothing left for this team (it still comes to the barriers)
+        if (idle) {  // nor for any of the workgroup?
+            const PrefixPlan x = a.plan[a.B - 1];
+            if ((int)(blockIdx.x * DENSE_WAVES) / a.team >= x.start + x.runs * a.Hkv) return;
+        }
         if (idle) d.b = 0;
     } else if (!dense_share(a.seq_len, a.B, a.Hkv, a.L_cap, d)) {
         return;
@@ -796,7 +804,9 @@ int dense_own_team(int B, int Hkv) {
     while (team > 1 && B * Hkv * team > 256 * DENSE_WAVES) team /= 2;
     return team;
 }
-int dense_own_wgs(int B, int Hkv) { return std::max(256, (B * Hkv + DENSE_WAVES - 1) / DENSE_WAVES); }
+int dense_own_wgs(int B, int Hkv, bool spare) {
+    return std::max(256, (B * Hkv + DENSE_WAVES - 1) / DENSE_WAVES) + (spare ? DENSE_OWN_SPARE : 0);
+}
 
 hipError_t launch_dense(const hata_ctx* c, const void* q, const void* K, const void* V, const int32_t* seq_len, int B,
                         float sm_scale, void* out, float* out_f32, hipStream_t s, const PageView* pages, int pre_rows) {
@@ -822,7 +832,7 @@ hipError_t launch_dense(const hata_ctx* c, const void* q, const void* K, const v
     const int64_t spare = splits == 1 && B > 1 ? std::max((int64_t)0, std::min((int64_t)256, c->dense_wgs_max - units)) : 0;
     a.sb = f.kv_stride_b; a.sh = f.kv_stride_h; a.sn = f.kv_stride_n;
     a.scale_log2 = sm_scale * 1.4426950408889634f;
-    const dim3 grid = pre_rows ? dim3((unsigned)dense_own_wgs(B, f.Hkv)) : B == 1 ? dim3((unsigned)splits, f.Hkv) : dim3((unsigned)(units * splits + spare));
+    const dim3 grid = pre_rows ? dim3((unsigned)dense_own_wgs(B, f.Hkv, true)) : B == 1 ? dim3((unsigned)splits, f.Hkv) : dim3((unsigned)(units * splits + spare));
 #define HATA_DENSE_FORM(F_) (pre_rows ? dense_kernel<F_, DENSE_OWN> : pages ? dense_kernel<F_, DENSE_PAGED> : dense_kernel<F_, DENSE_CONTIGUOUS>)
     const auto fn = c->HT >= 4 ? HATA_DENSE_FORM(DENSE_BF16X2) : c->G == 1 ? HATA_DENSE_FORM(DENSE_FP32_ONE_HEAD)
                     : c->G == 2 ? HATA_DENSE_FORM(DENSE_FP32_TWO_HEADS) : HATA_DENSE_FORM(DENSE_FP32);

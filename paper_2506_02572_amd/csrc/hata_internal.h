@@ -108,7 +108,7 @@ hipError_t launch_dense(const hata_ctx* c, const void* q, const void* K, const v
 #define HATA_PREFIX_GROUPS 1024  // groups beyond share nothing, and neither do batches of more sequences (what a workgroup has LDS for)
 #define HATA_PREFIX_MAX_B 16384
 size_t prefix_part_floats(int B, int Hkv, int G);
-int dense_own_wgs(int B, int Hkv);  // workgroups of the launch behind, and waves of its teams
+int dense_own_wgs(int B, int Hkv, bool spare);  // workgroups of the launch behind, and waves of its teams
 int dense_own_team(int B, int Hkv);
 hipError_t prepare_prefix();  // once per context
 hipError_t launch_prefix(const hata_ctx* c, const void* q, const void* K, const void* V, const PageView& pages, const int32_t* seq_len, int B,

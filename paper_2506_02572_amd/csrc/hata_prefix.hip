@@ -34,7 +34,7 @@ struct PrefixArgs {
     PrefixPlan* plan;
     float* part;
     PageView pv;
-    int B, Hq, Hkv, G, L_cap, n_groups, own_teams, own_run;  // of the launch behind: teams, and the fewest tiles of a run
+    int B, Hq, Hkv, G, L_cap, n_groups, own_teams, own_spare, own_run;  // of the launch behind: teams at once, with those to spare, and the fewest tiles of a run
     float scale_log2;
 };
 
@@ -201,14 +201,19 @@ __device__ __forceinline__ void prefix_plan(const PrefixArgs& a, int mpt, int* l
     }
     all = wave_sum64(all);
     longest = wave_max64(longest);
-    int run = max(a.own_run, (int)ceilf(all * (float)a.Hkv / (float)a.own_teams));
-    if (a.B * a.Hkv >= a.own_teams) run = max(run, (int)longest);  // (one a unit)
+    int run = 0;
     auto runs = [&](int b) { return (uint32_t)min((tiles(b) + run - 1) / run, PREFIX_OWN_RUNS); };
-    for (;; run += max(1, run >> 4)) {
-        float n = 0.f;  // (below 2^24)
-        for (int b = lane; b < a.B; b += 64) n += (float)runs(b);
-        if (wave_sum64(n) * (float)a.Hkv <= (float)a.own_teams || run >= (int)longest) break;
-    }
+    auto search = [&](int teams) {
+        run = max(a.own_run, (int)ceilf(all * (float)a.Hkv / (float)teams));
+        if (a.B * a.Hkv >= teams) run = max(run, (int)longest);  // (one a unit)
+        for (;; run += max(1, run >> 4)) {
+            float n = 0.f;  // (below 2^24)
+            for (int b = lane; b < a.B; b += 64) n += (float)runs(b);
+            if (wave_sum64(n) * (float)a.Hkv <= (float)teams || run >= (int)longest) return run;
+        }
+    };
+    const int spare = search(a.own_spare), at_once = search(a.own_teams);
+    if (at_once > 2 * spare + 8 * a.own_run) run = spare;  // (a second round of workgroups)
     uint32_t start = 0;
     for (int b0 = 0; b0 < a.B; b0 += 64) {
         const int b = b0 + lane;
@@ -647,7 +652,8 @@ hipError_t launch_prefix(const hata_ctx* c, const void* q, const void* K, const 
     a.seq_len = seq_len; a.group_start = group_start; a.shared_len = shared_len;
     a.plan = c->prefix_plan;
     const int team = dense_own_team(B, f.Hkv);
-    a.own_teams = dense_own_wgs(B, f.Hkv) * 8 / team;
+    a.own_teams = dense_own_wgs(B, f.Hkv, false) * 8 / team;
+    a.own_spare = dense_own_wgs(B, f.Hkv, true) * 8 / team;
     a.own_run = PREFIX_OWN_RUN * team;
     a.part = c->prefix_part;
     a.pv = pages;

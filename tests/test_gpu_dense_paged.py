@@ -266,6 +266,14 @@ def test_large_logits(hata):
         w.check()
 
 
+@pytest.mark.parametrize("B,Hkv", [(8, 2), (40, 8), (70, 16), (300, 8)])
+def test_one_sequence_much_longer_than_the_others(hata, B, Hkv):
+    for place in (0, B // 2, B - 1):
+        lens = [1040 + i % 50 for i in range(B)]
+        lens[place] = 20000
+        World(lens, [(B, 1024)], Hq=2 * Hkv, Hkv=Hkv, P=16, seed=place).check()
+
+
 @pytest.mark.parametrize("scale", [-SCALE, 0.0, 1e-30, 2.0])
 def test_scales(hata, scale):
     w = World([2100 + i for i in range(20)], [(20, 2048)], Hq=8, Hkv=2, P=16, seed=5, outliers=False)
