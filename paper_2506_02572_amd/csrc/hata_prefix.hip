@@ -613,8 +613,14 @@ __global__ __launch_bounds__(256, 1) void prefix_kernel(const PrefixArgs a) {
     }
 }
 
-// Query rows of a workgroup (waves with rows of their own): from the mean of the groups, 64, 128 or 256
-static int prefix_waves(int64_t rows_per_group) { return rows_per_group <= 64 ? 1 : rows_per_group <= 128 ? 2 : 4; }
+// Query rows of a workgroup (waves with rows of their own), 64, 128 or 256, from the mean of the groups.  A smaller tile has more runs, a
+// larger one reads the rows less often.  us of a call with 64 / 128 / 256, one group behind 32768 rows, eight KV heads, groups of
+// four: 64 query rows 44.6 / 46.1 / 61.2, 96 51.6 / 46.8 / 61.0, 128 52.2 / 50.8 / 63.4, 192 64.0 / 65.6 / 68.0, 256 79.0 / 68.5 / 73.8,
+// 384 100.8 / 88.1 / 97.2, 512 127.4 / 108.9 / 102.8; behind 4096 rows 64 27.0 / 27.6 / 28.8, 128 27.8 / 32.4 / 32.7, 256
+// 32.3 / 34.1 / 39.5 (how long the shared rows are is not known on the host).
+#define PREFIX_ROWS_64 64
+#define PREFIX_ROWS_128 448
+static int prefix_waves(int64_t rows_per_group) { return rows_per_group <= PREFIX_ROWS_64 ? 1 : rows_per_group <= PREFIX_ROWS_128 ? 2 : 4; }
 
 // Workgroups of a launch: one per compute unit, or as many as the (tile of query rows, KV head) need
 static int64_t prefix_wgs(int B, int Hkv, int G, int n_groups, int waves) {
@@ -629,7 +635,8 @@ size_t prefix_part_floats(int B, int Hkv, int G) {
     size_t most = 0;
     for (int waves = 1; waves <= 4; waves *= 2) {
         // the most groups that go by so many waves
-        const int64_t groups = waves == 1 ? std::min(B, HATA_PREFIX_GROUPS) : std::min((int64_t)std::min(B, HATA_PREFIX_GROUPS), (int64_t)B * G / (32 * waves));
+        const int64_t above = waves == 1 ? 0 : waves == 2 ? PREFIX_ROWS_64 : PREFIX_ROWS_128;
+        const int64_t groups = std::min((int64_t)std::min(B, HATA_PREFIX_GROUPS), above ? ((int64_t)B * G - 1) / above : (int64_t)B);
         if (groups < 1) continue;
         most = std::max(most, (size_t)prefix_wgs(B, Hkv, G, (int)groups, waves) * 64 * waves * (HATA_D + 2));
     }
