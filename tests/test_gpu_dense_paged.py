@@ -374,6 +374,45 @@ def test_two_contexts_at_once(hata):
         assert bool((err <= 0).all())
 
 
+def test_lengths_out_of_range_and_a_group_of_one_sequence(hata):
+    """Lengths below zero count as zero, above the context's rows as those; one sequence alone may be called a group."""
+    import torch
+    w = World([640, 640, 0, 700], [(4, 640)], Hq=8, Hkv=2, P=16, seed=13, L_cap=640)
+    w.lens = [640, 640, 0, 640]
+    ref = w.exact()
+    w.run()
+    w.dev[1].copy_(torch.tensor([641, 2 ** 31 - 1, -7, 700], dtype=torch.int32))
+    w.check(ref=ref)
+    w.check(groups=False, ref=ref)
+    one = World([300], [(1, 288)], Hq=8, Hkv=2, P=16, seed=14)
+    one.check()
+    # (and without the fp32 output)
+    want = one.out.clone()
+    one.out.zero_()
+    t, lens, starts, shared = one.dev
+    one.ctx.hata_dense_decode_paged(one.q, one.K, one.V, t, one.width, one.P, one.n_pages, lens, 1, starts, shared, 1, SCALE, one.out)
+    torch.cuda.synchronize()
+    assert torch.equal(one.out, want)
+
+
+def test_pools_in_pinned_host_memory(hata):
+    import torch
+    w = World([700 + i for i in range(6)], [(6, 640)], Hq=8, Hkv=2, P=16, seed=15)
+    ref = w.exact()
+    slots = torch.arange(5, dtype=torch.int32, device="cuda") + 16 * int(w.table[0, 40])  # rows of a block that is a sequence's own
+    x = torch.randn((5, 2, 2, D), device="cuda").to(torch.bfloat16)
+    for name in ("K", "V"):
+        host = torch.empty(getattr(w, name).shape, dtype=torch.bfloat16, pin_memory=True)
+        host.copy_(getattr(w, name))
+        setattr(w, name, host)
+    w.check(ref=ref)
+    w.check(groups=False, ref=ref)
+    w.ctx.hata_write_slots(x[:, 0], x[:, 1], 4 * D, D, slots, 5, w.K, w.V, None, w.P, w.n_pages, None)
+    torch.cuda.synchronize()
+    page = int(w.table[0, 40])
+    assert torch.equal(w.K[page, :, :5].transpose(0, 1), x[:, 0].cpu()) and torch.equal(w.V[page, :, :5].transpose(0, 1), x[:, 1].cpu())
+
+
 def test_twice_the_same_and_captured(hata):
     import torch
     w = World([3000 + 7 * i for i in range(40)], [(20, 2992), (18, 1600)], Hq=8, Hkv=2, P=16, seed=12)

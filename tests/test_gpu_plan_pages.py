@@ -222,6 +222,53 @@ def test_captured_turns_follow_their_inputs(hata):
     ctx.close()
 
 
+def test_what_may_be_left_out_and_what_may_be_the_same(hata):
+    """No starts and positions; lengths returned where the wanted ones were; a context for more sequences and fewer rows than the
+    table has room for (1000 rows, no whole number of pages)."""
+    import torch
+    P, width, n_pages, spare = 16, CAP // 16, 300, 90
+    now, then = [17, 1000, 0, 40, 990, 3], [18, 1001, 300, 0, 1000, 20]
+    rng = np.random.default_rng(1)
+    table, stack, n_pages = world(rng, now, P, width, spare)
+    ref = served(now, then, [-1] * 6, [0] * 6, table, P, stack, spare, 500, 1000)
+    put = lambda a: torch.from_numpy(np.ascontiguousarray(a, dtype=np.int32)).cuda()
+    ctx = hata.Context(40, 1, 1, 128, 32, 1000, 64)
+    d = {"table": put(table), "free": put(stack), "seq": put(then), "n_free": put([spare])}
+    slots = put([JUNK] * 500)
+    ctx.hata_plan_pages(put(now), d["seq"], 6, None, None, d["table"], width, P, n_pages, d["free"], d["n_free"], d["n_free"],
+                        d["seq"], None, slots, None, 500)
+    torch.cuda.synchronize()
+    for name in d:
+        assert np.array_equal(d[name].cpu().numpy(), np.asarray(ref[name])), name
+    assert np.array_equal(slots.cpu().numpy(), ref["slots"]) and ref["seq"][1] == 1000
+    ctx.close()
+
+
+def test_numbers_that_make_no_sense_stay_in_bounds(hata):
+    """A free list longer than there are pages, pages that do not exist: clamped, every slot written names a row of the pools."""
+    import torch
+    P, B, n_pages = 16, 4, 20
+    put = lambda a: torch.from_numpy(np.ascontiguousarray(a, dtype=np.int32)).cuda()
+    ctx = hata.Context(B, 1, 1, 128, 32, CAP, 64)
+    for n_free in (-5, 0, 20, 1 << 30):
+        table, free = put(np.full((B, CAP // P), 2 ** 31 - 1)), put(np.full(n_pages, -9))
+        guard = free.clone()
+        n_out, seq, slots = put([0]), put([0] * B), put([0] * 200)
+        ctx.hata_plan_pages(put([40, 500, 0, 16]), put([60, 0, 100, 17]), B, None, None, table, CAP // P, P, n_pages, free,
+                            put([n_free]), n_out, seq, None, slots, None, 200)
+        torch.cuda.synchronize()
+        s = slots.cpu().numpy()
+        assert ((s >= -1) & (s < n_pages * P)).all() and 0 <= int(n_out[0]) <= n_pages
+        assert free.numel() == guard.numel()
+    ctx.close()
+
+
+def test_the_largest_batch(hata):
+    rng = np.random.default_rng(9)
+    now = [int(n) for n in rng.integers(0, 200, 8191)]
+    check(hata, now, [max(0, n + int(d)) for n, d in zip(now, rng.integers(-30, 9, 8191))], P=64, spare=500, repeat=1)
+
+
 def test_on_another_stream(hata):
     import torch
     check(hata, [3, 16, 0], [4, 17, 50], stream=torch.cuda.Stream())
