@@ -251,15 +251,16 @@ def test_numbers_that_make_no_sense_stay_in_bounds(hata):
     put = lambda a: torch.from_numpy(np.ascontiguousarray(a, dtype=np.int32)).cuda()
     ctx = hata.Context(B, 1, 1, 128, 32, CAP, 64)
     for n_free in (-5, 0, 20, 1 << 30):
-        table, free = put(np.full((B, CAP // P), 2 ** 31 - 1)), put(np.full(n_pages, -9))
-        guard = free.clone()
+        table, free = put(np.full((B, CAP // P), 2 ** 31 - 1)), put(np.full(n_pages + 500, -9))
+        guard = put(np.full(500, 777))
+        free[n_pages:] = guard  # (rows behind the list, which is n_pages long)
         n_out, seq, slots = put([0]), put([0] * B), put([0] * 200)
         ctx.hata_plan_pages(put([40, 500, 0, 16]), put([60, 0, 100, 17]), B, None, None, table, CAP // P, P, n_pages, free,
                             put([n_free]), n_out, seq, None, slots, None, 200)
         torch.cuda.synchronize()
         s = slots.cpu().numpy()
         assert ((s >= -1) & (s < n_pages * P)).all() and 0 <= int(n_out[0]) <= n_pages
-        assert free.numel() == guard.numel()
+        assert torch.equal(free[n_pages:], guard)
     ctx.close()
 
 
