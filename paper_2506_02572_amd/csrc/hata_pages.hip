@@ -294,7 +294,7 @@ __global__ __launch_bounds__(256) void write_few_kernel(const WriteSlots a) {
 // says nothing, because they are as large or as small as the numbers get, infinite or NaN, are evaluated in fp64 as a whole.
 //
 // Bound by the bytes it moves (512 read and 512 written a row), then by the products, which do not overlap with them on this
-// device: those 20711 rows 38.7 us, 4.5 TB/s, where a large copy reaches 4.8; 16384 rows of 32 heads, r = 256, 166 us, 3.4 TB/s.
+// device: those 20711 rows 38.4 us, 4.5 TB/s, where a large copy reaches 4.8; 16384 rows of 32 heads, r = 256, 150 us, 3.7 TB/s.
 // Rounds of resident workgroups (write_rows_per_wg): 45.4 us with twice as many of half the rows.
 #define WRITE_ERROR 0x1p-16f
 #define WRITE_MAX_ROWS 1024  // of a workgroup
@@ -408,7 +408,7 @@ __global__ __launch_bounds__(R <= 128 ? 256 : 512, 2) void write_mfma_kernel(con
                 *reinterpret_cast<uint4*>(a.V + (int64_t)to * HATA_D + lsub * 8) = vpre[it];
             }
             if (lsub == 0) {
-                // (a row of zeros projects to zero, in any arithmetic, and so does any row where the weights are zeros)
+                // (a row of zeros projects to zero, in any arithmetic that holds the weights, and so does a finite row where they are zeros)
                 const bool in_range = n2 < (F16 ? 0x1p31f : 0x1p120f) && (n2 >= 0x1p-80f || some == 0.f);
                 s_norm[row] = in_range ? sqrtf(n2) : __builtin_huge_valf();
                 s_row[t0 - first + row] = to;
@@ -451,7 +451,7 @@ __global__ __launch_bounds__(R <= 128 ? 256 : 512, 2) void write_mfma_kernel(con
             float least = fabsf(acc[t][0]);
 #pragma unroll
             for (int i = 1; i < 16; ++i) least = fminf(least, fabsf(acc[t][i]));
-            const bool zeros = xn == 0.f || wn == 0.f;
+            const bool zeros = (xn == 0.f && wn < __builtin_huge_valf()) || wn == 0.f;  // (weights out of range may be infinite in the planes)
             const bool live = s_row[t0 - first + row] >= 0;
             if (__builtin_amdgcn_ballot_w64(live && !zeros && !(least > near)) != 0ull) {
                 uint32_t todo = 0;

@@ -153,6 +153,19 @@ def test_weights_of_every_size(hata):
     check(hata, K, V, W.astype(np.float32), slots, n_pages, 16, prepared=True)
 
 
+@pytest.mark.parametrize("prepared", [False, True])
+@pytest.mark.parametrize("T", [6, 200])
+@pytest.mark.parametrize("r", [32, 64, 128, 256])
+def test_rows_of_zeros_with_weights_beyond_the_narrow_types(hata, T, r, prepared):
+    """Finite weights that bf16 or fp16 hold as infinite project a row of zeros to zero all the same (the bit is set); infinite ones do not."""
+    K, V, W, slots, n_pages = make(2, T, 2, r, 16)
+    K[::3] = 0
+    K[::6, :, 1::2] = 0x8000  # (-0)
+    W[0, 7, 3] = 3.4e38
+    W[1, 4, 5], W[1, 9, 6] = np.inf, -1e6
+    check(hata, K, V, W, slots, n_pages, 16, prepared=prepared)
+
+
 def test_one_row_for_all_and_another_stream(hata):
     import torch
     K, V, W, slots, n_pages = make(8, 40, 2, 128, 16)
