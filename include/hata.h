@@ -359,8 +359,8 @@ int hata_write_slots(hata_ctx* ctx, const void* K_new, const void* V_new, int64_
  * give zeros and do not count), sequences outside every group share nothing.  group_start is ascending; entries are
  * clamped to [the entry before, B].  0 <= n_groups <= B (groups behind the 1024th, and batches of more than 16384
  * sequences, share nothing).  Numerics are those of hata_dense_decode, but that the softmax weights of shared rows (in whole
- * 64s of them, two sequences or more) are rounded to bf16, in the weighted sum and in the sum they are divided by alike;
- * out_f32 is what that gives.  out 8-byte, out_f32 16-byte aligned.  One launch, with groups two; no residency needed, no
+ * 64s of them, two sequences or more) are rounded to bf16, in the weighted sum and in the sum they are divided by alike,
+ * and that weights below 2^-70 of the largest one, and values below 2^-70, may count as zero there; out_f32 is what that gives.  out 8-byte, out_f32 16-byte aligned.  One launch, with groups two; no residency needed, no
  * in-kernel waits; may be captured. */
 int hata_dense_decode_paged(hata_ctx* ctx, const void* q, const void* K_pool, const void* V_pool, const int32_t* block_table,
                             int32_t max_blocks, int32_t page_rows, int32_t n_pages, const int32_t* seq_len, int32_t B,
