@@ -613,8 +613,8 @@ __global__ __launch_bounds__(256, 1) void prefix_kernel(const PrefixArgs a) {
     }
 }
 
-// Query rows of a workgroup (waves with rows of their own), 64, 128 or 256, from the mean of the groups.  A smaller tile has more runs, a
-// larger one reads the rows less often.  us of a call with 64 / 128 / 256, one group behind 32768 rows, eight KV heads, groups of
+// Query rows of a workgroup (waves with rows of their own), 64, 128 or 256, from the mean of the groups.  A tile larger than
+// the group leaves waves without query rows, where a smaller one's go over different rows; a larger one reads the rows less often.  us of a call with 64 / 128 / 256, one group behind 32768 rows, eight KV heads, groups of
 // four: 64 query rows 44.6 / 46.1 / 61.2, 96 51.6 / 46.8 / 61.0, 128 52.2 / 50.8 / 63.4, 192 64.0 / 65.6 / 68.0, 256 79.0 / 68.5 / 73.8,
 // 384 100.8 / 88.1 / 97.2, 512 127.4 / 108.9 / 102.8; behind 4096 rows 64 27.0 / 27.6 / 28.8, 128 27.8 / 32.4 / 32.7, 256
 // 32.3 / 34.1 / 39.5 (how long the shared rows are is not known on the host).
