@@ -354,13 +354,14 @@ int hata_write_slots(hata_ctx* ctx, const void* K_new, const void* V_new, int64_
  * document, samples of one prompt): those are read once for all of them.
  *   group_start [n_groups + 1], shared_len [n_groups] (device; may be NULL with n_groups = 0): the sequences group_start[g] ..
  *   group_start[g + 1] - 1 have the same pages in their block tables over rows 0 .. shared_len[g] - 1.
- * Every sequence attends over its rows 0 .. seq_len[b] - 1 as in hata_dense_decode, the groups decide only how often
+ * Every sequence attends over its rows 0 .. seq_len[b] - 1 as in hata_dense_decode, the groups decide how often
  * rows are read: shared_len is clamped to the shortest sequence of the group that has rows at all (sequences without rows
  * give zeros and do not count), sequences outside every group share nothing.  group_start is ascending; entries are
  * clamped to [the entry before, B].  0 <= n_groups <= B (groups behind the 1024th, and batches of more than 16384
- * sequences, share nothing).  Numerics are those of hata_dense_decode, but that the softmax weights of shared rows (in whole
- * 64s of them, two sequences or more) are rounded to bf16, in the weighted sum and in the sum they are divided by alike,
- * and that weights below 2^-70 of the largest one, and values below 2^-70, may count as zero there; out_f32 is what that gives.  out 8-byte, out_f32 16-byte aligned.  One launch, with groups two; no residency needed, no
+ * sequences, share nothing).  Numerics are those of hata_dense_decode, whose softmax weights are two bf16 terms (16 bits)
+ * or, with 1, 2, 3, 6, 7, 9, 11, 13 or 14 query heads to a KV head, fp32.  The weights of shared rows (whole 64s of them, two sequences
+ * or more) are two bf16 terms for any number of heads, with the same effect where a value is infinite (the output may be NaN), and
+ * weights below 2^-70 of the largest one, and values below 2^-70, may count as zero there.  out 8-byte, out_f32 16-byte aligned.  One launch, with groups two; no residency needed, no
  * in-kernel waits; may be captured. */
 int hata_dense_decode_paged(hata_ctx* ctx, const void* q, const void* K_pool, const void* V_pool, const int32_t* block_table,
                             int32_t max_blocks, int32_t page_rows, int32_t n_pages, const int32_t* seq_len, int32_t B,

@@ -8,11 +8,14 @@
 //     192 registers) and goes over 32 rows at a time on v_mfma_f32_32x32x16_bf16: S^T = K Q^T, O^T += V^T P^T.  In S^T a lane has 16
 //     rows of ONE query row, which are what the second product wants from it as P: nothing crosses lanes.
 //   - WQ waves share what they read (rows come into LDS by direct loads, 64 of K and of V a stage), 4 / WQ go over different rows.
-//   - The maximum is followed loosely: scaling a wave's sums takes 1500 cycles, as much as the products of 32 rows, so the reference
-//     m_i is set PREFIX_LOOSE (binary) orders above the highest score when one passes it.  Weights are at most 1 all the same, and as
-//     floating-point numbers keep their precision; what is lost are weights 2^-70 of the largest, and values below 2^-70.
-//   - Weights are rounded to bf16 (to nearest: half a step, 2^-8 relative; their sum is of the rounded ones), which halves the second
-//     product against two terms, and the matrix cores are what bounds groups of more than some 200 query rows a KV head.
+//   - The maximum is followed loosely: scaling a wave's sums takes 1500 cycles, as much as two thirds of the products of 32 rows, so the
+//     reference m_i is set PREFIX_LOOSE (binary) orders above the highest score when one passes it.  Weights are at most 1 all the same,
+//     and as floating-point numbers keep their precision; what is lost are weights 2^-70 of the largest, and values below 2^-70.
+//     (32 sequences behind 32768 rows, 256 heavy ones behind 16384, us with 32, 40 and 56 orders: 77.9 / 74.0 / 70.8, 282 / 277 / 274)
+//   - A weight is two bf16 terms, the upper half of its bits and the rest to nearest (2^-16 relative together; their sum is of the terms),
+//     as in dense_kernel with four heads and more: the fp32 output is as exact as without groups (2-norm 9e-7 of 2112 rows either way).
+//     One term, 2^-8, is a third less to multiply, but made the fp32 output as coarse as the bf16 one: 32 sequences behind 32768 rows, 72
+//     in three groups, 12 behind 131072 and 256 behind 16384 took 61.2, 165, 108 and 219 us with it, 66.4, 177, 111 and 272 with two.  The matrix cores bound groups of more than some 140 query rows a KV head.
 #include <algorithm>
 #include "hata_attn_core.h"
 #include "hata_device.h"
@@ -238,6 +241,17 @@ __device__ __forceinline__ float max3(float a, float b, float c) {
     return r;
 }
 
+// Two weights as two bf16 terms each, of one sign: the upper half, and what is left of it rounded to nearest
+__device__ __forceinline__ uint32_t prefix_high(float x, float y) {
+    return __builtin_amdgcn_perm(__float_as_uint(y), __float_as_uint(x), 0x07060302u);
+}
+__device__ __forceinline__ uint32_t prefix_low(float x, float y) {
+    f32x2_t e;
+    e[0] = x - __uint_as_float(__float_as_uint(x) & 0xffff0000u);
+    e[1] = y - __uint_as_float(__float_as_uint(y) & 0xffff0000u);
+    return __builtin_bit_cast(uint32_t, __builtin_convertvector(e, bf16x2_t));
+}
+
 template <int N>
 __device__ __forceinline__ void prefix_wait() { asm volatile("s_waitcnt vmcnt(%0)" ::"n"(N) : "memory"); }
 
@@ -380,19 +394,19 @@ __global__ __launch_bounds__(256, 1) void prefix_kernel(const PrefixArgs a) {
             pin();
         }
     };
-    auto weights = [&](const f32x16_t (&sc)[2], uint32_t (&p)[2][8]) {
+    // (p: the terms of two rows' weights, [high or low][query row][two rows])
+    auto weights = [&](const f32x16_t (&sc)[2], uint32_t (&p)[2][2][8]) {
 #pragma unroll
         for (int t = 0; t < 2; ++t)
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
-                f32x2_t e;
-                e[0] = fast_exp2(fmaf(sc[t][2 * i], scale, -sub[t]));
-                e[1] = fast_exp2(fmaf(sc[t][2 * i + 1], scale, -sub[t]));
-                p[t][i] = __builtin_bit_cast(uint32_t, __builtin_convertvector(e, bf16x2_t));
-                l[t] = dot2_bf16(p[t][i], 0x3f803f80u, l[t]);
+                const float x = fast_exp2(fmaf(sc[t][2 * i], scale, -sub[t])), y = fast_exp2(fmaf(sc[t][2 * i + 1], scale, -sub[t]));
+                p[0][t][i] = prefix_high(x, y);
+                p[1][t][i] = prefix_low(x, y);
+                l[t] = dot2_bf16(p[1][t][i], 0x3f803f80u, dot2_bf16(p[0][t][i], 0x3f803f80u, l[t]));
             }
     };
-    auto values = [&](const char* vt, const uint32_t (&p)[2][8]) {
+    auto values = [&](const char* vt, const uint32_t (&p)[2][2][8]) {
 #pragma unroll
         for (int x = 0; x < 2; ++x)
 #pragma unroll
@@ -407,9 +421,11 @@ __global__ __launch_bounds__(256, 1) void prefix_kernel(const PrefixArgs a) {
                 }
                 const bf16x8_t vf = __builtin_bit_cast(bf16x8_t, make_uint4(v[0].x, v[0].y, v[1].x, v[1].y));
 #pragma unroll
-                for (int t = 0; t < 2; ++t)
-                    acc[t][c] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(
-                        vf, __builtin_bit_cast(bf16x8_t, make_uint4(p[t][4 * x], p[t][4 * x + 1], p[t][4 * x + 2], p[t][4 * x + 3])), acc[t][c], 0, 0, 0);
+                for (int k = 0; k < 2; ++k)
+#pragma unroll
+                    for (int t = 0; t < 2; ++t)
+                        acc[t][c] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(
+                            vf, __builtin_bit_cast(bf16x8_t, make_uint4(p[k][t][4 * x], p[k][t][4 * x + 1], p[k][t][4 * x + 2], p[k][t][4 * x + 3])), acc[t][c], 0, 0, 0);
             }
     };
     auto at_stage = [&](int s) { return (const char*)smem + (s % NBUF) * STAGE * 512 + wk * PART * 256; };  // K; V is STAGE * 256 bytes behind
@@ -432,7 +448,7 @@ __global__ __launch_bounds__(256, 1) void prefix_kernel(const PrefixArgs a) {
             else prefix_wait<0>();
             if (k0 + s * STAGE + wk * PART < k1) {
                 f32x16_t sc[2];
-                uint32_t p[2][8];
+                uint32_t p[2][2][8];
                 float top[2];
                 products(at_stage(s), sc);
                 highest(sc, top);
@@ -457,7 +473,7 @@ __global__ __launch_bounds__(256, 1) void prefix_kernel(const PrefixArgs a) {
         for (int s = 0; s < stages; ++s) {
 #pragma unroll
             for (int i = 0; i < SUBS; ++i) {
-                uint32_t p[2][8];
+                uint32_t p[2][2][4];  // [turn and turn][query row][two rows]
                 follow(top);
                 // stage s + 1 is there once only the one behind it is outstanding; everybody is done with stage s - 1, whose place
                 // the requests of this turn fill
@@ -484,15 +500,20 @@ __global__ __launch_bounds__(256, 1) void prefix_kernel(const PrefixArgs a) {
                 for (int t = 0; t < 2; ++t)
 #pragma unroll
                     for (int j = 0; j < 16; ++j) next[t][j] = 0.f;
-                f32x2_t e[3];  // two weights on their way: arguments, then exponentials
+                // (arguments, then weights, in the scores' place)
                 auto argument = [&](int j) {
-                    e[j % 3][0] = fmaf(sc[j / 8][2 * (j % 8)], scale, -sub[j / 8]);
-                    e[j % 3][1] = fmaf(sc[j / 8][2 * (j % 8) + 1], scale, -sub[j / 8]);
+                    sc[j / 8][2 * (j % 8)] = fmaf(sc[j / 8][2 * (j % 8)], scale, -sub[j / 8]);
+                    sc[j / 8][2 * (j % 8) + 1] = fmaf(sc[j / 8][2 * (j % 8) + 1], scale, -sub[j / 8]);
                 };
-                auto power = [&](int j) { e[j % 3][0] = fast_exp2(e[j % 3][0]); e[j % 3][1] = fast_exp2(e[j % 3][1]); };
-                auto round = [&](int j) {
-                    p[j / 8][j % 8] = __builtin_bit_cast(uint32_t, __builtin_convertvector(e[j % 3], bf16x2_t));
-                    l[j / 8] = dot2_bf16(p[j / 8][j % 8], 0x3f803f80u, l[j / 8]);
+                auto power = [&](int j) {
+                    sc[j / 8][2 * (j % 8)] = fast_exp2(sc[j / 8][2 * (j % 8)]);
+                    sc[j / 8][2 * (j % 8) + 1] = fast_exp2(sc[j / 8][2 * (j % 8) + 1]);
+                };
+                // group g of the second product: term g % 2 of the weights of rows 16 (g / 2) ..; two rows' of query row t
+                auto term = [&](int g, int t, int i) {
+                    const float x = sc[t][8 * (g / 2) + 2 * i], y = sc[t][8 * (g / 2) + 2 * i + 1];
+                    p[g % 2][t][i] = g % 2 ? prefix_low(x, y) : prefix_high(x, y);
+                    l[t] = dot2_bf16(p[g % 2][t][i], 0x3f803f80u, l[t]);
                 };
                 argument(0);
                 power(0);
@@ -504,15 +525,15 @@ __global__ __launch_bounds__(256, 1) void prefix_kernel(const PrefixArgs a) {
                     if (j % 2 == 1 && j / 2 + 3 < 8) kf[j / 2 % 3] = k_piece(j / 2 + 3);
                     if (j + 1 < 16) power(j + 1);
                     if (j + 2 < 16) argument(j + 2);
-                    round(j);
+                    if (j % 8 < 4) term(0, j / 8, j % 8);
                     if (turn && j % 2 == 0) fetch(dst + (j / 4) * 1024 + (j / 2 % 2) * STAGE * 256, off[j / 4], j / 2 % 2 ? v_from : k_from);
                     __builtin_amdgcn_sched_barrier(0);
                 }
-                auto v_piece_at = [&](int j) {  // channels 32 (j % 4) of rows 16 (j / 4) ..
+                auto v_piece_at = [&](int j) {  // channels 32 (j % 4) of rows 16 (j / 8) ..
                     uint2 v[2];
 #pragma unroll
                     for (int y = 0; y < 2; ++y) {
-                        const int r = 16 * (j / 4) + 8 * y + v_row;
+                        const int r = 16 * (j / 8) + 8 * y + v_row;
                         v[y] = __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4_t*)const_cast<char*>(
                             vt + r * 256 + (((4 * (j % 4) + v_piece) ^ prefix_swizzle(r)) << 4) + (lane & 1) * 8)));
                     }
@@ -521,21 +542,22 @@ __global__ __launch_bounds__(256, 1) void prefix_kernel(const PrefixArgs a) {
                 bf16x8_t vf[3] = {v_piece_at(0), v_piece_at(1), v_piece_at(2)};
                 __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-                for (int j = 0; j < 16; ++j) {
-                    const int t = j % 2, x = j / 8, c = j / 2 % 4;
+                for (int j = 0; j < 32; ++j) {
+                    const int g = j / 8, t = j % 2, c = j / 2 % 4, i = j / 2 % 4;
+                    const auto& w = p[g % 2][t];
                     acc[t][c] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(
-                        vf[j / 2 % 3], __builtin_bit_cast(bf16x8_t, make_uint4(p[t][4 * x], p[t][4 * x + 1], p[t][4 * x + 2], p[t][4 * x + 3])), acc[t][c], 0, 0, 0);
-                    if (j % 2 == 1 && j / 2 + 3 < 8) vf[j / 2 % 3] = v_piece_at(j / 2 + 3);
-                    if (j == 1) {
-                        asm volatile("" : "+v"(next[0]));
-                        top[0] = fmaxf(next[0][0], next[0][1]);
+                        vf[j / 2 % 3], __builtin_bit_cast(bf16x8_t, make_uint4(w[0], w[1], w[2], w[3])), acc[t][c], 0, 0, 0);
+                    if (j % 2 == 1 && j / 2 + 3 < 16) vf[j / 2 % 3] = v_piece_at(j / 2 + 3);
+                    if (g < 3) term(g + 1, t, i);
+                    if (g % 2) {  // (the groups with less to do beside them)
+                        const int k = g / 2;
+                        if (j % 8 == 0) {
+                            asm volatile("" : "+v"(next[k]));
+                            top[k] = fmaxf(next[k][0], next[k][1]);
+                        } else {
+                            top[k] = max3(top[k], next[k][2 * (j % 8)], next[k][2 * (j % 8) + 1]);
+                        }
                     }
-                    if (j == 8) {
-                        asm volatile("" : "+v"(next[1]));
-                        top[1] = fmaxf(next[1][0], next[1][1]);
-                    }
-                    if (j >= 1 && j < 8) top[0] = max3(top[0], next[0][2 * j], next[0][2 * j + 1]);
-                    if (j >= 9) top[1] = max3(top[1], next[1][2 * (j - 8)], next[1][2 * (j - 8) + 1]);
                     __builtin_amdgcn_sched_barrier(0);
                 }
                 top[0] *= scale;
@@ -614,10 +636,11 @@ __global__ __launch_bounds__(256, 1) void prefix_kernel(const PrefixArgs a) {
 }
 
 // Query rows of a workgroup (waves with rows of their own), 64, 128 or 256, from the mean of the groups.  A tile larger than
-// the group leaves waves without query rows, where a smaller one's go over different rows; a larger one reads the rows less often.  us of a call with 64 / 128 / 256, one group behind 32768 rows, eight KV heads, groups of
-// four: 64 query rows 44.6 / 46.1 / 61.2, 96 51.6 / 46.8 / 61.0, 128 52.2 / 50.8 / 63.4, 192 64.0 / 65.6 / 68.0, 256 79.0 / 68.5 / 73.8,
-// 384 100.8 / 88.1 / 97.2, 512 127.4 / 108.9 / 102.8; behind 4096 rows 64 27.0 / 27.6 / 28.8, 128 27.8 / 32.4 / 32.7, 256
-// 32.3 / 34.1 / 39.5 (how long the shared rows are is not known on the host).
+// the group leaves waves without query rows, where a smaller one's go over different rows; a larger one reads the rows less often.
+// us of a call with 64 / 128 / 256, one group behind 32768 rows and up to 200 of their own, eight KV heads, groups of four: 64 query rows
+// 48.2 / 55.9 / 77.0, 96 59.4 / 57.0 / 75.5, 128 60.0 / 58.4 / 75.9, 192 77.3 / 81.1 / 82.8, 256 92.4 / 85.3 / 88.0, 384 127 / 114 / 126,
+// 448 149 / 135 / 131, 512 155 / 138 / 134; behind 4096 rows 64 30.1 / 30.9 / 33.2, 128 31.1 / 34.9 / 36.1, 256 38.3 / 39.8 / 45.0, 512
+// 55.2 / 51.5 / 54.6 (how long the shared rows are is not known on the host).
 #define PREFIX_ROWS_64 64
 #define PREFIX_ROWS_128 448
 static int prefix_waves(int64_t rows_per_group) { return rows_per_group <= PREFIX_ROWS_64 ? 1 : rows_per_group <= PREFIX_ROWS_128 ? 2 : 4; }
