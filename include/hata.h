@@ -343,8 +343,9 @@ int hata_plan_pages(hata_ctx* ctx, const int32_t* len_now, const int32_t* len_ne
  * same strides for both, e.g. those of the columns of a fused projection's output; multiples of 8, not negative), its d
  * values contiguous.  Rows whose slot is negative or not in the pools go nowhere; rows of the pools that no slot names are
  * left as they are.  No two rows may have the same slot.  codes_pool and W_H both NULL: no codes (the cache of a dense
- * layer; a row that hata_decode_step_paged appends).  Any r.  The codes are those of an evaluation in fp64, whatever the
- * number of rows: equal to what hata_decode_step appends.  (hata_prepare_weights of the same W_H makes calls with many rows
+ * layer; a row that hata_decode_step_paged appends).  Any r.  A bit is the sign of a sum in fp64 (NaN: 0), of products that are
+ * exact there, added up in one order whatever the number of rows: a key has one code.  It is that of the exact projection, and so what
+ * hata_decode_step appends, unless the projection is below 2^-46 of the sum of its products' sizes.  (hata_prepare_weights of the same W_H makes calls with many rows
  * faster.)  n_tokens is not bounded by L_cap or B_max. */
 int hata_write_slots(hata_ctx* ctx, const void* K_new, const void* V_new, int64_t stride_t, int64_t stride_h, const int32_t* slots,
                      int32_t n_tokens, void* K_pool, void* V_pool, uint32_t* codes_pool, int32_t page_rows, int32_t n_pages,

@@ -285,16 +285,17 @@ __global__ __launch_bounds__(256) void write_few_kernel(const WriteSlots a) {
 // Many rows: the projection on the matrix cores, as in encode_mfma_kernel (M = 32 hash columns of a wave, N = 32 rows; prepared
 // fp16 planes, or three bf16 planes split here), and the values next to zero once more in fp64.
 //
-// A sum of the matrix cores is within WRITE_ERROR |x| |w| of the exact one (Euclidean norms; at most 24 instructions, each off by a few units
-// in the last place of a partial sum, which |x| |w| bounds).  A sum that is not above that (one value in some 7000 of normally
-// distributed ones) is in doubt: it goes on a list, and once the workgroup is through its rows, sixteen lanes evaluate each of
-// them in fp64, where the products are exact.  (Evaluated where they were found, by a wave each, they cost a latency a stage.
-// 20711 rows, eight heads, r = 128, us: 46.0 that way, 38.7 with the list, 37.4 with none in doubt.)
+// A sum of the matrix cores is within half of WRITE_ERROR |x| |w| of the exact one (Euclidean norms; at most 24 instructions, each off by a
+// few units in the last place of a partial sum, which |x| |w| bounds).  A sum that is not above the whole (one value in some 7000 of
+// normally distributed ones) is in doubt: it goes on a list, and once the workgroup is through its rows, each of them is evaluated as
+// fewer rows are (hash_pass): in fp64, where the products are exact, with the same roundings of the sums.  So a key's code does not
+// depend on the number of rows, not even where its products cancel further than fp64 reaches.  (Evaluated where they were found, by a wave each, they cost a latency a stage.
+// 20711 rows, eight heads, r = 128, us: 46.0 that way, 38.2 with the list by sixteen lanes of the vector ALU an item, 37.2 as here.)
 // fp16 planes: x loses up to 2^-24 below 2^-14 and saturates at 65504, the weights 2^-22 of their size or 2^-25; rows of which that
 // says nothing, because they are as large or as small as the numbers get, infinite or NaN, are evaluated in fp64 as a whole.
 //
 // Bound by the bytes it moves (512 read and 512 written a row), then by the products, which do not overlap with them on this
-// device: those 20711 rows 38.4 us, 4.5 TB/s, where a large copy reaches 4.8; 16384 rows of 32 heads, r = 256, 150 us, 3.7 TB/s.
+// device: those 20711 rows 37.2 us, 4.65 TB/s, where a large copy reaches 4.8; 16384 rows of 32 heads, r = 256, 143 us, 3.9 TB/s.
 // Rounds of resident workgroups (write_rows_per_wg): 45.4 us with twice as many of half the rows.
 #define WRITE_ERROR 0x1p-16f
 #define WRITE_MAX_ROWS 1024  // of a workgroup
@@ -375,22 +376,6 @@ __global__ __launch_bounds__(R <= 128 ? 256 : 512, 2) void write_mfma_kernel(con
     norm2 = wave_max64(norm2);
     const bool no_w = !doubt && __builtin_amdgcn_ballot_w64(some_w != 0.f) == 0ull;
     const float wn = no_w ? 0.f : doubt || norm2 < 0x1p-80f ? __builtin_huge_valf() : sqrtf(norm2);
-
-    // row t of the workgroup, hash column col, by the lanes of a row of sixteen; every one of them gets the answer
-    auto exact_bit = [&](int t, int col) {
-        const uint4 x = *reinterpret_cast<const uint4*>(Kh + (first + t) * a.st + lsub * 8);
-        const float* wc = a.W_H + ((int64_t)h * HATA_D + lsub * 8) * R + col;
-        float wv[8];
-#pragma unroll
-        for (int e = 0; e < 8; ++e) wv[e] = wc[e * R];
-        const uint32_t xv[4] = {x.x, x.y, x.z, x.w};
-        double s = 0.0;
-#pragma unroll
-        for (int e = 0; e < 4; ++e) s = fma((double)bf16_hi(xv[e]), (double)wv[2 * e + 1], fma((double)bf16_lo(xv[e]), (double)wv[2 * e], s));
-#pragma unroll
-        for (int o = 8; o >= 1; o >>= 1) s += __shfl_xor(s, o, 16);
-        return s >= 0.0;
-    };
 
     for (int t0 = first; t0 < last; t0 += STAGE) {
         __syncthreads();  // the previous stage has been consumed
@@ -476,20 +461,37 @@ __global__ __launch_bounds__(R <= 128 ? 256 : 512, 2) void write_mfma_kernel(con
         }
     }
     __syncthreads();
-    auto settle = [&](uint32_t item, bool own) {
-        const bool one = exact_bit((int)(item / R), (int)(item % R));
-        if (own && lsub == 0) {
-            uint32_t* word = &s_code[item / 32];
-            if (one) atomicOr(word, 1u << (item % 32));
-            else atomicAnd(word, ~(1u << (item % 32)));
+    // Bits in doubt, sixteen a wave: hash_pass' instruction and its order of the channels, so that the sums round as they do there.  Its
+    // four blocks take four columns and four vectors each, of which the diagonal is looked at: lane l has a part of item l % 16, and
+    // the lanes with l / 16 = l % 4 get the sum of theirs.
+    auto settle = [&](int n, auto item_of) {  // item: row of the workgroup * R + column
+        for (int i0 = 16 * wave; i0 < n; i0 += THREADS / 4) {
+            const uint32_t item = item_of(min(i0 + (lane & 15), n - 1));
+            uint4 x[4];
+            hash_load_x(Kh + (first + (int)(item / R)) * a.st, x);
+            const float* wc = a.W_H + ((int64_t)h * HATA_D + 32 * (lane >> 4)) * R + item % R;
+            float wv[32];
+#pragma unroll
+            for (int s = 0; s < 32; ++s) wv[s] = wc[s * R];
+            double acc = 0.0;
+#pragma unroll
+            for (int s = 0; s < 32; ++s) {
+                const uint32_t pair = (&x[s / 8].x)[s / 2 % 4];
+                acc = __builtin_amdgcn_mfma_f64_4x4x4f64((double)wv[s], (double)(s % 2 ? bf16_hi(pair) : bf16_lo(pair)), acc, 0, 0, 0);
+            }
+            if (lane >> 4 == (lane & 3) && i0 + (lane & 15) < n) {
+                uint32_t* word = &s_code[item / 32];
+                if (acc >= 0.0) atomicOr(word, 1u << (item % 32));
+                else atomicAnd(word, ~(1u << (item % 32)));
+            }
         }
     };
-    const int doubts = min(s_doubts, WRITE_DOUBTS);
-    for (int i = tid / 16; i < (doubts + THREADS / 16 - 1) / (THREADS / 16) * (THREADS / 16); i += THREADS / 16)
-        settle(s_doubt[min(i, doubts - 1)], i < doubts);
+    settle(min(s_doubts, WRITE_DOUBTS), [&](int i) { return s_doubt[i]; });
     for (int k = 0; k < (s_wholes ? WRITE_MAX_ROWS / 32 : 0); ++k)
-        for (uint32_t rows = s_whole[k]; rows; rows &= rows - 1)
-            for (int c = tid / 16; c < R; c += THREADS / 16) settle((uint32_t)(32 * k + __ffs(rows) - 1) * R + c, true);
+        for (uint32_t rows = s_whole[k]; rows; rows &= rows - 1) {
+            const uint32_t row = 32 * k + __ffs(rows) - 1;
+            settle(R, [&](int i) { return row * R + i; });
+        }
     __syncthreads();
     // the code words, 16 bytes a thread where a code is as long
     if constexpr (WD >= 4) {
