@@ -645,10 +645,10 @@ __global__ __launch_bounds__(256, 1) void prefix_kernel(const PrefixArgs a) {
 #define PREFIX_ROWS_128 448
 static int prefix_waves(int64_t rows_per_group) { return rows_per_group <= PREFIX_ROWS_64 ? 1 : rows_per_group <= PREFIX_ROWS_128 ? 2 : 4; }
 
-// Workgroups of a launch: one per compute unit, or as many as the (tile of query rows, KV head) need
+// Workgroups of a launch: one per compute unit, or as many as the (tile of query rows, KV head) of groups with two members and more need
 static int64_t prefix_wgs(int B, int Hkv, int G, int n_groups, int waves) {
     const int mpt = 64 * waves / G;
-    const int64_t tiles = (B + (int64_t)n_groups * (mpt - 1)) / mpt * Hkv;
+    const int64_t tiles = (B + (int64_t)std::min(n_groups, B / 2) * (mpt - 1)) / mpt * Hkv;
     return std::max((int64_t)256, (tiles + 255) / 256 * 256);
 }
 
