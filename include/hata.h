@@ -320,7 +320,7 @@ int hata_prefill_write_paged(hata_ctx* ctx, const void* K_new, const void* V_new
  *                           written: pages released in this call are put behind them, in the order of sequences and blocks, and
  *                           taken in the same call already
  *   n_free, n_free_out [1]  their number before and after the call (may be the same address)
- *   seq_len     [B]         output: len_next[b] where the request was granted, else len_now[b] (0 for a fork); may be
+ *   seq_len     [B]         output: len_next[b] where the request was granted, else len_now[b] in the range below (0 for a fork); may be
  *                           len_now or len_next
  *   token_start [B + 1] or NULL  output: the packed rows of sequence b are token_start[b] .. token_start[b + 1] - 1, whether
  *                           granted or not; values above max_tokens are given as max_tokens
@@ -346,13 +346,15 @@ int hata_plan_pages(hata_ctx* ctx, const int32_t* len_now, const int32_t* len_ne
  * layer; a row that hata_decode_step_paged appends).  Any r.  A bit is the sign of a sum in fp64 (NaN: 0), of products that are
  * exact there, added up in one order whatever the number of rows: a key has one code.  It is that of the exact projection, and so what
  * hata_decode_step appends, unless the projection is below 2^-46 of the sum of its products' sizes.  (hata_prepare_weights of the same W_H makes calls with many rows
- * faster.)  n_tokens is not bounded by L_cap or B_max. */
+ * faster; r other than 32, 64, 128 and 256 makes them several times slower.)  n_tokens is not bounded by L_cap or B_max. */
 int hata_write_slots(hata_ctx* ctx, const void* K_new, const void* V_new, int64_t stride_t, int64_t stride_h, const int32_t* slots,
                      int32_t n_tokens, void* K_pool, void* V_pool, uint32_t* codes_pool, int32_t page_rows, int32_t n_pages,
                      const float* W_H, void* stream);
 
 /* hata_dense_decode on the paged layout, where the first rows of some sequences are the same pages (a system prompt, a
- * document, samples of one prompt): those are read once for all of them.
+ * document, samples of one prompt): those are read once for all of them.  It pays to name a group from some 80000 rows on that are not
+ * read again (members less one times the rows they share; eight KV heads): 32 sequences behind 2048 rows, eight behind 12000, two behind
+ * 100000.  A call with groups is a second launch, 16 us at least and 19 with a whole 64 of shared rows, where a call without takes 8.
  *   group_start [n_groups + 1], shared_len [n_groups] (device; may be NULL with n_groups = 0): the sequences group_start[g] ..
  *   group_start[g + 1] - 1 have the same pages in their block tables over rows 0 .. shared_len[g] - 1.
  * Every sequence attends over its rows 0 .. seq_len[b] - 1 as in hata_dense_decode, the groups decide how often

@@ -236,8 +236,11 @@ hipError_t launch_plan_pages(const hata_ctx* c, const PagePlan& p, hipStream_t s
 // grid = (slices of COLS hash columns, Hkv, runs of WRITE_ROWS packed rows); the first slice copies the rows.  Codes in fp64
 // (hata_hash.h), four rows at a time.
 #define WRITE_ROWS 16
-// Rows up to which a call with codes goes this way: us, eight heads, r = 128, this way / by the matrix cores with prepared weights:
-// 64 rows 6.5 / 6.2, 128 6.8 / 7.2, 512 10.1 / 8.3, 1024 15.8 / 8.8; r = 256, 64 and 256 rows 6.3 / 6.7, 9.6 / 8.4
+// Rows up to which a call with codes goes this way: us, eight heads, r = 128, this way / by the matrix cores with prepared weights / without:
+// 64 rows 6.3 / 6.2 / 9.4, 128 6.3 / 6.4 / 9.5, 256 6.5 / 6.6 / 9.8, 512 9.2 / 6.9 / 9.9, 1024 14.7 / 7.6 / 10.4; r = 256, 64 6.2 / 7.0 / 12.0,
+// 128 6.5 / 7.3 / 12.4, 256 9.2 / 7.5 / 12.4, 512 14.8 / 8.6 / 13.0.  (One number for both: a server's weights are fixed, and prepared; without
+// that, 129 to some 400 rows take up to 4 us longer than they would this way.)  Widths other than 32, 64, 128 and 256 go this way at any
+// number of rows: no configuration here has one.  20711 rows, r = 96: 286 us.
 #define HATA_WRITE_FEW 128
 struct WriteSlots {
     const uint16_t *K_new, *V_new;
@@ -295,7 +298,8 @@ __global__ __launch_bounds__(256) void write_few_kernel(const WriteSlots a) {
 // says nothing, because they are as large or as small as the numbers get, infinite or NaN, are evaluated in fp64 as a whole.
 //
 // Bound by the bytes it moves (512 read and 512 written a row), then by the products, which do not overlap with them on this
-// device: those 20711 rows 37.2 us, 4.65 TB/s, where a large copy reaches 4.8; 16384 rows of 32 heads, r = 256, 143 us, 3.9 TB/s.
+// device: those 20711 rows 37.2 us, 4.65 TB/s, where a large copy reaches 4.8; 16384 rows of 32 heads, r = 256, 144 us, 3.9 TB/s.  (Three planes, split
+// here by every workgroup, where the weights are not prepared: 42.9 and 168 us.)
 // Rounds of resident workgroups (write_rows_per_wg): 45.4 us with twice as many of half the rows.
 #define WRITE_ERROR 0x1p-16f
 #define WRITE_MAX_ROWS 1024  // of a workgroup

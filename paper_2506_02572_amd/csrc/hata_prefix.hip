@@ -15,7 +15,8 @@
 //   - A weight is two bf16 terms, the upper half of its bits and the rest to nearest (2^-16 relative together; their sum is of the terms),
 //     as in dense_kernel with four heads and more: the fp32 output is as exact as without groups (2-norm 9e-7 of 2112 rows either way).
 //     One term, 2^-8, is a third less to multiply, but made the fp32 output as coarse as the bf16 one: 32 sequences behind 32768 rows, 72
-//     in three groups, 12 behind 131072 and 256 behind 16384 took 61.2, 165, 108 and 219 us with it, 66.4, 177, 111 and 272 with two.  The matrix cores bound groups of more than some 140 query rows a KV head.
+//     in three groups, 12 behind 131072 and 256 behind 16384 took 65, 170, 109 and 224 us with it, on one card in turn 72, 183, 112 and
+//     280 with two.  The matrix cores bound groups of more than some 140 query rows a KV head.
 #include <algorithm>
 #include "hata_attn_core.h"
 #include "hata_device.h"
@@ -47,7 +48,7 @@ struct PrefixArgs {
 // which the launch's workgroups suffice, one per (group, KV head, tile of query rows, run).  The tiles of query rows of a run are
 // neighbours on one XCD, whose L2 then serves all but the first of them.  The last workgroup writes the plan that the launch behind
 // goes by.  (A workgroup more than there are compute units would have to wait for one.)  It has nothing else to do, unless the
-// others' runs would be longer for that by more than the plan takes (5 us; a tile of rows takes 0.6 us for 64 query rows).
+// others' runs would be longer for that by more than the plan takes (5 us; a tile of rows takes 0.8 us for 64 query rows).
 struct PrefixShare { int g, h, split, ns, qt, tiles, item, first, members, lead; };
 struct PrefixGroups { int *start, *least, *count, *lead; };  // in LDS: first member [n + 1]; tiles in common, members that have rows, the first of them [n]
 
@@ -127,7 +128,7 @@ __device__ __forceinline__ void prefix_items(const PrefixArgs& a, const PrefixGr
         if (items == (uint32_t)wgs && !with_last) with_last = run;  // (the workgroup with the plan would have an item too)
         if (items < (uint32_t)wgs || run >= (int)longest) break;
     }
-    if (with_last && (run - with_last) * mpt * a.G > 8 * 64) run = with_last;
+    if (with_last && (run - with_last) * mpt * a.G > 6 * 64) run = with_last;
     uint32_t base = 0;
     for (int g0 = 0; g0 < n; g0 += 64) {
         const int g = g0 + lane, qt = g0 ? qtiles(g) : qt0, ns = splits(g0 ? tiles(g) : tiles0, run);
@@ -640,7 +641,9 @@ __global__ __launch_bounds__(256, 1) void prefix_kernel(const PrefixArgs a) {
 // us of a call with 64 / 128 / 256, one group behind 32768 rows and up to 200 of their own, eight KV heads, groups of four: 64 query rows
 // 48.2 / 55.9 / 77.0, 96 59.4 / 57.0 / 75.5, 128 60.0 / 58.4 / 75.9, 192 77.3 / 81.1 / 82.8, 256 92.4 / 85.3 / 88.0, 384 127 / 114 / 126,
 // 448 149 / 135 / 131, 512 155 / 138 / 134; behind 4096 rows 64 30.1 / 30.9 / 33.2, 128 31.1 / 34.9 / 36.1, 256 38.3 / 39.8 / 45.0, 512
-// 55.2 / 51.5 / 54.6 (how long the shared rows are is not known on the host).
+// 55.2 / 51.5 / 54.6 (how long the shared rows are is not known on the host).  The mean is of all sequences, those in no group too, which
+// is what the host knows: with eight sequences behind 32768 rows and 150 alone, of 1024 rows each, it gives 256 to a group of 32 query rows,
+// 171 us (148 with 64, 208 without groups).
 #define PREFIX_ROWS_64 64
 #define PREFIX_ROWS_128 448
 static int prefix_waves(int64_t rows_per_group) { return rows_per_group <= PREFIX_ROWS_64 ? 1 : rows_per_group <= PREFIX_ROWS_128 ? 2 : 4; }
