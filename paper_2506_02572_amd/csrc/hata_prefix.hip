@@ -13,7 +13,8 @@
 //     and as floating-point numbers keep their precision; what is lost are weights 2^-70 of the largest, and values below 2^-70.
 //     (32 sequences behind 32768 rows, 256 heavy ones behind 16384, us with 32, 40 and 56 orders: 77.9 / 74.0 / 70.8, 282 / 277 / 274)
 //   - A weight is two bf16 terms, the upper half of its bits and the rest to nearest (2^-16 relative together; their sum is of the terms),
-//     as in dense_kernel with four heads and more: the fp32 output is as exact as without groups (2-norm 9e-7 of 2112 rows either way).
+//     as in dense_kernel with four heads and more: the fp32 output is as exact as without groups (2-norm of the error, 2112
+//     rows: 3.6e-6, and 6.7e-6 without, where the second term is cut off; 1.9e-7 with the fp32 weights that own rows of fewer heads have).
 //     One term, 2^-8, is a third less to multiply, but made the fp32 output as coarse as the bf16 one: 32 sequences behind 32768 rows, 72
 //     in three groups, 12 behind 131072 and 256 behind 16384 took 65, 170, 109 and 224 us with it, on one card in turn 72, 183, 112 and
 //     280 with two.  The matrix cores bound groups of more than some 140 query rows a KV head.
