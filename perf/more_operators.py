@@ -278,7 +278,7 @@ def prepare_tree(c, seed):
     for b in range(B):
         seen[start[b]:start[b + 1], :n[b]] = ancestors(rng, n[b])
     s = {"case": c, "P": P, "n_pages": n_pages, "base": base, "n": n, "lens": lens, "T": T, "words": words, "width": table.shape[1],
-         "table": ints(table), "seq": ints(lens), "start": ints(start),
+         "table": ints(table), "committed": ints(base), "seq": ints(lens), "start": ints(start),
          "mask": None if c["chain"] else ints(np.packbits(seen, axis=1, bitorder="little").view(np.int32)),
          "K": src.rows(n_pages, Hkv, P, D), "V": src.rows(n_pages, Hkv, P, D),
          "q": src.rows(T, Hkv, Hq // Hkv, D).reshape(T, Hq, D).contiguous(),
@@ -301,8 +301,8 @@ def prepare_keep(c, seed):
         k = int(rng.integers(0, c["path"] + 1))
         path[b, :k] = np.sort(rng.permutation(n[b])[:k])
         n_path.append(min(k, n[b]))
-    s = {"case": c, "P": P, "n_pages": n_pages, "width": table.shape[1], "table": ints(table), "seq": ints(lens),
-         "start": ints(np.concatenate([[0], np.cumsum(n)])), "path": ints(path), "n_path": ints(n_path), "seq_out": ints([0] * B),
+    s = {"case": c, "P": P, "n_pages": n_pages, "width": table.shape[1], "table": ints(table), "committed": ints(base), "seq": ints(lens),
+         "path": ints(path), "n_path": ints(n_path), "seq_out": ints([0] * B),
          "K": src.rows(n_pages, Hkv, P, D), "V": src.rows(n_pages, Hkv, P, D), "codes": None}
     if r:
         s["codes"] = torch.randint(-2 ** 31, 2 ** 31, (n_pages, Hkv, P, r // 32), device="cuda", generator=src.g).to(torch.int32)
@@ -330,11 +330,11 @@ def run_own(s):
                                     s["slots"], K.shape[0], s["rotary"], s["K"], s["V"], s["codes"], s["P"], s["n_pages"], s["W"])
         return append_outputs(s)
     if c["kind"] == "keep":
-        ctx.hata_keep_rows(s["K"], s["V"], s["codes"], s["table"], s["width"], s["P"], s["n_pages"], s["seq"], s["start"], c["B"],
+        ctx.hata_keep_rows(s["K"], s["V"], s["codes"], s["table"], s["width"], s["P"], s["n_pages"], s["committed"], s["seq"], c["B"],
                            s["path"], s["n_path"], c["path"], s["seq_out"])
         return keep_outputs(s)
-    ctx.hata_dense_tree_paged(s["q"], s["K"], s["V"], s["table"], s["width"], s["P"], s["n_pages"], s["seq"], c["B"], s["start"],
-                              s["T"], c["draft"], s["mask"], s["words"], SCALE, s["out"], None, s["scratch"])
+    ctx.hata_dense_tree_paged(s["q"], s["K"], s["V"], s["table"], s["width"], s["P"], s["n_pages"], s["committed"], s["seq"], c["B"],
+                              s["start"], s["T"], c["draft"], s["mask"], s["words"], SCALE, s["out"], None, s["scratch"])
     return s["out"]
 
 
@@ -433,8 +433,7 @@ def plain_tree(s):
 
 def plain_keep(s):
     c, P = s["case"], s["P"]
-    start = s["start"].long()
-    base = s["seq"].long() - (start[1:] - start[:-1])
+    base = s["committed"].long()
     i = torch.arange(c["path"], device=base.device)
     b, i = torch.nonzero(i[None, :] < s["n_path"][:, None], as_tuple=True)
     source, to = base[b] + s["path"].long()[b, i], base[b] + i
@@ -524,14 +523,14 @@ def exact_tree(s):
 def exact_keep(s):
     """Sequence by sequence, row by row."""
     c, P = s["case"], s["P"]
-    table, seq, start, path, n_path = [s[k].cpu().numpy() for k in ("table", "seq", "start", "path", "n_path")]
+    table, committed, path, n_path = [s[k].cpu().numpy() for k in ("table", "committed", "path", "n_path")]
     out = {"seq_len": np.zeros(c["B"], np.int64)}
     pools = {k: s[k].view(torch.int16).cpu().numpy() for k in ("K", "V")}
     if s["codes"] is not None:
         pools["codes"] = s["codes"].cpu().numpy()
     before = {k: v.copy() for k, v in pools.items()}
     for b in range(c["B"]):
-        base = int(seq[b]) - int(start[b + 1] - start[b])
+        base = int(committed[b])
         out["seq_len"][b] = base + int(n_path[b])
         for i in range(int(n_path[b])):
             a, z = base + int(path[b, i]), base + i
