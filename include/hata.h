@@ -371,6 +371,91 @@ int hata_dense_decode_paged(hata_ctx* ctx, const void* q, const void* K_pool, co
                             const int32_t* group_start, const int32_t* shared_len, int32_t n_groups, float sm_scale, void* out,
                             float* out_f32, void* stream);
 
+/*
+ * Drafted tokens on a paged cache, and rotary positions.  A turn of a server that drafts: hata_plan_pages (len_next = len_now + drafted
+ * tokens) -> hata_rotate_write_slots (drafted tokens' keys and values into their slots, rotated by the positions of their depth in the
+ * tree) -> hata_dense_tree_paged -> the model's choice of a path -> hata_keep_rows (its rows moved together) -> the next turn's
+ * hata_plan_pages, with the pages behind the path set back.  All of them only enqueue, and may be captured.
+ *
+ * Rotary positions.  Channels come in pairs (a, b), pair i turned by t = position * freq[i]:
+ *   y_a = m (x_a cos t - x_b sin t),  y_b = m (x_a sin t + x_b cos t)
+ * evaluated in fp64 (t is the fp64 product; m cos t and m sin t are rounded to fp64) and rounded to bf16 once, so that a row has the same
+ * bits whichever call rotates it, and how many with it.  Channels from dims on are copied.  Positions may be any int32.  (NaN and
+ * infinities go by the formula: an infinite x_a makes y_b NaN at t = 0.)
+ */
+typedef struct {
+    const double* freq;  /* [dims / 2] fp64, DEVICE: radians a position */
+    int32_t dims;        /* rotated channels of a head, the first ones: a multiple of 16, 16 .. d */
+    int32_t interleaved; /* pair i is channels i and i + dims / 2 (0), or 2 i and 2 i + 1 (1) */
+    float magnitude;     /* m; 1 unless the scaling asks for another */
+} hata_rotary;
+
+/* Frequencies of dims / 2 pairs, freq[i] = base^(-2 i / dims), scaled for contexts longer than the `original` one (HOST pointers;
+ * freq is then copied to the device once).  scaling NULL or kind HATA_ROTARY_NONE: as they are; *magnitude = 1 but for the last kind.
+ *   LINEAR  freq / factor
+ *   BASE    base * factor^(dims / (dims - 2)) in the place of base (dims > 2)
+ *   BANDS   by the turns that a pair makes over the original context, original * freq / (2 pi): from `high` turns on kept, up to `low`
+ *           divided by factor, in between a mean of both, weighted linearly by the turns
+ *   RAMP    the same by the pair's number, linearly between the pair that makes `high` turns (rounded down) and the one that makes `low`
+ *           (rounded up), found from freq[i] = base^(-2 i / dims); *magnitude = 0.1 ln(factor) + 1 for factor > 1
+ * HATA_EUNSUPPORTED for dims as above, HATA_EINVAL for a base not above 1, a factor or original not above 0, high not above low > 0. */
+typedef enum { HATA_ROTARY_NONE = 0, HATA_ROTARY_LINEAR = 1, HATA_ROTARY_BASE = 2, HATA_ROTARY_BANDS = 3, HATA_ROTARY_RAMP = 4 } hata_rotary_kind;
+typedef struct {
+    int32_t kind;               /* hata_rotary_kind */
+    double factor;
+    double low, high, original; /* BANDS and RAMP */
+} hata_rotary_scaling;
+int hata_rotary_frequencies(int32_t dims, double base, const hata_rotary_scaling* scaling, double* freq, float* magnitude);
+
+/* Packed rows rotated: n_heads heads of each of n_tokens rows, x and out with strides as in hata_write_slots.  back != 0: by -t, which
+ * is the gradient of the forward call (its transpose, m included).  out may be x with the same strides; otherwise they must not
+ * overlap.  Any number of tokens; the context's shape does not matter. */
+int hata_rotate(hata_ctx* ctx, const void* x, int64_t stride_t, int64_t stride_h, int32_t n_heads, const int32_t* positions,
+                int32_t n_tokens, const hata_rotary* rotary, int32_t back, void* out, int64_t out_stride_t, int64_t out_stride_h,
+                void* stream);
+
+/* hata_write_slots with the keys rotated on the way (positions [n_tokens], as hata_plan_pages gives them, or of the tokens' depth in a
+ * tree), and the queries of the same rows: q_out [n_tokens, Hq, d], contiguous, of every row, also of those that go nowhere.  q and q_out
+ * both NULL: no queries; q_out may be q where its strides are q_out's.  Key codes are those of the rotated keys as the cache
+ * holds them, in every other way as in hata_write_slots. */
+int hata_rotate_write_slots(hata_ctx* ctx, const void* q, int64_t q_stride_t, int64_t q_stride_h, void* q_out, const void* K_new,
+                            const void* V_new, int64_t stride_t, int64_t stride_h, const int32_t* positions, const int32_t* slots,
+                            int32_t n_tokens, const hata_rotary* rotary, void* K_pool, void* V_pool, uint32_t* codes_pool,
+                            int32_t page_rows, int32_t n_pages, const float* W_H, void* stream);
+
+/* Dense attention of drafted tokens on the paged layout: token i of sequence b, which is packed row t = token_start[b] + i of q and out
+ * [n_tokens, Hq, d], attends over rows 0 .. base_len[b] - 1, which every token of b sees, and of the rows behind them, base_len[b] + j <
+ * seq_len[b] for the sequence's drafted token j, over those that its mask names.
+ *   base_len, seq_len [B]    rows before the draft, and with it (hata_plan_pages' len_now and seq_len: a request that was not granted has
+ *                            no rows behind base_len); clamped to 0 <= base_len <= seq_len <= min(L_cap, max_blocks * page_rows)
+ *   token_start [B + 1]      ascending, as hata_plan_pages gives it; entries are clamped to [0, n_tokens].  Packed rows of no sequence, and a sequence's
+ *                            tokens from max_draft on, are left as they are
+ *   max_draft (host)         1 .. 256, the most tokens a sequence has
+ *   mask [n_tokens, mask_words] or NULL: bit j % 32 of word j / 32 says whether the row's token sees drafted token j of its
+ *                            sequence; nothing is implied, not even that it sees itself.  mask_words >= max_draft / 32.  NULL: j <= i
+ *                            (a chain; a chunk of a prompt).  Drafted rows from max_draft on are seen by nobody
+ * A token that sees no row gives zeros.  A row that a token does not see has no effect on it, whatever is in the row (NaN,
+ * infinities).  out 16-byte aligned, out_f32 NULL or 16-byte aligned.  n_tokens * Hq < 2^24.
+ * scratch: device memory of the caller, 256-byte aligned, of hata_tree_scratch_bytes for the same numbers or larger ones; it carries nothing from
+ * one call to the next, and calls that may overlap need one each.  (It is not part of the context's workspace: contexts that never draft do
+ * not pay for it.)  No residency needed, no in-kernel waits. */
+int hata_tree_scratch_bytes(const hata_ctx* ctx, int32_t B, int32_t n_tokens, int32_t max_draft, size_t* out);
+int hata_dense_tree_paged(hata_ctx* ctx, const void* q, const void* K_pool, const void* V_pool, const int32_t* block_table,
+                          int32_t max_blocks, int32_t page_rows, int32_t n_pages, const int32_t* base_len, const int32_t* seq_len,
+                          int32_t B, const int32_t* token_start, int32_t n_tokens, int32_t max_draft, const uint32_t* mask,
+                          int32_t mask_words, float sm_scale, void* out, float* out_f32, void* scratch, size_t scratch_bytes,
+                          void* stream);
+
+/* The rows of the accepted path moved together: row base_len[b] + i of sequence b becomes what row base_len[b] + path[b, i] was, for
+ * i < n_path[b], in K_pool, V_pool and codes_pool (NULL: no codes), for every KV head.  path [B, max_path], n_path [B] (clamped to
+ * [0, max_path]), max_path 1 .. 256: a path ends in front of the first entry that is not above the one before it (they ascend from the root on),
+ * or names no row of the draft (base_len[b] + path[b, i] >= seq_len[b], or negative).
+ *   seq_len_out [B]          output: base_len[b] and the entries of the path; no input of the call
+ * The pages that hold the path's rows belong to one sequence.  base_len, seq_len: as in hata_dense_tree_paged.  One launch. */
+int hata_keep_rows(hata_ctx* ctx, void* K_pool, void* V_pool, uint32_t* codes_pool, const int32_t* block_table, int32_t max_blocks,
+                   int32_t page_rows, int32_t n_pages, const int32_t* base_len, const int32_t* seq_len, int32_t B, const int32_t* path,
+                   const int32_t* n_path, int32_t max_path, int32_t* seq_len_out, void* stream);
+
 /* Host-side query of how hata_decode_step() runs a batch of B sequences; nothing is enqueued.
  * *n_launches: 1 (single-launch form) or 3 (the form without in-kernel waits, also where its first two launches go as one: see
  * hata_decode_step); *chunk: cached keys per scoring workgroup for a batch of this size (the launch that encodes and scores may give one up

@@ -251,6 +251,13 @@ inline int make_page_view(const hata_ctx* c, const int32_t* block_table, int32_t
     pv->table = block_table; pv->max_blocks = max_blocks; pv->shift = shift; pv->n_pages = n_pages;
     return HATA_OK;
 }
+// Strides of packed rows: not negative, whole 16-byte pieces
+inline bool row_strides(int64_t t, int64_t h) { return t >= 0 && h >= 0 && t % 8 == 0 && h % 8 == 0; }
+inline int check_rotary(const hata_rotary* r) {
+    if (!r || !r->freq || !aligned(r->freq, 8) || (r->interleaved & ~1)) return HATA_EINVAL;
+    if (r->dims < 16 || r->dims > 128 || r->dims % 16 != 0) return HATA_EUNSUPPORTED;
+    return HATA_OK;
+}
 inline int hip_rc(hipError_t e) { return e == hipSuccess ? HATA_OK : HATA_EHIP; }
 
 }  // namespace
@@ -707,6 +714,129 @@ int hata_dense_decode_paged(hata_ctx* ctx, const void* q, const void* K_pool, co
         if (e != hipSuccess) return HATA_EHIP;
     }
     return hip_rc(hata::launch_dense(ctx, q, K_pool, V_pool, seq_len, B, sm_scale, out, out_f32, (hipStream_t)stream, &pv, pre_rows));
+}
+
+int hata_rotary_frequencies(int32_t dims, double base, const hata_rotary_scaling* scaling, double* freq, float* magnitude) {
+    if (!freq || !magnitude) return HATA_EINVAL;
+    if (dims < 16 || dims > 128 || dims % 16 != 0) return HATA_EUNSUPPORTED;
+    if (!(base > 1.0) || !(base < 1e300)) return HATA_EINVAL;
+    if (scaling && scaling->kind != HATA_ROTARY_NONE) {
+        const hata_rotary_scaling& f = *scaling;
+        if (f.kind < HATA_ROTARY_NONE || f.kind > HATA_ROTARY_RAMP) return HATA_EINVAL;
+        if (!(f.factor > 0.0) || !(f.factor < 1e300)) return HATA_EINVAL;
+        if (f.kind >= HATA_ROTARY_BANDS && (!(f.low > 0.0) || !(f.high > f.low) || !(f.high < 1e300) || !(f.original > 0.0) || !(f.original < 1e300)))
+            return HATA_EINVAL;
+    }
+    return hata::rotary_frequencies(dims / 2, base, scaling, freq, magnitude);
+}
+
+int hata_rotate(hata_ctx* ctx, const void* x, int64_t stride_t, int64_t stride_h, int32_t n_heads, const int32_t* positions,
+                int32_t n_tokens, const hata_rotary* rotary, int32_t back, void* out, int64_t out_stride_t, int64_t out_stride_h,
+                void* stream) {
+    if (!ctx || n_tokens < 0 || n_heads < 1 || n_heads > 65535) return HATA_EINVAL;
+    if (!x || !out || !positions) return HATA_EINVAL;
+    const int rc = check_rotary(rotary);
+    if (rc != HATA_OK) return rc;
+    if (!row_strides(stride_t, stride_h) || !row_strides(out_stride_t, out_stride_h)) return HATA_EINVAL;
+    if (!aligned(x, 16) || !aligned(out, 16) || !aligned(positions, 4)) return HATA_EINVAL;
+    if (n_tokens == 0) return HATA_OK;
+    hata::RotateRows a = {};
+    a.x = (const uint16_t*)x; a.out = (uint16_t*)out; a.positions = positions;
+    a.st = stride_t; a.sh = stride_h; a.out_st = out_stride_t; a.out_sh = out_stride_h;
+    a.freq = rotary->freq; a.magnitude = rotary->magnitude; a.dims = rotary->dims; a.interleaved = rotary->interleaved;
+    a.n = n_tokens; a.heads = n_heads; a.back = back;
+    return hip_rc(hata::launch_rotate(a, (hipStream_t)stream));
+}
+
+int hata_rotate_write_slots(hata_ctx* ctx, const void* q, int64_t q_stride_t, int64_t q_stride_h, void* q_out, const void* K_new,
+                            const void* V_new, int64_t stride_t, int64_t stride_h, const int32_t* positions, const int32_t* slots,
+                            int32_t n_tokens, const hata_rotary* rotary, void* K_pool, void* V_pool, uint32_t* codes_pool,
+                            int32_t page_rows, int32_t n_pages, const float* W_H, void* stream) {
+    if (!ctx || n_tokens < 0) return HATA_EINVAL;
+    if (!K_new || !V_new || !positions || !slots || !K_pool || !V_pool || !codes_pool != !W_H || !q != !q_out) return HATA_EINVAL;
+    int rc = check_rotary(rotary);
+    if (rc != HATA_OK) return rc;
+    if (!row_strides(stride_t, stride_h) || (q && !row_strides(q_stride_t, q_stride_h))) return HATA_EINVAL;
+    if (!aligned(q, 16) || !aligned(q_out, 16) || !aligned(K_new, 16) || !aligned(V_new, 16) || !aligned(K_pool, 16) || !aligned(V_pool, 16) ||
+        !aligned(codes_pool, 16) || !aligned(W_H, 16) || !aligned(slots, 4) || !aligned(positions, 4))
+        return HATA_EINVAL;
+    int shift = 0;
+    rc = check_pools(ctx, page_rows, n_pages, &shift);
+    if (rc != HATA_OK) return rc;
+    if (n_tokens == 0) return HATA_OK;
+    const hata_config& f = ctx->cfg;
+    hata::RotateRows a = {};
+    a.x = (const uint16_t*)q; a.out = (uint16_t*)q_out; a.positions = positions; a.slots = slots;
+    a.st = q_stride_t; a.sh = q_stride_h; a.out_st = (int64_t)f.Hq * f.d; a.out_sh = f.d;
+    a.K_new = (const uint16_t*)K_new; a.V_new = (const uint16_t*)V_new; a.kv_st = stride_t; a.kv_sh = stride_h;
+    a.K = (uint16_t*)K_pool; a.V = (uint16_t*)V_pool;
+    a.freq = rotary->freq; a.magnitude = rotary->magnitude; a.dims = rotary->dims; a.interleaved = rotary->interleaved;
+    a.n = n_tokens; a.heads = q ? f.Hq : 0; a.Hkv = f.Hkv; a.shift = shift; a.rows = n_pages << shift;
+    hipError_t e = hata::launch_rotate(a, (hipStream_t)stream);
+    if (e == hipSuccess && codes_pool)
+        e = hata::launch_slot_codes(ctx, slots, n_tokens, K_pool, codes_pool, shift, n_pages, W_H, (hipStream_t)stream);
+    return hip_rc(e);
+}
+
+int hata_tree_scratch_bytes(const hata_ctx* ctx, int32_t B, int32_t n_tokens, int32_t max_draft, size_t* out) {
+    const int rc = check_call(ctx, B);
+    if (rc != HATA_OK) return rc;
+    if (!out || n_tokens < 0 || max_draft < 1) return HATA_EINVAL;
+    if (max_draft > HATA_TREE_MAX_DRAFT) return HATA_EUNSUPPORTED;
+    *out = hata::tree_scratch_bytes(B, ctx->cfg.Hkv, ctx->G, n_tokens, max_draft);
+    return HATA_OK;
+}
+
+int hata_dense_tree_paged(hata_ctx* ctx, const void* q, const void* K_pool, const void* V_pool, const int32_t* block_table,
+                          int32_t max_blocks, int32_t page_rows, int32_t n_pages, const int32_t* base_len, const int32_t* seq_len,
+                          int32_t B, const int32_t* token_start, int32_t n_tokens, int32_t max_draft, const uint32_t* mask,
+                          int32_t mask_words, float sm_scale, void* out, float* out_f32, void* scratch, size_t scratch_bytes,
+                          void* stream) {
+    int rc = check_call(ctx, B);
+    if (rc != HATA_OK) return rc;
+    if (!q || !K_pool || !V_pool || !base_len || !seq_len || !token_start || !out) return HATA_EINVAL;
+    if (n_tokens < 0 || max_draft < 1) return HATA_EINVAL;
+    if (max_draft > HATA_TREE_MAX_DRAFT) return HATA_EUNSUPPORTED;
+    if (mask && ((int64_t)mask_words * 32 < max_draft || mask_words > (1 << 16))) return HATA_EINVAL;
+    if (!aligned(q, 16) || !aligned(K_pool, 16) || !aligned(V_pool, 16) || !aligned(out, 16) || !aligned(out_f32, 16) ||
+        !aligned(block_table, 4) || !aligned(base_len, 4) || !aligned(seq_len, 4) || !aligned(token_start, 4) || !aligned(mask, 4))
+        return HATA_EINVAL;
+    hata::PageView pv;
+    rc = make_page_view(ctx, block_table, max_blocks, page_rows, n_pages, &pv);
+    if (rc != HATA_OK) return rc;
+    if ((int64_t)n_tokens * ctx->cfg.Hq > 0x7fffffffll / 128) return HATA_EUNSUPPORTED;
+    if (!scratch || !aligned(scratch, kAlign) || scratch_bytes < hata::tree_scratch_bytes(B, ctx->cfg.Hkv, ctx->G, n_tokens, max_draft))
+        return HATA_EWORKSPACE;
+    if (n_tokens == 0) return HATA_OK;
+    const int64_t cap = (int64_t)max_blocks * page_rows;
+    const hata_config& f = ctx->cfg;
+    const hata::TreeArgs a = {(const uint16_t*)q, (const uint16_t*)K_pool, (const uint16_t*)V_pool, base_len, seq_len, token_start, mask,
+                              (uint16_t*)out, out_f32, pv, B, f.Hq, f.Hkv, ctx->G, cap < f.L_cap ? (int)cap : f.L_cap, n_tokens,
+                              max_draft, mask_words, sm_scale * 1.4426950408889634f};
+    return hip_rc(hata::launch_tree(ctx, a, (hipStream_t)stream));
+}
+
+int hata_keep_rows(hata_ctx* ctx, void* K_pool, void* V_pool, uint32_t* codes_pool, const int32_t* block_table, int32_t max_blocks,
+                   int32_t page_rows, int32_t n_pages, const int32_t* base_len, const int32_t* seq_len, int32_t B, const int32_t* path,
+                   const int32_t* n_path, int32_t max_path, int32_t* seq_len_out, void* stream) {
+    int rc = check_call(ctx, B);
+    if (rc != HATA_OK) return rc;
+    if (!K_pool || !V_pool || !base_len || !seq_len || !path || !n_path || !seq_len_out || max_path < 1) return HATA_EINVAL;
+    if (max_path > HATA_TREE_MAX_DRAFT) return HATA_EUNSUPPORTED;
+    // (several workgroups read what one of them would have written)
+    if (seq_len_out == base_len || seq_len_out == seq_len || seq_len_out == n_path || seq_len_out == path) return HATA_EINVAL;
+    if (!aligned(K_pool, 16) || !aligned(V_pool, 16) || !aligned(codes_pool, 16)) return HATA_EINVAL;
+    for (const void* p : {(const void*)block_table, (const void*)base_len, (const void*)seq_len, (const void*)path, (const void*)n_path,
+                          (const void*)seq_len_out})
+        if (!aligned(p, 4)) return HATA_EINVAL;
+    hata::PageView pv;
+    rc = make_page_view(ctx, block_table, max_blocks, page_rows, n_pages, &pv);
+    if (rc != HATA_OK) return rc;
+    const int64_t cap = (int64_t)max_blocks * page_rows;
+    const hata_config& f = ctx->cfg;
+    const hata::KeepRows a = {(uint16_t*)K_pool, (uint16_t*)V_pool, codes_pool, base_len, seq_len, path, n_path, seq_len_out, pv,
+                              f.Hkv, ctx->Wd, cap < f.L_cap ? (int)cap : f.L_cap, max_path};
+    return hip_rc(hata::launch_keep_rows(a, B, (hipStream_t)stream));
 }
 
 int hata_step_plan(const hata_ctx* ctx, int32_t B, int32_t* n_launches, int32_t* chunk, int32_t* n_chunks) {

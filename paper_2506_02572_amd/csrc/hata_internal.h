@@ -127,6 +127,46 @@ hipError_t launch_plan_pages(const hata_ctx* c, const PagePlan& p, hipStream_t s
 hipError_t launch_write_slots(const hata_ctx* c, const void* K_new, const void* V_new, int64_t stride_t, int64_t stride_h,
                               const int32_t* slots, int n_tokens, void* K_pool, void* V_pool, uint32_t* codes, int shift, int n_pages,
                               const float* W_H, hipStream_t s);
+// codes of rows that lie in their slots already
+hipError_t launch_slot_codes(const hata_ctx* c, const int32_t* slots, int n_tokens, const void* K_pool, uint32_t* codes, int shift,
+                             int n_pages, const float* W_H, hipStream_t s);
+// Packed rows to rotate: `heads` heads into `out`, and with Hkv > 0 keys (rotated) and values (not) into the slots of the pools
+struct RotateRows {
+    const uint16_t* x;
+    uint16_t* out;
+    const uint16_t *K_new, *V_new;
+    uint16_t *K, *V;
+    const int32_t *positions, *slots;
+    const double* freq;
+    int64_t st, sh, out_st, out_sh, kv_st, kv_sh;  // strides in elements
+    double magnitude;
+    int n, heads, Hkv, dims, interleaved, back, shift, rows, per;  // rows: of one head in the pools; per: heads of a wave
+};
+hipError_t launch_rotate(const RotateRows& a, hipStream_t s);
+int rotary_frequencies(int pairs, double base, const hata_rotary_scaling* sc, double* freq, float* magnitude);
+// Drafted tokens of B sequences over their pages
+#define HATA_TREE_MAX_DRAFT 256
+struct TreeArgs {
+    const uint16_t *q, *K, *V;
+    const int32_t *base, *seq_len, *token_start;
+    const uint32_t* mask;  // [n_tokens, words], or nullptr: a token sees those before it and itself
+    uint16_t* out;
+    float* out_f32;
+    PageView pv;
+    int B, Hq, Hkv, G, L_cap, n_tokens, max_draft, words;
+    float scale_log2;
+};
+size_t tree_scratch_bytes(int B, int Hkv, int G, int n_tokens, int max_draft);
+hipError_t launch_tree(const hata_ctx* c, const TreeArgs& a, hipStream_t s);
+struct KeepRows {
+    uint16_t *K, *V;
+    uint32_t* codes;
+    const int32_t *base, *seq_len, *path, *n_path;
+    int32_t* seq_len_out;
+    PageView pv;
+    int Hkv, Wd, L_cap, max_path;
+};
+hipError_t launch_keep_rows(const KeepRows& a, int B, hipStream_t s);
 hipError_t prepare_topk();   // once per context
 hipError_t prepare_attention(const hata_ctx* c);  // once per context
 hipError_t launch_topk(const hata_ctx* c, const uint16_t* scores, const int32_t* seq_len,

@@ -250,6 +250,7 @@ struct WriteSlots {
     const float* W_H;
     int64_t st, sh;
     int n, Hkv, r, shift, rows;  // rows: of one head in the pools
+    bool held;  // the rows lie in their slots already (K_new, V_new are not read)
 };
 
 __device__ __forceinline__ int64_t slot_row(const WriteSlots& a, int slot, int h) {
@@ -261,7 +262,7 @@ __global__ __launch_bounds__(256) void write_few_kernel(const WriteSlots a) {
     constexpr int WPS = COLS / 32;
     __shared__ uint32_t s_codes[(WRITE_ROWS + 4) * WPS];
     const int tid = threadIdx.x, h = blockIdx.y, t0 = blockIdx.z * WRITE_ROWS, nv = min(WRITE_ROWS, a.n - t0);
-    if (blockIdx.x == 0) {
+    if (blockIdx.x == 0 && !a.held) {
         const int t = t0 + (tid >> 4), o = (tid & 15) * 8;
         const int slot = t < a.n ? a.slots[t] : -1;
         if (slot >= 0 && slot < a.rows) {
@@ -275,7 +276,10 @@ __global__ __launch_bounds__(256) void write_few_kernel(const WriteSlots a) {
     hw.fetch(a.W_H + (int64_t)h * HATA_D * a.r + blockIdx.x * COLS, a.r);
     for (int v0 = 0; v0 < nv; v0 += 4) {
         uint4 x[4];
-        hash_load_x(a.K_new + (int64_t)(t0 + min(v0 + (tid & 3), nv - 1)) * a.st + h * a.sh, x);
+        const int t = t0 + min(v0 + (tid & 3), nv - 1);
+        const uint16_t* row = a.K_new + (int64_t)t * a.st + h * a.sh;
+        if (a.held) row = a.K + slot_row(a, clampi(a.slots[t], 0, a.rows - 1), h) * HATA_D;
+        hash_load_x(row, x);
         hash_pass<COLS>(hw, x, s_codes, WPS, v0, nv);
     }
     __syncthreads();
@@ -526,7 +530,7 @@ hipError_t launch_write_slots(const hata_ctx* c, const void* K_new, const void* 
                               const float* W_H, hipStream_t s) {
     const hata_config& f = c->cfg;
     const WriteSlots all = {(const uint16_t*)K_new, (const uint16_t*)V_new, slots, (uint16_t*)K_pool, (uint16_t*)V_pool, codes, W_H,
-                            stride_t, stride_h, n_tokens, f.Hkv, f.r, shift, n_pages << shift};
+                            stride_t, stride_h, n_tokens, f.Hkv, f.r, shift, n_pages << shift, false};
     const int most = 65535 * WRITE_ROWS;  // rows of a launch
     for (int t0 = 0; t0 < n_tokens; t0 += most) {
         WriteSlots a = all;
@@ -557,6 +561,23 @@ hipError_t launch_write_slots(const hata_ctx* c, const void* K_new, const void* 
         const hipError_t e = hipGetLastError();
         if (e != hipSuccess) return e;
         if (n_tokens - t0 <= most) break;  // (t0 stays below 2^31)
+    }
+    return hipSuccess;
+}
+
+hipError_t launch_slot_codes(const hata_ctx* c, const int32_t* slots, int n_tokens, const void* K_pool, uint32_t* codes, int shift,
+                             int n_pages, const float* W_H, hipStream_t s) {
+    const hata_config& f = c->cfg;
+    const int most = 65535 * WRITE_ROWS, cols = f.r % 64 == 0 ? 64 : 32;
+    for (int t0 = 0; t0 < n_tokens;) {
+        const int n = std::min(most, n_tokens - t0);
+        const WriteSlots a = {nullptr, nullptr, slots + t0, (uint16_t*)K_pool, nullptr, codes, W_H, 0, 0, n, f.Hkv, f.r, shift, n_pages << shift, true};
+        hipLaunchKernelGGL((cols == 64 ? write_few_kernel<64> : write_few_kernel<32>), dim3(f.r / cols, f.Hkv, (n + WRITE_ROWS - 1) / WRITE_ROWS),
+                           dim3(256), 0, s, a);
+        const hipError_t e = hipGetLastError();
+        if (e != hipSuccess) return e;
+        if (n_tokens - t0 <= most) break;
+        t0 += most;
     }
     return hipSuccess;
 }

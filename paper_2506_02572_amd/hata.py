@@ -19,7 +19,8 @@ EXPORTS = (
     "hata_destroy", "hata_encode_keys", "hata_prepare_weights",
     "hata_prefill_write", "hata_prefill_write_paged", "hata_encode_query", "hata_hamming_score", "hata_topk", "hata_sparse_decode",
     "hata_sparse_decode_static", "hata_gather_rows", "hata_dense_decode", "hata_decode_step", "hata_select_step", "hata_decode_step_paged", "hata_plan_pages", "hata_write_slots",
-    "hata_dense_decode_paged", "hata_step_plan", "hata_step_sub_batches", "hata_set_step_mode", "hata_keep_step_scores", "hata_set_wait_limit",
+    "hata_dense_decode_paged", "hata_rotary_frequencies", "hata_rotate", "hata_rotate_write_slots", "hata_tree_scratch_bytes",
+    "hata_dense_tree_paged", "hata_keep_rows", "hata_step_plan", "hata_step_sub_batches", "hata_set_step_mode", "hata_keep_step_scores", "hata_set_wait_limit",
     "hata_check",
     "hata_host_device_pointer", "hata_step_buffers", "hata_probe_mfma_stream",
 )
@@ -43,6 +44,17 @@ class hata_tuning(ctypes.Structure):
     _fields_ = [("chunk", ctypes.c_int32), ("attn_rows", ctypes.c_int32), ("par_merge", ctypes.c_int32),
                 ("shared_device", ctypes.c_int32)]
 
+
+class hata_rotary(ctypes.Structure):
+    _fields_ = [("freq", ctypes.c_void_p), ("dims", ctypes.c_int32), ("interleaved", ctypes.c_int32), ("magnitude", ctypes.c_float)]
+
+
+class hata_rotary_scaling(ctypes.Structure):
+    _fields_ = [("kind", ctypes.c_int32), ("factor", ctypes.c_double), ("low", ctypes.c_double), ("high", ctypes.c_double),
+                ("original", ctypes.c_double)]
+
+
+ROTARY_KINDS = ("none", "linear", "base", "bands", "ramp")
 
 _lib = None
 _vp = ctypes.c_void_p
@@ -95,6 +107,16 @@ def load_library(build_if_missing: bool = True) -> ctypes.CDLL:
     lib.hata_write_slots.argtypes = [_vp, _vp, _vp, ctypes.c_int64, ctypes.c_int64, _vp, _i32, _vp, _vp, _vp, _i32, _i32, _vp, _vp]
     lib.hata_dense_decode_paged.argtypes = [_vp, _vp, _vp, _vp, _vp, _i32, _i32, _i32, _vp, _i32, _vp, _vp, _i32, ctypes.c_float,
                                             _vp, _vp, _vp]
+    i64 = ctypes.c_int64
+    lib.hata_rotary_frequencies.argtypes = [_i32, ctypes.c_double, ctypes.POINTER(hata_rotary_scaling), ctypes.POINTER(ctypes.c_double),
+                                            ctypes.POINTER(ctypes.c_float)]
+    lib.hata_rotate.argtypes = [_vp, _vp, i64, i64, _i32, _vp, _i32, ctypes.POINTER(hata_rotary), _i32, _vp, i64, i64, _vp]
+    lib.hata_rotate_write_slots.argtypes = [_vp, _vp, i64, i64, _vp, _vp, _vp, i64, i64, _vp, _vp, _i32, ctypes.POINTER(hata_rotary),
+                                            _vp, _vp, _vp, _i32, _i32, _vp, _vp]
+    lib.hata_tree_scratch_bytes.argtypes = [_vp, _i32, _i32, _i32, ctypes.POINTER(ctypes.c_size_t)]
+    lib.hata_dense_tree_paged.argtypes = [_vp, _vp, _vp, _vp, _vp, _i32, _i32, _i32, _vp, _vp, _i32, _vp, _i32, _i32, _vp, _i32,
+                                          ctypes.c_float, _vp, _vp, _vp, ctypes.c_size_t, _vp]
+    lib.hata_keep_rows.argtypes = [_vp, _vp, _vp, _vp, _vp, _i32, _i32, _i32, _vp, _vp, _i32, _vp, _vp, _i32, _vp, _vp]
     lib.hata_step_plan.argtypes = [_vp, _i32, ctypes.POINTER(_i32), ctypes.POINTER(_i32), ctypes.POINTER(_i32)]
     lib.hata_step_sub_batches.argtypes = [_vp, _i32, ctypes.POINTER(_i32)]
     lib.hata_set_step_mode.argtypes = [_vp, _i32]
@@ -152,6 +174,36 @@ def _stream(stream=None):
         torch.cuda.init()
         _raw_stream = torch._C._cuda_getCurrentRawStream, torch._C._cuda_getDevice
     return _raw_stream[0](_raw_stream[1]())
+
+
+def rotary_frequencies(dims, base, kind="none", factor=1.0, low=1.0, high=4.0, original=8192.0):
+    """(radians a position of the dims / 2 pairs as a list, factor of the rotated channels), see hata_rotary_frequencies."""
+    if kind not in ROTARY_KINDS:
+        raise HataError(f"scaling {kind!r} is none of {ROTARY_KINDS}")
+    freq, magnitude = (ctypes.c_double * max(dims // 2, 1))(), ctypes.c_float()
+    scaling = hata_rotary_scaling(ROTARY_KINDS.index(kind), factor, low, high, original)
+    _check(load_library().hata_rotary_frequencies(dims, base, ctypes.byref(scaling), freq, ctypes.byref(magnitude)),
+           "hata_rotary_frequencies")
+    return list(freq), magnitude.value
+
+
+class Rotary:
+    """What a model's rotary positions are: frequencies (fp64 device tensor, one a pair), layout of the pairs, factor."""
+
+    def __init__(self, freq, interleaved=False, magnitude=1.0):
+        import torch
+        if freq.dtype != torch.float64 or not freq.is_cuda or not freq.is_contiguous() or freq.dim() != 1:
+            raise HataError("frequencies: a contiguous fp64 device tensor, one a pair of channels")
+        self.freq = freq
+        self.struct = hata_rotary(freq.data_ptr(), 2 * freq.numel(), 1 if interleaved else 0, magnitude)
+        self.ref = ctypes.byref(self.struct)
+
+    @classmethod
+    def scaled(cls, dims, base, interleaved=False, device="cuda:0", **scaling):
+        """The frequencies of hata_rotary_frequencies; scaling: kind, factor, low, high, original."""
+        import torch
+        freq, magnitude = rotary_frequencies(dims, base, **scaling)
+        return cls(torch.tensor(freq, dtype=torch.float64, device=device), interleaved, magnitude)
 
 
 @dataclass
@@ -326,6 +378,50 @@ class Context:
                                                n_groups, sm_scale, _ptr(out), _ptr(out_f32), _stream(stream))
         if rc:
             _check(rc, "hata_dense_decode_paged")
+
+    def hata_rotate(self, x, stride_t, stride_h, n_heads, positions, n_tokens, rotary, back, out, out_stride_t, out_stride_h,
+                    stream=None):
+        rc = self._lib.hata_rotate(self._h, _ptr(x), stride_t, stride_h, n_heads, _ptr(positions), n_tokens, rotary.ref,
+                                   1 if back else 0, _ptr(out), out_stride_t, out_stride_h, _stream(stream))
+        if rc:
+            _check(rc, "hata_rotate")
+
+    def hata_rotate_write_slots(self, q, q_stride_t, q_stride_h, q_out, K_new, V_new, stride_t, stride_h, positions, slots, n_tokens,
+                                rotary, K_pool, V_pool, codes_pool, page_rows, n_pages, W_H, stream=None):
+        rc = self._lib.hata_rotate_write_slots(self._h, _ptr(q), q_stride_t, q_stride_h, _ptr(q_out), _ptr(K_new), _ptr(V_new), stride_t,
+                                               stride_h, _ptr(positions), _ptr(slots), n_tokens, rotary.ref, _ptr(K_pool), _ptr(V_pool),
+                                               _ptr(codes_pool), page_rows, n_pages, _ptr(W_H), _stream(stream))
+        if rc:
+            _check(rc, "hata_rotate_write_slots")
+
+    def hata_tree_scratch_bytes(self, B, n_tokens, max_draft):
+        n = ctypes.c_size_t(0)
+        rc = self._lib.hata_tree_scratch_bytes(self._h, B, n_tokens, max_draft, ctypes.byref(n))
+        if rc:
+            _check(rc, "hata_tree_scratch_bytes")
+        return n.value
+
+    def hata_tree_scratch(self, B, n_tokens, max_draft):
+        """A tensor that hata_dense_tree_paged takes as scratch, for so many sequences, tokens and tokens a sequence, or fewer."""
+        import torch
+        return torch.empty(self.hata_tree_scratch_bytes(B, n_tokens, max_draft), dtype=torch.uint8, device=self.device)
+
+    def hata_dense_tree_paged(self, q, K_pool, V_pool, block_table, max_blocks, page_rows, n_pages, base_len, seq_len, B, token_start,
+                              n_tokens, max_draft, mask, mask_words, sm_scale, out, out_f32, scratch, stream=None):
+        rc = self._lib.hata_dense_tree_paged(self._h, _ptr(q), _ptr(K_pool), _ptr(V_pool), _ptr(block_table), max_blocks, page_rows,
+                                             n_pages, _ptr(base_len), _ptr(seq_len), B, _ptr(token_start), n_tokens, max_draft,
+                                             _ptr(mask), mask_words, sm_scale, _ptr(out), _ptr(out_f32), _ptr(scratch),
+                                             0 if scratch is None else scratch.numel() * scratch.element_size(), _stream(stream))
+        if rc:
+            _check(rc, "hata_dense_tree_paged")
+
+    def hata_keep_rows(self, K_pool, V_pool, codes_pool, block_table, max_blocks, page_rows, n_pages, base_len, seq_len, B, path, n_path,
+                       max_path, seq_len_out, stream=None):
+        rc = self._lib.hata_keep_rows(self._h, _ptr(K_pool), _ptr(V_pool), _ptr(codes_pool), _ptr(block_table), max_blocks, page_rows,
+                                      n_pages, _ptr(base_len), _ptr(seq_len), B, _ptr(path), _ptr(n_path), max_path, _ptr(seq_len_out),
+                                      _stream(stream))
+        if rc:
+            _check(rc, "hata_keep_rows")
 
     def hata_step_plan(self, B):
         """(n_launches, chunk, n_chunks) of hata_decode_step for a batch of B sequences."""
