@@ -11,7 +11,7 @@ LIB = os.path.join(HERE, "libhata.so")
 OBJ = os.path.join(HERE, "_build")
 SOURCES = ["hata_api.hip", "hata_encode.hip", "hata_score.hip", "hata_topk.hip", "hata_attn.hip", "hata_dense.hip", "hata_gather.hip", "hata_pages.hip", "hata_prefix.hip", "hata_rotary.hip", "hata_tree.hip", "hata_coop.hip", "hata_unit.hip",
            "hata_train.hip", "hata_probe.hip"]
-HEADERS = ["hata_device.h", "hata_internal.h", "hata_select.h", "hata_trace.h", "hata_attn_core.h", "hata_encode_core.h", "hata_hash.h", "hata_rotary.h", os.path.join("..", "..", "include", "hata.h"),
+HEADERS = ["hata_device.h", "hata_internal.h", "hata_select.h", "hata_trace.h", "hata_attn_core.h", "hata_encode_core.h", "hata_hash.h", "hata_rotary.h", "hata_shared_rows.h", os.path.join("..", "..", "include", "hata.h"),
            os.path.join("..", "..", "include", "hata_train.h")]
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 FLAGS = [

@@ -333,7 +333,7 @@ int hata_create_tuned(hata_ctx** ctx_out, const hata_config* cfg, const hata_tun
         return HATA_EHIP;
     }
     if (hata::prepare_topk() != hipSuccess || hata::prepare_attention(c) != hipSuccess || hata::prepare_dense() != hipSuccess ||
-        hata::prepare_pages() != hipSuccess || hata::prepare_prefix() != hipSuccess) {
+        hata::prepare_pages() != hipSuccess || hata::prepare_prefix() != hipSuccess || hata::prepare_tree() != hipSuccess) {
         delete c;
         return HATA_EHIP;
     }
@@ -812,8 +812,8 @@ int hata_dense_tree_paged(hata_ctx* ctx, const void* q, const void* K_pool, cons
     const hata_config& f = ctx->cfg;
     const hata::TreeArgs a = {(const uint16_t*)q, (const uint16_t*)K_pool, (const uint16_t*)V_pool, base_len, seq_len, token_start, mask,
                               (uint16_t*)out, out_f32, pv, B, f.Hq, f.Hkv, ctx->G, cap < f.L_cap ? (int)cap : f.L_cap, n_tokens,
-                              max_draft, mask_words, sm_scale * 1.4426950408889634f};
-    return hip_rc(hata::launch_tree(ctx, a, (hipStream_t)stream));
+                              max_draft, mask_words, sm_scale * 1.4426950408889634f, nullptr, nullptr, nullptr, 0};
+    return hip_rc(hata::launch_tree(a, scratch, (hipStream_t)stream));
 }
 
 int hata_keep_rows(hata_ctx* ctx, void* K_pool, void* V_pool, uint32_t* codes_pool, const int32_t* block_table, int32_t max_blocks,

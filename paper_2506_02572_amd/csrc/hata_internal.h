@@ -146,6 +146,7 @@ hipError_t launch_rotate(const RotateRows& a, hipStream_t s);
 int rotary_frequencies(int pairs, double base, const hata_rotary_scaling* sc, double* freq, float* magnitude);
 // Drafted tokens of B sequences over their pages
 #define HATA_TREE_MAX_DRAFT 256
+struct TreeUnit { int item, step, ns, rows, first, h; };  // a KV head of a tile of tokens: its partial results, query rows and first token
 struct TreeArgs {
     const uint16_t *q, *K, *V;
     const int32_t *base, *seq_len, *token_start;
@@ -155,9 +156,15 @@ struct TreeArgs {
     PageView pv;
     int B, Hq, Hkv, G, L_cap, n_tokens, max_draft, words;
     float scale_log2;
+    // in the caller's scratch
+    int* n_units;
+    TreeUnit* units;
+    float* part;
+    int max_units;
 };
 size_t tree_scratch_bytes(int B, int Hkv, int G, int n_tokens, int max_draft);
-hipError_t launch_tree(const hata_ctx* c, const TreeArgs& a, hipStream_t s);
+hipError_t prepare_tree();  // once per context
+hipError_t launch_tree(const TreeArgs& a, void* scratch, hipStream_t s);
 struct KeepRows {
     uint16_t *K, *V;
     uint32_t* codes;
