@@ -783,7 +783,7 @@ int hata_tree_scratch_bytes(const hata_ctx* ctx, int32_t B, int32_t n_tokens, in
     if (rc != HATA_OK) return rc;
     if (!out || n_tokens < 0 || max_draft < 1) return HATA_EINVAL;
     if (max_draft > HATA_TREE_MAX_DRAFT) return HATA_EUNSUPPORTED;
-    *out = hata::tree_scratch_bytes(B, ctx->cfg.Hkv, ctx->G, n_tokens, max_draft);
+    *out = hata::tree_scratch_bytes(ctx->G, max_draft);
     return HATA_OK;
 }
 
@@ -805,14 +805,14 @@ int hata_dense_tree_paged(hata_ctx* ctx, const void* q, const void* K_pool, cons
     rc = make_page_view(ctx, block_table, max_blocks, page_rows, n_pages, &pv);
     if (rc != HATA_OK) return rc;
     if ((int64_t)n_tokens * ctx->cfg.Hq > 0x7fffffffll / 128) return HATA_EUNSUPPORTED;
-    if (!scratch || !aligned(scratch, kAlign) || scratch_bytes < hata::tree_scratch_bytes(B, ctx->cfg.Hkv, ctx->G, n_tokens, max_draft))
+    if (!scratch || !aligned(scratch, kAlign) || scratch_bytes < hata::tree_scratch_bytes(ctx->G, max_draft))
         return HATA_EWORKSPACE;
     if (n_tokens == 0) return HATA_OK;
     const int64_t cap = (int64_t)max_blocks * page_rows;
     const hata_config& f = ctx->cfg;
     const hata::TreeArgs a = {(const uint16_t*)q, (const uint16_t*)K_pool, (const uint16_t*)V_pool, base_len, seq_len, token_start, mask,
                               (uint16_t*)out, out_f32, pv, B, f.Hq, f.Hkv, ctx->G, cap < f.L_cap ? (int)cap : f.L_cap, n_tokens,
-                              max_draft, mask_words, sm_scale * 1.4426950408889634f, nullptr, nullptr, nullptr, 0};
+                              max_draft, mask_words, sm_scale * 1.4426950408889634f, nullptr, nullptr, 0};
     return hip_rc(hata::launch_tree(a, scratch, (hipStream_t)stream));
 }
 

@@ -146,7 +146,7 @@ hipError_t launch_rotate(const RotateRows& a, hipStream_t s);
 int rotary_frequencies(int pairs, double base, const hata_rotary_scaling* sc, double* freq, float* magnitude);
 // Drafted tokens of B sequences over their pages
 #define HATA_TREE_MAX_DRAFT 256
-struct TreeUnit { int item, step, ns, rows, first, h; };  // a KV head of a tile of tokens: its partial results, query rows and first token
+struct TreeSplit { int last, rows, first, h; };  // a unit that workgroup i begins and workgroup `last` ends (-1: none), its query rows, first token, KV head
 struct TreeArgs {
     const uint16_t *q, *K, *V;
     const int32_t *base, *seq_len, *token_start;
@@ -157,12 +157,11 @@ struct TreeArgs {
     int B, Hq, Hkv, G, L_cap, n_tokens, max_draft, words;
     float scale_log2;
     // in the caller's scratch
-    int* n_units;
-    TreeUnit* units;
+    TreeSplit* splits;
     float* part;
-    int max_units;
+    int part_rows;
 };
-size_t tree_scratch_bytes(int B, int Hkv, int G, int n_tokens, int max_draft);
+size_t tree_scratch_bytes(int G, int max_draft);
 hipError_t prepare_tree();  // once per context
 hipError_t launch_tree(const TreeArgs& a, void* scratch, hipStream_t s);
 struct KeepRows {

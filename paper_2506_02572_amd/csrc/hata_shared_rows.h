@@ -41,36 +41,51 @@ template <int N>
 __device__ __forceinline__ void prefix_wait() { asm volatile("s_waitcnt vmcnt(%0)" ::"n"(N) : "memory"); }
 
 __device__ __forceinline__ void store_output(uint16_t* out, float* out_f32, int64_t at, float4 o) {
-    *reinterpret_cast<uint2*>(out + at) = make_uint2(f32_to_bf16(o.x) | f32_to_bf16(o.y) << 16, f32_to_bf16(o.z) | f32_to_bf16(o.w) << 16);
+    f32x2_t lo, hi;
+    lo[0] = o.x; lo[1] = o.y; hi[0] = o.z; hi[1] = o.w;
+    *reinterpret_cast<uint2*>(out + at) = make_uint2(__builtin_bit_cast(uint32_t, __builtin_convertvector(lo, bf16x2_t)),
+                                                     __builtin_bit_cast(uint32_t, __builtin_convertvector(hi, bf16x2_t)));
     if (out_f32) *reinterpret_cast<float4*>(out_f32 + at) = o;
 }
 
-// What a workgroup of four waves has to do: `members` sequences or tokens, packed rows w.first .. of q, of KV head w.h, against split w.split of
-// w.ns of w.tiles tiles of rows of sequence w.lead's table; smem: PREFIX_LDS bytes.  The sums go to a.part as partial result w.item,
-//   [M][HATA_D], then [M][2] (reference, sum).
+// What a workgroup of four waves has to do: the query rows of w.members sequences or tokens (packed rows w.first .. of q) and KV head w.h, and
+// of the rows of sequence w.lead's table split w.split of w.ns of w.tiles tiles; smem: PREFIX_LDS bytes.  The sums go to partial result
+// w.item, [M][HATA_D], then [M][2] (reference, sum).
 // WQ: waves with query rows of their own, T: of 32 query rows of a wave, one or two.  A stage is 4 / WQ parts (one per wave with the same
 // query rows) of PART rows, K and V.
-// DRAFT: the rows are w.end, the last ones of them, from w.base on, are seen by those query rows only whose bit is set in `seen`
-// [members][SEEN_WORDS] (LDS; bits of rows from w.end on are not), and with w.ns = 1 the results are final.
+// DRAFT: tiles w.t0 .. w.t1 - 1 of w.end rows, the last ones of which, from w.base on, are seen by those members only whose bit is set in `seen`
+// [members][SEEN_WORDS] (LDS; no bit of a row from w.end on is); w.final: no other workgroup has rows of these query rows, the results go to
+// a.out.  Partial results are a.part_rows high.
 #define SEEN_WORDS 9  // of 256 drafted rows; the last is 0
+struct DraftTables {   // in LDS
+    const uint32_t* seen;
+    const int *row, *member;  // of query row r: r / G * Hq + r % G, r / G
+};
 template <int WQ, int T, bool DRAFT, class Args, class Work>
-__device__ __forceinline__ void shared_rows(const Args& a, const Work& w, char* smem, const uint32_t* seen = nullptr) {
+__device__ __forceinline__ void shared_rows(const Args& a, const Work& w, char* smem, const DraftTables& tables = {}) {
     static_assert(T == 2 || WQ == 1, "waves with 32 query rows have the same ones");
     constexpr int WK = 4 / WQ, PART = WQ == 4 ? 64 : 32, STAGE = WK * PART, SUBS = PART / 32;
     constexpr int NBUF = 256 / STAGE;                                // stages in LDS: 128 KB
     constexpr int BLOCKS = PART / WQ / 16;                           // blocks of 16 rows a wave requests of a stage, K and V
     constexpr int M = 32 * T * WQ;
-    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    int tid = threadIdx.x;
+    if constexpr (DRAFT) asm volatile("" : "+v"(tid));  // (nothing is kept from one call of a kernel's loop to the next)
+    const int lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int wq = wave % WQ, wk = wave / WQ, n = lane & 31, half = lane >> 5;
     const int G = a.G, rows = w.members * G;
     // rows of this workgroup, in tiles of 64; of a stage of 128 that reaches over the end the waves behind it have nothing to do
-    const int t0 = (int)((int64_t)w.tiles * w.split / w.ns), t1 = (int)((int64_t)w.tiles * (w.split + 1) / w.ns);
-    int k1 = t1 * PREFIX_TILE;
+    int t0, t1, k1;
     [[maybe_unused]] int base = 0, end = 0;
     if constexpr (DRAFT) {
+        t0 = w.t0;
+        t1 = w.t1;
         base = w.base;
         end = w.end;
-        k1 = min(k1, end);
+        k1 = min(t1 * PREFIX_TILE, end);
+    } else {
+        t0 = (int)((int64_t)w.tiles * w.split / w.ns);
+        t1 = (int)((int64_t)w.tiles * (w.split + 1) / w.ns);
+        k1 = t1 * PREFIX_TILE;
     }
     const int k0 = t0 * PREFIX_TILE, stages = (k1 - k0 + STAGE - 1) / STAGE;
 
@@ -79,7 +94,9 @@ __device__ __forceinline__ void shared_rows(const Args& a, const Work& w, char* 
 #pragma unroll
     for (int t = 0; t < T; ++t) {
         const int r = min(32 * T * wq + 32 * t + n, rows - 1);
-        const uint16_t* qr = a.q + ((int64_t)(w.first + r / G) * a.Hq + w.h * G + r % G) * HATA_D + 8 * half;
+        const uint16_t* qr = a.q + 8 * half;
+        if constexpr (DRAFT) qr += (int64_t)(w.first * a.Hq + w.h * G + tables.row[r]) * HATA_D;
+        else qr += ((int64_t)(w.first + r / G) * a.Hq + w.h * G + r % G) * HATA_D;
 #pragma unroll
         for (int s = 0; s < 8; ++s) qb[t][s] = *reinterpret_cast<const uint4*>(qr + 16 * s);
     }
@@ -112,7 +129,16 @@ __device__ __forceinline__ void shared_rows(const Args& a, const Work& w, char* 
 #pragma unroll
         for (int j = 0; j < BLOCKS; ++j) pages[j] = table[first_row(s, j) >> a.pv.shift];
     };
-    look_up(0);
+    constexpr int FIRST = NBUF - (WQ > 1);  // stages requested before the first is waited for
+    [[maybe_unused]] int first_pages[FIRST][BLOCKS];
+    if constexpr (DRAFT) {
+#pragma unroll
+        for (int s = 0; s < FIRST; ++s)
+#pragma unroll
+            for (int j = 0; j < BLOCKS; ++j) first_pages[s][j] = table[first_row(s, j) >> a.pv.shift];
+    } else {
+        look_up(0);
+    }
     // this wave's rows of a stage: PART wk + 16 BLOCKS wq + 16 j ..; lane l of an instruction fetches, of row 4 i + l / 16 of a block,
     // the piece that belongs at slot l % 16
     uint32_t off[4];
@@ -122,12 +148,12 @@ __device__ __forceinline__ void shared_rows(const Args& a, const Work& w, char* 
     // by one tile of query rows, mostly: 12 sequences behind 131072 rows 119 -> 108 us, 32 behind 32768 68 -> 63; with eight tiles
     // it is the same, and slower where the caches hold the rows already)
     auto fetch = [&](uint32_t dst, uint32_t o, const uint16_t* p) {
-        if constexpr (WQ <= 2)
+        if constexpr (WQ <= 2 || DRAFT)
             asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2 nt" ::"s"(dst), "v"(o), "s"(p) : "memory", "m0");
         else
             asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(dst), "v"(o), "s"(p) : "memory", "m0");
     };
-    auto request = [&](int s) {
+    auto request = [&](int s, bool ahead = true) {
 #pragma unroll
         for (int j = 0; j < BLOCKS; ++j) {
             const int row = first_row(s, j), page = clampi(pages[j], 0, a.pv.n_pages - 1);
@@ -139,7 +165,7 @@ __device__ __forceinline__ void shared_rows(const Args& a, const Work& w, char* 
                 fetch(dst + STAGE * 256 + i * 1024, off[i], a.V + at);
             }
         }
-        look_up(s + 1);
+        if (ahead) look_up(s + 1);
     };
     // The sums and the query rows live in the accumulation registers, where the matrix instructions take them from, the scores in the
     // others; said at every turn, or the compiler moves the sums to and fro
@@ -247,7 +273,7 @@ __device__ __forceinline__ void shared_rows(const Args& a, const Work& w, char* 
         const int r0 = k0 + s * STAGE + from, d = r0 - base;
 #pragma unroll
         for (int t = 0; t < T; ++t) {
-            const uint32_t* bits = seen + min((32 * T * wq + 32 * t + n) / G, w.members - 1) * SEEN_WORDS;
+            const uint32_t* bits = tables.seen + tables.member[32 * T * wq + 32 * t + n] * SEEN_WORDS;  // (of a member that is not there: anything)
             uint32_t see = 0;
             if (d < 0) see = d <= -32 ? ~0u : ((1u << -d) - 1) | bits[0] << -d;
             else if (d < 256) see = (uint32_t)(((unsigned long long)bits[(d >> 5) + 1] << 32 | bits[d >> 5]) >> (d & 31));
@@ -289,7 +315,7 @@ __device__ __forceinline__ void shared_rows(const Args& a, const Work& w, char* 
                 const uint16_t* v = a.V + ((((int64_t)page * a.Hkv + w.h) << a.pv.shift) + (row & ((1 << a.pv.shift) - 1))) * HATA_D;
 #pragma unroll
                 for (int t = 0; t < T; ++t) {
-                    const bool sees = seen[min((32 * T * wq + 32 * t + n) / G, w.members - 1) * SEEN_WORDS + k] >> (j & 31) & 1;
+                    const bool sees = tables.seen[tables.member[32 * T * wq + 32 * t + n] * SEEN_WORDS + k] >> (j & 31) & 1;
 #pragma unroll
                     for (int c = 0; c < 4; ++c)
 #pragma unroll
@@ -307,7 +333,7 @@ __device__ __forceinline__ void shared_rows(const Args& a, const Work& w, char* 
     auto at_stage = [&](int s) { return (const char*)smem + (s % NBUF) * STAGE * 512 + wk * PART * 256; };  // K; V is STAGE * 256 bytes behind
 
     // (the wait for the query rows is one for every request so far: the first stage's only)
-    request(0);
+    if constexpr (!DRAFT) request(0);
 #pragma unroll
     for (int t = 0; t < T; ++t)
 #pragma unroll
@@ -315,8 +341,18 @@ __device__ __forceinline__ void shared_rows(const Args& a, const Work& w, char* 
             asm volatile("" : "+a"(qb[t][s].x), "+a"(qb[t][s].y), "+a"(qb[t][s].z), "+a"(qb[t][s].w));
     pin();
     // (with several query waves a stage behind the last one is the last rows once more: as many requests are outstanding everywhere)
-    for (int s = 1; s < NBUF - (WQ > 1); ++s)
-        if (WQ > 1 || s < stages) request(s);
+    if constexpr (DRAFT) {  // (their pages are looked up together, beside the query rows)
+#pragma unroll
+        for (int s = 0; s < FIRST; ++s)
+            if (WQ > 1 || s < stages) {
+#pragma unroll
+                for (int j = 0; j < BLOCKS; ++j) pages[j] = first_pages[s][j];
+                request(s, s + 1 == FIRST);
+            }
+    } else {
+        for (int s = 1; s < NBUF - (WQ > 1); ++s)
+            if (WQ > 1 || s < stages) request(s);
+    }
     if constexpr (WQ == 1) {
         // rows of this wave alone: nothing is waited for but its own requests
         for (int s = 0; s < stages; ++s) {
@@ -356,9 +392,23 @@ __device__ __forceinline__ void shared_rows(const Args& a, const Work& w, char* 
                 __syncthreads();
             }
         }
-        products(at_stage(0), sc);
-        highest(sc, top);
-        for (int s = 0; s < stages; ++s) {
+        bool idle = false;
+        if constexpr (DRAFT) idle = 64 * wq >= rows;
+        if (idle) {  // (no query rows: this wave's requests and barriers alone)
+            for (int s = 0; s < stages; ++s) {
+                prefix_wait<(NBUF - 3) * 8>();
+                __syncthreads();
+                if (s + 1 < stages && k0 + (s + 2) * STAGE > base) {
+                    clean(s + 1, 0, tid, 256, STAGE);
+                    __syncthreads();
+                }
+                request(s + NBUF - 1);
+            }
+        } else {
+            products(at_stage(0), sc);
+            highest(sc, top);
+        }
+        for (int s = 0; s < (idle ? 0 : stages); ++s) {
 #pragma unroll
             for (int i = 0; i < SUBS; ++i) {
                 uint32_t p[2][2][4];  // [turn and turn][query row][two rows]
@@ -521,13 +571,17 @@ __device__ __forceinline__ void shared_rows(const Args& a, const Work& w, char* 
     }
     __syncthreads();
     bool final = false;
-    if constexpr (DRAFT) final = w.ns == 1;
-    float* out = a.part + (int64_t)w.item * (M * (HATA_D + 2));
+    int part_rows = M;
+    if constexpr (DRAFT) {
+        final = w.final;
+        part_rows = a.part_rows;
+    }
+    float* out = a.part + (int64_t)w.item * (part_rows * (HATA_D + 2));
     if (!final && wk == 0 && half == 0) {
 #pragma unroll
         for (int t = 0; t < T; ++t)
             if (64 * wq + 32 * t + n < rows)
-                *reinterpret_cast<float2*>(out + M * HATA_D + 2 * (64 * wq + 32 * t + n)) = make_float2(top[t], total[t]);
+                *reinterpret_cast<float2*>(out + part_rows * HATA_D + 2 * (64 * wq + 32 * t + n)) = make_float2(top[t], total[t]);
     }
     // eight rows a turn, four turns together
     const int r8 = tid / 32, c4 = tid % 32 * 4;
@@ -551,7 +605,7 @@ __device__ __forceinline__ void shared_rows(const Args& a, const Work& w, char* 
                     if (r >= rows) continue;
                     const float f = s_inverse[r];
                     o[j].x *= f; o[j].y *= f; o[j].z *= f; o[j].w *= f;
-                    store_output(a.out, a.out_f32, ((int64_t)(w.first + r / G) * a.Hq + w.h * G + r % G) * HATA_D + c4, o[j]);
+                    store_output(a.out, a.out_f32, (int64_t)(w.first * a.Hq + w.h * G + tables.row[r]) * HATA_D + c4, o[j]);
                 }
                 continue;
             }

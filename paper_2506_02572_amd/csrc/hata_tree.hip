@@ -15,105 +15,57 @@ __device__ __forceinline__ int pool_row(const PageView& pv, int b, int n, int h,
 
 // ---- which workgroup does what ----
 //
-// A unit is a KV head of a tile of a sequence's tokens (M / G of them: M query rows).  Every workgroup works out for itself the shortest
-// run of rows (in tiles of PREFIX_TILE) at which the launch's workgroups suffice, one per (unit, run); the tiles of tokens of a run are
-// neighbours on one XCD.  Batches of more than TREE_SPLIT_B sequences have enough units: a run each.
-#define TREE_SPLIT_B 4096
-struct TreeRun { int members, tiles, split, ns, h, first, lead, item, base, end, draft0, n; };
-struct TreeSequence { int t0, n, base, end, tiles, qt; };
+// A unit is a KV head of a tile of a sequence's tokens (TREE_ROWS / G of them at most), and costs TREE_START and a weight that goes by its
+// query rows for every tile of rows.  All units, one behind the other, are cut into as many equal pieces as there are workgroups, wherever that
+// falls; a workgroup goes through what lies in its piece.  Of these at most its first and its last one share a unit with
+// other workgroups: they leave partial results (2 i, or 2 i + 1 where the unit begins in workgroup i), and the workgroup with the unit's
+// first rows a record for the second launch.  Every workgroup works its share out from the lengths.
+#define TREE_ROWS 256
+#define TREE_WGS 256
+#define TREE_START 100  // what a unit costs beside its rows (as weights: tenths of a microsecond)
+#define TREE_LEAST 33   // what a piece costs at least: the largest weight
+struct TreeRun { int members, t0, t1, h, first, lead, item, base, end, draft0; bool final; };
+struct TreeSequence { int t0, n, base, end; };
 
-__device__ __forceinline__ TreeSequence tree_sequence(const TreeArgs& a, int mpt, int b) {
-    TreeSequence q = {0, 0, 0, 0, 0, 0};
+__device__ __forceinline__ TreeSequence tree_sequence(const TreeArgs& a, int b) {
+    TreeSequence q = {0, 0, 0, 0};
     if (b >= a.B) return q;
     q.t0 = clampi(a.token_start[b], 0, a.n_tokens);
     q.n = clampi(clampi(a.token_start[b + 1], 0, a.n_tokens) - q.t0, 0, a.max_draft);
     const int L = clampi(a.seq_len[b], 0, a.L_cap);
     q.base = clampi(a.base[b], 0, L);
     q.end = min(L, q.base + q.n);
-    q.tiles = max(1, (q.end + PREFIX_TILE - 1) / PREFIX_TILE);
-    q.qt = (q.n + mpt - 1) / mpt;
     return q;
 }
+// Of a tile of rows, with 32, 64, 128 and 256 query rows (measured in ragged batches)
+__device__ __forceinline__ int tree_weight(int rows) { return rows <= 32 ? 8 : rows <= 64 ? 12 : rows <= 128 ? 20 : 33; }
+struct TreeCosts {
+    int tiles, qt, full, last;  // weights of a tile of TREE_ROWS query rows and of the last one
+    __device__ __forceinline__ TreeCosts(const TreeSequence& q, int G) {
+        const int mpt = TREE_ROWS / G;
+        tiles = max(1, (q.end + PREFIX_TILE - 1) / PREFIX_TILE);
+        qt = (q.n + mpt - 1) / mpt;
+        full = tree_weight(TREE_ROWS);
+        last = tree_weight((q.n - (qt - 1) * mpt) * G);
+    }
+    __device__ __forceinline__ int64_t unit(int weight) const { return TREE_START + (int64_t)tiles * weight; }
+    __device__ __forceinline__ int64_t head() const { return qt ? (qt - 1) * unit(full) + unit(last) : 0; }
+};
 
-// smem: [min(B, TREE_SPLIT_B)] words
-__device__ __forceinline__ bool tree_share(const TreeArgs& a, int mpt, uint32_t* lds, TreeRun& w) {
-    const int tid = threadIdx.x, lane = tid & 63, item = (int)((blockIdx.x % 8) * (gridDim.x / 8) + blockIdx.x / 8);
-    const bool split = a.B <= TREE_SPLIT_B;
-    if (split) {
-        for (int b = tid; b < a.B; b += 256) {
-            const TreeSequence q = tree_sequence(a, mpt, b);
-            lds[b] = (uint32_t)q.tiles | (uint32_t)q.qt << 20;
-        }
-        __syncthreads();
-    }
-    int run = 0x3fffffff;
-    auto packed = [&](int b) {
-        if (split) return b < a.B ? lds[b] : 0u;
-        const TreeSequence q = tree_sequence(a, mpt, b);
-        return (uint32_t)q.tiles | (uint32_t)q.qt << 20;
-    };
-    auto splits = [&](uint32_t p) { return min((int)((p & 0xfffffu) + run - 1) / run, PREFIX_MAX_SPLITS); };
-    float units = 0.f;
-    if (split) {
-        float all = 0.f, longest = 0.f;
-        for (int b = lane; b < a.B; b += 64) {
-            const uint32_t p = lds[b];
-            units += (float)(p >> 20);
-            all += (float)(p >> 20) * (float)(p & 0xfffffu);
-            if (p >> 20) longest = fmaxf(longest, (float)(p & 0xfffffu));
-        }
-        all = wave_sum64(all);
-        longest = wave_max64(longest);
-        for (run = max(1, (int)ceilf(all * (float)a.Hkv / (float)gridDim.x)); run < (int)longest; run += max(1, run >> 4)) {
-            float items = 0.f;  // (below 2^24)
-            for (int b = lane; b < a.B; b += 64) {
-                const uint32_t p = lds[b];
-                items += (float)((p >> 20) * splits(p));
-            }
-            if (wave_sum64(items) * (float)a.Hkv <= (float)gridDim.x) break;
-        }
-    } else if (blockIdx.x == 0) {
-        for (int b0 = 0; b0 < a.B; b0 += 64) units += (float)(packed(b0 + lane) >> 20);
-    }
-    if (blockIdx.x == 0) {
-        units = wave_sum64(units);
-        if (tid == 0) *a.n_units = (int)units * a.Hkv;
-    }
-    int base = 0, unit = 0;
-    bool found = false;
-    for (int b0 = 0; b0 < a.B && !found; b0 += 64) {
-        const uint32_t p = packed(b0 + lane);
-        const int qt = (int)(p >> 20), ns = splits(p), mine = a.Hkv * qt * ns;
-        const int upto = base + (int)wave_incl_scan((uint32_t)mine), at = upto - mine;
-        const int unit_upto = unit + (int)wave_incl_scan((uint32_t)(a.Hkv * qt));
-        const unsigned long long here = __builtin_amdgcn_ballot_w64(item >= at && item < upto);
-        if (here) {
-            found = true;
-            const int l = __ffsll(here) - 1, b = b0 + l;
-            const int in = item - __builtin_amdgcn_readlane(at, l), qts = __builtin_amdgcn_readlane(qt, l), u0 = __builtin_amdgcn_readlane(unit_upto - a.Hkv * qt, l);
-            w.ns = __builtin_amdgcn_readlane(ns, l);
-            const int q = in % qts;
-            w.split = in / qts % w.ns;
-            w.h = in / (qts * w.ns);
-            const TreeSequence s = tree_sequence(a, mpt, b);
-            w.tiles = s.tiles;
-            w.lead = b;
-            w.item = item;
-            w.base = s.base;
-            w.end = s.end;
-            w.n = s.n;
-            w.draft0 = q * mpt;
-            w.first = s.t0 + w.draft0;
-            w.members = min(mpt, s.n - w.draft0);
-            const int u = u0 + w.h * qts + q;
-            if (w.split == 0 && tid == 0 && u < a.max_units) a.units[u] = TreeUnit{item, qts, w.ns, w.members * a.G, w.first, w.h};
-        }
-        base = __builtin_amdgcn_readlane(upto, 63);
-        unit = __builtin_amdgcn_readlane(unit_upto, 63);
-    }
-    __syncthreads();  // (the LDS is used anew)
-    return found;
+// x / d of numbers that are not negative, mostly below 2^32
+__device__ __forceinline__ int64_t quotient(int64_t x, int64_t d) {
+    if (((uint64_t)x | (uint64_t)d) >> 32) return x / d;
+    return (uint32_t)x / (uint32_t)d;
 }
+
+struct TreeShare {
+    int64_t pre[257];  // what lies in front of every thread's sequences
+    int64_t at;        // the sequence that the next unit belongs to, and what lies in front of it
+    int b;
+    TreeSequence q;
+    uint32_t seen[TREE_ROWS * SEEN_WORDS];
+    int row[TREE_ROWS], member[TREE_ROWS];  // of DraftTables
+};
 
 // Which drafted rows the tokens of this workgroup see
 __device__ __forceinline__ void tree_seen(const TreeArgs& a, const TreeRun& w, uint32_t* seen) {
@@ -126,69 +78,153 @@ __device__ __forceinline__ void tree_seen(const TreeArgs& a, const TreeRun& w, u
     }
 }
 
-template <int WQ, int T>
+template <bool SMALL>
 __global__ __launch_bounds__(256, 1) void tree_kernel(const TreeArgs a) {
-    constexpr int M = 32 * T * WQ;
     extern __shared__ __attribute__((aligned(16))) char smem[];
-    __shared__ uint32_t s_seen[M * SEEN_WORDS];
-    TreeRun w;
-    if (!tree_share(a, M / a.G, reinterpret_cast<uint32_t*>(smem), w)) return;
-    if (w.end == 0) {  // no rows at all
-        const int G = a.G;
-        for (int i = threadIdx.x; i < w.members * G * (HATA_D / 4); i += 256) {
-            const int r = i / (HATA_D / 4);
-            store_output(a.out, a.out_f32, ((int64_t)(w.first + r / G) * a.Hq + w.h * G + r % G) * HATA_D + i % (HATA_D / 4) * 4,
-                         make_float4(0.f, 0.f, 0.f, 0.f));
+    __shared__ TreeShare s;
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    const int wg = (int)((blockIdx.x % 8) * (TREE_WGS / 8) + blockIdx.x / 8), G = a.G, mpt = TREE_ROWS / G;
+    // what every thread's sequences cost, and all of them
+    const int per = (a.B + 255) / 256, b0 = tid * per;
+    const TreeSequence own = tree_sequence(a, b0);
+    int64_t mine = a.Hkv * TreeCosts(own, G).head();
+    for (int b = b0 + 1; b < b0 + per; ++b) mine += a.Hkv * TreeCosts(tree_sequence(a, b), G).head();
+    {
+        int64_t upto = mine;
+        for (int d = 1; d < 64; d <<= 1) {
+            const int64_t v = __shfl_up(upto, d, 64);
+            if (lane >= d) upto += v;
         }
-        return;
+        if (lane == 63) s.pre[wave] = upto;
+        __syncthreads();
+        int64_t front = 0;
+        for (int k = 0; k < wave; ++k) front += s.pre[k];
+        __syncthreads();
+        s.pre[tid + 1] = front + upto;
+        if (tid == 0) s.pre[0] = 0;
+        __syncthreads();
     }
-    if ((int64_t)w.tiles * (w.split + 1) / w.ns * PREFIX_TILE > w.base) tree_seen(a, w, s_seen);
-    __syncthreads();
-    shared_rows<WQ, T, true>(a, w, smem, s_seen);
+    s.row[tid] = tid / G * a.Hq + tid % G;
+    s.member[tid] = tid / G;
+    const DraftTables tables = {s.seen, s.row, s.member};
+    const int64_t total = s.pre[256];
+    const int pieces = (int)max((int64_t)1, min((int64_t)TREE_WGS, total / TREE_LEAST));
+    const int64_t p0 = quotient(total * min(wg, pieces), pieces), p1 = quotient(total * min(wg + 1, pieces), pieces);
+    TreeSplit split = {-1, 0, 0, 0};  // the unit that begins here and goes on elsewhere
+    int seen_of = -1, seen_first = -1;
+    int64_t pos = p0;
+    while (pos < p1) {
+        // the sequence that has the unit at pos
+        if (s.pre[tid] <= pos && pos < s.pre[tid + 1]) {
+            int b = b0;
+            int64_t at = s.pre[tid];
+            TreeSequence q = own;
+            for (int64_t c = a.Hkv * TreeCosts(q, G).head(); at + c <= pos; c = a.Hkv * TreeCosts(q, G).head()) {
+                at += c;
+                q = tree_sequence(a, ++b);
+            }
+            s.at = at;
+            s.b = b;
+            s.q = q;
+        }
+        __syncthreads();
+        const TreeSequence q = {__builtin_amdgcn_readfirstlane(s.q.t0), __builtin_amdgcn_readfirstlane(s.q.n),
+                                __builtin_amdgcn_readfirstlane(s.q.base), __builtin_amdgcn_readfirstlane(s.q.end)};
+        const int b = __builtin_amdgcn_readfirstlane(s.b);
+        const TreeCosts c(q, G);
+        const int64_t at = s.at, head = c.head(), full = c.unit(c.full);
+        int h = __builtin_amdgcn_readfirstlane((int)quotient(pos - at, head));
+        int tile = __builtin_amdgcn_readfirstlane(min((int)quotient(pos - at - h * head, full), c.qt - 1));
+        int64_t u0 = at + h * head + tile * full;
+        // its units, as far as they lie in this workgroup's piece
+        for (; h < a.Hkv && pos < p1; ++h, tile = 0)
+            for (; tile < c.qt && pos < p1; ++tile) {
+                const int weight = tile == c.qt - 1 ? c.last : c.full;
+                const int64_t u1 = u0 + c.unit(weight);
+                auto tile_at = [&](int64_t x) { return (int)((uint32_t)max((int)(x - u0) - TREE_START, 0) / (uint32_t)weight); };
+                TreeRun w;
+                w.t0 = __builtin_amdgcn_readfirstlane(p0 <= u0 ? 0 : tile_at(p0));
+                w.t1 = __builtin_amdgcn_readfirstlane(p1 >= u1 ? c.tiles : tile_at(p1));
+                w.h = h;
+                w.lead = b;
+                w.base = q.base;
+                w.end = q.end;
+                w.draft0 = tile * mpt;
+                w.first = q.t0 + w.draft0;
+                w.members = min(mpt, q.n - w.draft0);
+                w.final = w.t0 == 0 && w.t1 == c.tiles;
+                w.item = 2 * wg + (w.t0 == 0 ? 1 : 0);
+                pos = u0 = u1;
+                if (w.t1 == w.t0) continue;
+                if (w.t0 == 0 && !w.final)  // (the last workgroup whose piece begins below u1)
+                    split = TreeSplit{(int)quotient(u1 * pieces - 1, total), w.members * G, w.first, w.h};
+                if (w.end == 0) {  // no rows at all
+                    for (int i = tid; i < w.members * G * (HATA_D / 4); i += 256) {
+                        const int r = i / (HATA_D / 4);
+                        store_output(a.out, a.out_f32, (int64_t)(w.first * a.Hq + w.h * G + s.row[r]) * HATA_D + i % (HATA_D / 4) * 4,
+                                     make_float4(0.f, 0.f, 0.f, 0.f));
+                    }
+                    continue;
+                }
+                if (w.t1 * PREFIX_TILE > w.base && (seen_of != b || seen_first != w.first)) {  // (the same for all heads)
+                    tree_seen(a, w, s.seen);
+                    seen_of = b;
+                    seen_first = w.first;
+                }
+                __syncthreads();
+                const int rows = w.members * G;
+                if (SMALL || rows <= 32) shared_rows<1, 1, true>(a, w, smem, tables);
+                else if (rows <= 64) shared_rows<1, 2, true>(a, w, smem, tables);
+                else if (rows <= 128) shared_rows<2, 2, true>(a, w, smem, tables);
+                else shared_rows<4, 2, true>(a, w, smem, tables);
+                __syncthreads();  // (the LDS is used anew)
+            }
+        __syncthreads();
+    }
+    if (tid == 0) a.splits[wg] = split;
 }
 
-// The runs' results joined: eight query rows a workgroup, half a wave each
+// The results of the units that several workgroups have, joined: eight query rows a workgroup, half a wave each
 #define TREE_MERGE_ROWS 8
-__global__ __launch_bounds__(256) void tree_merge_kernel(const TreeArgs a, int M) {
-    __shared__ float s_f[TREE_MERGE_ROWS][PREFIX_MAX_SPLITS];
-    if ((int)blockIdx.x >= *a.n_units) return;
-    const TreeUnit u = a.units[blockIdx.x];
+__global__ __launch_bounds__(256) void tree_merge_kernel(const TreeArgs a) {
+    __shared__ float s_f[TREE_MERGE_ROWS][TREE_WGS];
+    const TreeSplit u = a.splits[blockIdx.x];
     const int row = threadIdx.x >> 5, r = blockIdx.y * TREE_MERGE_ROWS + row, lane = threadIdx.x & 31;
-    if (u.ns == 1 || (int)blockIdx.y * TREE_MERGE_ROWS >= u.rows) return;
-    const int at = min(r, u.rows - 1);
-    const int64_t size = (int64_t)M * (HATA_D + 2), step = u.step * size;
-    const float* part = a.part + u.item * size;
+    if (u.last < 0 || (int)blockIdx.y * TREE_MERGE_ROWS >= u.rows) return;
+    const int at = min(r, u.rows - 1), ns = u.last - (int)blockIdx.x + 1;
+    const int64_t size = (int64_t)a.part_rows * (HATA_D + 2);
+    const float* part = a.part + 2 * (int64_t)blockIdx.x * size;
+    auto of_split = [&](int s) { return part + (s ? 2 * s : 1) * size; };
     float top = HATA_NEG_INF, l = 0.f;
-    float2 ml[PREFIX_MAX_SPLITS / 32];
+    float2 ml[TREE_WGS / 32];
 #pragma unroll
-    for (int j = 0; j < PREFIX_MAX_SPLITS / 32; ++j) {
+    for (int j = 0; j < TREE_WGS / 32; ++j) {
         const int s = 32 * j + lane;
         ml[j] = make_float2(HATA_NEG_INF, 0.f);
-        if (s < u.ns) ml[j] = *reinterpret_cast<const float2*>(part + s * step + M * HATA_D + 2 * at);
+        if (s < ns) ml[j] = *reinterpret_cast<const float2*>(of_split(s) + a.part_rows * HATA_D + 2 * at);
         top = fmaxf(top, ml[j].x);
     }
     for (int m = 16; m; m >>= 1) top = fmaxf(top, __shfl_xor(top, m, 64));
     const float sub = top == HATA_NEG_INF ? 0.f : top;
 #pragma unroll
-    for (int j = 0; j < PREFIX_MAX_SPLITS / 32; ++j) {
+    for (int j = 0; j < TREE_WGS / 32; ++j) {
         const int s = 32 * j + lane;
         const float f = ml[j].x == HATA_NEG_INF ? (top == HATA_NEG_INF ? 1.f : 0.f) : fast_exp2(ml[j].x - sub);
-        if (s < u.ns) {
+        if (s < ns) {
             s_f[row][s] = f;
             l = fmaf(f, ml[j].y, l);
         }
     }
     for (int m = 16; m; m >>= 1) l += __shfl_xor(l, m, 64);
     __syncthreads();
-    const float* p = part + at * HATA_D + 4 * lane;
     float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
-    for (int s0 = 0; s0 < u.ns; s0 += 8) {
+    for (int s0 = 0; s0 < ns; s0 += 8) {
         float4 v[8];
 #pragma unroll
-        for (int j = 0; j < 8; ++j) v[j] = *reinterpret_cast<const float4*>(p + min(s0 + j, u.ns - 1) * step);
+        for (int j = 0; j < 8; ++j) v[j] = *reinterpret_cast<const float4*>(of_split(min(s0 + j, ns - 1)) + at * HATA_D + 4 * lane);
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
-            if (s0 + j >= u.ns) break;
+            if (s0 + j >= ns) break;
             const float f = s_f[row][s0 + j];
             o.x = fmaf(f, v[j].x, o.x); o.y = fmaf(f, v[j].y, o.y); o.z = fmaf(f, v[j].z, o.z); o.w = fmaf(f, v[j].w, o.w);
         }
@@ -199,30 +235,16 @@ __global__ __launch_bounds__(256) void tree_merge_kernel(const TreeArgs a, int M
     store_output(a.out, a.out_f32, ((int64_t)(u.first + r / a.G) * a.Hq + u.h * a.G + r % a.G) * HATA_D + 4 * lane, o);
 }
 
-// Query rows of a workgroup, from the mean of the sequences (what the host knows)
-static int tree_rows(int B, int G, int n_tokens) {
-    const int64_t rows = ((int64_t)n_tokens * G + B - 1) / B;
-    return rows <= 32 ? 32 : rows <= 64 ? 64 : rows <= 448 ? 128 : 256;
-}
-static int64_t tree_units(int B, int Hkv, int G, int n_tokens, int M) {
-    const int mpt = M / G;
-    return (n_tokens + (int64_t)B * (mpt - 1)) / mpt * Hkv;
-}
-static int64_t tree_wgs(int64_t units) { return std::max((int64_t)256, (units + 255) / 256 * 256); }
-
-// [the number of units][their records][partial results], for any tile of query rows that fewer tokens or sequences may go by
-static size_t tree_part_offset(int64_t units) { return 256 + ((size_t)units * sizeof(TreeUnit) + 255) / 256 * 256; }
-size_t tree_scratch_bytes(int B, int Hkv, int G, int n_tokens, int) {
-    size_t most = 0;
-    for (int M : {32, 64, 128, 256}) {
-        const int64_t units = tree_units(B, Hkv, G, n_tokens, M);
-        most = std::max(most, tree_part_offset(units) + (size_t)tree_wgs(units) * M * (HATA_D + 2) * 4);
-    }
-    return most;
+// Query rows of a unit are never more than this
+static int tree_part_rows(int G, int max_draft) { return (int64_t)max_draft * G <= 32 ? 32 : TREE_ROWS; }
+// [a record a workgroup][two partial results a workgroup]
+#define TREE_SPLITS_BYTES (TREE_WGS * sizeof(TreeSplit))
+size_t tree_scratch_bytes(int G, int max_draft) {
+    return TREE_SPLITS_BYTES + (size_t)2 * TREE_WGS * tree_part_rows(G, max_draft) * (HATA_D + 2) * 4;
 }
 
 hipError_t prepare_tree() {
-    for (const void* fn : {(const void*)tree_kernel<1, 1>, (const void*)tree_kernel<1, 2>, (const void*)tree_kernel<2, 2>, (const void*)tree_kernel<4, 2>}) {
+    for (const void* fn : {(const void*)tree_kernel<true>, (const void*)tree_kernel<false>}) {
         const hipError_t e = hipFuncSetAttribute(fn, hipFuncAttributeMaxDynamicSharedMemorySize, PREFIX_LDS);
         if (e != hipSuccess) return e;
     }
@@ -231,18 +253,14 @@ hipError_t prepare_tree() {
 
 hipError_t launch_tree(const TreeArgs& args, void* scratch, hipStream_t s) {
     TreeArgs a = args;
-    const int M = tree_rows(a.B, a.G, a.n_tokens);
-    const int64_t units = tree_units(a.B, a.Hkv, a.G, a.n_tokens, M);
-    a.n_units = (int*)scratch;
-    a.units = (TreeUnit*)((char*)scratch + 256);
-    a.part = (float*)((char*)scratch + tree_part_offset(units));
-    a.max_units = (int)units;
-    const dim3 grid((unsigned)tree_wgs(units));
-    hipLaunchKernelGGL((M == 32 ? tree_kernel<1, 1> : M == 64 ? tree_kernel<1, 2> : M == 128 ? tree_kernel<2, 2> : tree_kernel<4, 2>), grid, dim3(256),
-                       PREFIX_LDS, s, a);
-    hipError_t e = hipGetLastError();
-    if (e != hipSuccess || units == 0) return e;
-    hipLaunchKernelGGL(tree_merge_kernel, dim3((unsigned)units, M / TREE_MERGE_ROWS), dim3(256), 0, s, a, M);
+    a.part_rows = tree_part_rows(a.G, a.max_draft);
+    a.splits = (TreeSplit*)scratch;
+    a.part = (float*)((char*)scratch + TREE_SPLITS_BYTES);
+    hipLaunchKernelGGL((a.part_rows == 32 ? tree_kernel<true> : tree_kernel<false>), dim3(TREE_WGS), dim3(256), PREFIX_LDS, s, a);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+    const int rows = std::min(a.max_draft * a.G, a.part_rows);
+    hipLaunchKernelGGL(tree_merge_kernel, dim3(TREE_WGS, (rows + TREE_MERGE_ROWS - 1) / TREE_MERGE_ROWS), dim3(256), 0, s, a);
     return hipGetLastError();
 }
 
