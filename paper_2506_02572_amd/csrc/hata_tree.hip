@@ -15,15 +15,14 @@ __device__ __forceinline__ int pool_row(const PageView& pv, int b, int n, int h,
 
 // ---- which workgroup does what ----
 //
-// A unit is a KV head of a tile of a sequence's tokens (TREE_ROWS / G of them at most), and costs TREE_START and a weight that goes by its
-// query rows for every tile of rows.  All units, one behind the other, are cut into as many equal pieces as there are workgroups, wherever that
+// A unit is a KV head of a tile of a sequence's tokens (TREE_ROWS / G of them at most), and costs tree_start and for every tile of rows
+// tree_weight.  All units, one behind the other, are cut into as many equal pieces as there are workgroups, wherever that
 // falls; a workgroup goes through what lies in its piece.  Of these at most its first and its last one share a unit with
 // other workgroups: they leave partial results (2 i, or 2 i + 1 where the unit begins in workgroup i), and the workgroup with the unit's
 // first rows a record for the second launch.  Every workgroup works its share out from the lengths.
 #define TREE_ROWS 256
 #define TREE_WGS 256
-#define TREE_START 100  // what a unit costs beside its rows (as weights: tenths of a microsecond)
-#define TREE_LEAST 33   // what a piece costs at least: the largest weight
+#define TREE_LEAST 35   // what a piece costs at least: the largest weight
 struct TreeRun { int members, t0, t1, h, first, lead, item, base, end, draft0; bool final; };
 struct TreeSequence { int t0, n, base, end; };
 
@@ -37,8 +36,9 @@ __device__ __forceinline__ TreeSequence tree_sequence(const TreeArgs& a, int b) 
     q.end = min(L, q.base + q.n);
     return q;
 }
-// Of a tile of rows, with 32, 64, 128 and 256 query rows (measured in ragged batches)
-__device__ __forceinline__ int tree_weight(int rows) { return rows <= 32 ? 8 : rows <= 64 ? 12 : rows <= 128 ? 20 : 33; }
+// Tenths of a microsecond: of a tile of rows, with 32, 64, 128 and 256 query rows, and of a unit beside its rows (measured in ragged batches)
+__device__ __forceinline__ int tree_weight(int rows) { return rows <= 32 ? 8 : rows <= 64 ? 12 : rows <= 128 ? 21 : 35; }
+__device__ __forceinline__ int tree_start(int weight) { return weight == 8 ? 70 : 130; }
 struct TreeCosts {
     int tiles, qt, full, last;  // weights of a tile of TREE_ROWS query rows and of the last one
     __device__ __forceinline__ TreeCosts(const TreeSequence& q, int G) {
@@ -48,7 +48,7 @@ struct TreeCosts {
         full = tree_weight(TREE_ROWS);
         last = tree_weight((q.n - (qt - 1) * mpt) * G);
     }
-    __device__ __forceinline__ int64_t unit(int weight) const { return TREE_START + (int64_t)tiles * weight; }
+    __device__ __forceinline__ int64_t unit(int weight) const { return tree_start(weight) + (int64_t)tiles * weight; }
     __device__ __forceinline__ int64_t head() const { return qt ? (qt - 1) * unit(full) + unit(last) : 0; }
 };
 
@@ -141,7 +141,7 @@ __global__ __launch_bounds__(256, 1) void tree_kernel(const TreeArgs a) {
             for (; tile < c.qt && pos < p1; ++tile) {
                 const int weight = tile == c.qt - 1 ? c.last : c.full;
                 const int64_t u1 = u0 + c.unit(weight);
-                auto tile_at = [&](int64_t x) { return (int)((uint32_t)max((int)(x - u0) - TREE_START, 0) / (uint32_t)weight); };
+                auto tile_at = [&](int64_t x) { return (int)((uint32_t)max((int)(x - u0) - tree_start(weight), 0) / (uint32_t)weight); };
                 TreeRun w;
                 w.t0 = __builtin_amdgcn_readfirstlane(p0 <= u0 ? 0 : tile_at(p0));
                 w.t1 = __builtin_amdgcn_readfirstlane(p1 >= u1 ? c.tiles : tile_at(p1));
