@@ -772,10 +772,7 @@ int hata_rotate_write_slots(hata_ctx* ctx, const void* q, int64_t q_stride_t, in
     a.K = (uint16_t*)K_pool; a.V = (uint16_t*)V_pool;
     a.freq = rotary->freq; a.magnitude = rotary->magnitude; a.dims = rotary->dims; a.interleaved = rotary->interleaved;
     a.n = n_tokens; a.heads = q ? f.Hq : 0; a.Hkv = f.Hkv; a.shift = shift; a.rows = n_pages << shift;
-    hipError_t e = hata::launch_rotate(a, (hipStream_t)stream);
-    if (e == hipSuccess && codes_pool)
-        e = hata::launch_slot_codes(ctx, slots, n_tokens, K_pool, codes_pool, shift, n_pages, W_H, (hipStream_t)stream);
-    return hip_rc(e);
+    return hip_rc(hata::launch_rotate_write(ctx, a, codes_pool, W_H, (hipStream_t)stream));
 }
 
 int hata_tree_scratch_bytes(const hata_ctx* ctx, int32_t B, int32_t n_tokens, int32_t max_draft, size_t* out) {

@@ -127,9 +127,6 @@ hipError_t launch_plan_pages(const hata_ctx* c, const PagePlan& p, hipStream_t s
 hipError_t launch_write_slots(const hata_ctx* c, const void* K_new, const void* V_new, int64_t stride_t, int64_t stride_h,
                               const int32_t* slots, int n_tokens, void* K_pool, void* V_pool, uint32_t* codes, int shift, int n_pages,
                               const float* W_H, hipStream_t s);
-// codes of rows that lie in their slots already
-hipError_t launch_slot_codes(const hata_ctx* c, const int32_t* slots, int n_tokens, const void* K_pool, uint32_t* codes, int shift,
-                             int n_pages, const float* W_H, hipStream_t s);
 // Packed rows to rotate: `heads` heads into `out`, and with Hkv > 0 keys (rotated) and values (not) into the slots of the pools
 struct RotateRows {
     const uint16_t* x;
@@ -143,6 +140,7 @@ struct RotateRows {
     int n, heads, Hkv, dims, interleaved, back, shift, rows, per;  // rows: of one head in the pools; per: heads of a wave
 };
 hipError_t launch_rotate(const RotateRows& a, hipStream_t s);
+hipError_t launch_rotate_write(const hata_ctx* c, const RotateRows& rows, uint32_t* codes, const float* W_H, hipStream_t s);
 int rotary_frequencies(int pairs, double base, const hata_rotary_scaling* sc, double* freq, float* magnitude);
 // Drafted tokens of B sequences over their pages
 #define HATA_TREE_MAX_DRAFT 256

@@ -5,6 +5,7 @@
 #include "hata_encode_core.h"
 #include "hata_hash.h"
 #include "hata_internal.h"
+#include "hata_rotary.h"
 
 namespace hata {
 
@@ -250,7 +251,12 @@ struct WriteSlots {
     const float* W_H;
     int64_t st, sh;
     int n, Hkv, r, shift, rows;  // rows: of one head in the pools
-    bool held;  // the rows lie in their slots already (K_new, V_new are not read)
+    // with rotation: angles, and the queries of the same rows
+    RotaryArgs rot;
+    const uint16_t* q;
+    uint16_t* q_out;
+    int64_t q_st, q_sh;
+    int G;
 };
 
 __device__ __forceinline__ int64_t slot_row(const WriteSlots& a, int slot, int h) {
@@ -262,7 +268,7 @@ __global__ __launch_bounds__(256) void write_few_kernel(const WriteSlots a) {
     constexpr int WPS = COLS / 32;
     __shared__ uint32_t s_codes[(WRITE_ROWS + 4) * WPS];
     const int tid = threadIdx.x, h = blockIdx.y, t0 = blockIdx.z * WRITE_ROWS, nv = min(WRITE_ROWS, a.n - t0);
-    if (blockIdx.x == 0 && !a.held) {
+    if (blockIdx.x == 0) {
         const int t = t0 + (tid >> 4), o = (tid & 15) * 8;
         const int slot = t < a.n ? a.slots[t] : -1;
         if (slot >= 0 && slot < a.rows) {
@@ -276,16 +282,69 @@ __global__ __launch_bounds__(256) void write_few_kernel(const WriteSlots a) {
     hw.fetch(a.W_H + (int64_t)h * HATA_D * a.r + blockIdx.x * COLS, a.r);
     for (int v0 = 0; v0 < nv; v0 += 4) {
         uint4 x[4];
-        const int t = t0 + min(v0 + (tid & 3), nv - 1);
-        const uint16_t* row = a.K_new + (int64_t)t * a.st + h * a.sh;
-        if (a.held) row = a.K + slot_row(a, clampi(a.slots[t], 0, a.rows - 1), h) * HATA_D;
-        hash_load_x(row, x);
+        hash_load_x(a.K_new + (int64_t)(t0 + min(v0 + (tid & 3), nv - 1)) * a.st + h * a.sh, x);
         hash_pass<COLS>(hw, x, s_codes, WPS, v0, nv);
     }
     __syncthreads();
     for (int i = tid; i < nv * WPS; i += 256) {
         const int slot = a.slots[t0 + i / WPS];
         if (slot >= 0 && slot < a.rows) a.codes[slot_row(a, slot, h) * (a.r / 32) + blockIdx.x * WPS + i % WPS] = s_codes[i];
+    }
+}
+
+// The same with the keys rotated on the way, through LDS, and one workgroup more for every KV head: the queries of its group.  A thread
+// has a piece of a row (RotaryPiece) and works its angles out for itself, for all of the group's heads.
+template <int COLS>
+__global__ __launch_bounds__(256) void rotate_write_few_kernel(const WriteSlots a) {
+    constexpr int WPS = COLS / 32;
+    __shared__ uint32_t s_codes[(WRITE_ROWS + 4) * WPS];
+    __shared__ __attribute__((aligned(16))) uint16_t s_key[WRITE_ROWS * HATA_D];
+    const int tid = threadIdx.x, h = blockIdx.y, t0 = blockIdx.z * WRITE_ROWS, nv = min(WRITE_ROWS, a.n - t0);
+    const int p = tid & 7, v = (tid >> 3) & (WRITE_ROWS - 1), second = tid >> 7, t = t0 + min(v, nv - 1);
+    const RotaryPiece piece(p, a.rot.dims, a.rot.interleaved);
+    const int slices = a.codes ? a.r / COLS : 1;
+    if ((int)blockIdx.x == slices) {  // queries
+        const RotaryAngles angles(a.rot, p);
+        const int position = a.rot.positions[t];
+        if (v >= nv) return;
+        for (int g = second; g < a.G; g += 2) {
+            const uint16_t* from = a.q + t * a.q_st + (h * a.G + g) * a.q_sh;
+            uint16_t* to = a.q_out + ((int64_t)t * a.Hkv * a.G + h * a.G + g) * HATA_D;
+            uint4 x[2] = {*reinterpret_cast<const uint4*>(from + piece.at[0]), *reinterpret_cast<const uint4*>(from + piece.at[1])};
+            angles.rotate(a.rot, x, position);
+            *reinterpret_cast<uint4*>(to + piece.at[0]) = x[0];
+            *reinterpret_cast<uint4*>(to + piece.at[1]) = x[1];
+        }
+        return;
+    }
+    HashWeights<COLS> hw;
+    if (a.codes) hw.fetch(a.W_H + (int64_t)h * HATA_D * a.r + blockIdx.x * COLS, a.r);
+    const int slot = a.slots[t];
+    const bool live = v < nv && slot >= 0 && slot < a.rows;
+    const int64_t from = t * a.st + h * a.sh, to = live ? slot_row(a, slot, h) * HATA_D : 0;
+    if (!second) {  // keys
+        uint4 x[2] = {*reinterpret_cast<const uint4*>(a.K_new + from + piece.at[0]), *reinterpret_cast<const uint4*>(a.K_new + from + piece.at[1])};
+        RotaryAngles(a.rot, p).rotate(a.rot, x, a.rot.positions[t]);
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            *reinterpret_cast<uint4*>(s_key + v * HATA_D + piece.at[i]) = x[i];
+            if (live && blockIdx.x == 0) *reinterpret_cast<uint4*>(a.K + to + piece.at[i]) = x[i];
+        }
+    } else if (live && blockIdx.x == 0) {
+#pragma unroll
+        for (int i = 0; i < 2; ++i) *reinterpret_cast<uint4*>(a.V + to + piece.at[i]) = *reinterpret_cast<const uint4*>(a.V_new + from + piece.at[i]);
+    }
+    if (!a.codes) return;
+    __syncthreads();
+    for (int v0 = 0; v0 < nv; v0 += 4) {
+        uint4 x[4];
+        hash_load_x(s_key + min(v0 + (tid & 3), nv - 1) * HATA_D, x);
+        hash_pass<COLS>(hw, x, s_codes, WPS, v0, nv);
+    }
+    __syncthreads();
+    for (int i = tid; i < nv * WPS; i += 256) {
+        const int to_slot = a.slots[t0 + i / WPS];
+        if (to_slot >= 0 && to_slot < a.rows) a.codes[slot_row(a, to_slot, h) * (a.r / 32) + blockIdx.x * WPS + i % WPS] = s_codes[i];
     }
 }
 
@@ -308,11 +367,13 @@ __global__ __launch_bounds__(256) void write_few_kernel(const WriteSlots a) {
 #define WRITE_ERROR 0x1p-16f
 #define WRITE_MAX_ROWS 1024  // of a workgroup
 #define WRITE_DOUBTS 512
-template <int R, bool F16>
+// ROTATE: a thread has a piece of a row instead (RotaryPiece: two parts of 16 bytes), and rotates the key between the load and its uses.
+template <int R, bool F16, bool ROTATE>
 __global__ __launch_bounds__(R <= 128 ? 256 : 512, 2) void write_mfma_kernel(const WriteSlots a, const uint4* __restrict__ planes, int rows_per_wg) {
     constexpr int COLW = R / 32, KP = R >= 128 ? 1 : 128 / R;  // waves by columns, by rows
     constexpr int THREADS = 64 * COLW * KP, NT = R >= 128 ? 2 : 1, STAGE = 32 * NT * KP, WD = R / 32;
-    constexpr int ROWS_PER_IT = THREADS / 16, NIT = STAGE / ROWS_PER_IT;
+    constexpr int PARTS = ROTATE ? 2 : 1, LANES = 16 / PARTS;  // of 16 bytes; threads of a row
+    constexpr int ROWS_PER_IT = THREADS / LANES, NIT = STAGE / ROWS_PER_IT;
     __shared__ __attribute__((aligned(16))) uint16_t tile[STAGE * HATA_MFMA_PITCH];
     __shared__ __attribute__((aligned(16))) uint32_t s_code[WRITE_MAX_ROWS * WD];
     __shared__ float s_norm[STAGE];
@@ -326,24 +387,38 @@ __global__ __launch_bounds__(R <= 128 ? 256 : 512, 2) void write_mfma_kernel(con
     const uint16_t* Kh = a.K_new + h * a.sh;
     const uint16_t* Vh = a.V_new + h * a.sh;
 
-    const int lrow = tid >> 4, lsub = tid & 15;
-    uint4 pre[NIT], vpre[NIT];
+    const int lrow = tid / LANES, lsub = tid % LANES;
+    int at[PARTS];  // first channels of this thread's parts
+    uint4 pre[NIT][PARTS], vpre[NIT][PARTS];
     int slot[NIT];
+    [[maybe_unused]] int position[NIT];
+    if constexpr (ROTATE) {
+        const RotaryPiece piece(lsub, a.rot.dims, a.rot.interleaved);
+        at[0] = piece.at[0];
+        at[1] = piece.at[1];
+    } else {
+        at[0] = lsub * 8;
+    }
     auto load_stage = [&](int t0) {
 #pragma unroll
         for (int it = 0; it < NIT; ++it) {
             const int t = t0 + it * ROWS_PER_IT + lrow;
             slot[it] = a.slots[min(t, last - 1)];
+            if constexpr (ROTATE) position[it] = a.rot.positions[min(t, last - 1)];
             if (t >= last) slot[it] = -1;
         }
 #pragma unroll
         for (int it = 0; it < NIT; ++it) {
-            const int64_t o = min(t0 + it * ROWS_PER_IT + lrow, last - 1) * a.st + lsub * 8;
-            pre[it] = load_once(Kh + o);
-            vpre[it] = load_once(Vh + o);
+            const int64_t o = min(t0 + it * ROWS_PER_IT + lrow, last - 1) * a.st;
+#pragma unroll
+            for (int p = 0; p < PARTS; ++p) {
+                pre[it][p] = load_once(Kh + o + at[p]);
+                vpre[it][p] = load_once(Vh + o + at[p]);
+            }
         }
     };
     load_stage(first);
+    [[maybe_unused]] const RotaryAngles angles(a.rot, ROTATE ? lsub : 0);
     if (tid == 0) s_doubts = s_wholes = 0;
     if (tid < WRITE_MAX_ROWS / 32) s_whole[tid] = 0;
 
@@ -390,15 +465,26 @@ __global__ __launch_bounds__(R <= 128 ? 256 : 512, 2) void write_mfma_kernel(con
 #pragma unroll
         for (int it = 0; it < NIT; ++it) {
             const int row = it * ROWS_PER_IT + lrow;
-            const uint4 x = pre[it];
-            *reinterpret_cast<uint4*>(&tile[row * HATA_MFMA_PITCH + lsub * 8]) = F16 ? __builtin_bit_cast(uint4, bf16x8_to_f16(x)) : x;
-            const float n2 = row_sum16(dot2_bf16(x.x, x.x, dot2_bf16(x.y, x.y, dot2_bf16(x.z, x.z, dot2_bf16(x.w, x.w, 0.f)))));
-            const float some = row_max16(((x.x | x.y | x.z | x.w) & 0x7fff7fffu) ? 1.f : 0.f);
+            if constexpr (ROTATE) angles.rotate(a.rot, pre[it], position[it]);
+            float n2 = 0.f;
+            uint32_t bits = 0;
+#pragma unroll
+            for (int p = 0; p < PARTS; ++p) {
+                const uint4 x = pre[it][p];
+                *reinterpret_cast<uint4*>(&tile[row * HATA_MFMA_PITCH + at[p]]) = F16 ? __builtin_bit_cast(uint4, bf16x8_to_f16(x)) : x;
+                n2 = dot2_bf16(x.x, x.x, dot2_bf16(x.y, x.y, dot2_bf16(x.z, x.z, dot2_bf16(x.w, x.w, n2))));
+                bits |= x.x | x.y | x.z | x.w;
+            }
+            n2 = ROTATE ? row_sum8(n2) : row_sum16(n2);
+            const float some = ROTATE ? row_max8((bits & 0x7fff7fffu) ? 1.f : 0.f) : row_max16((bits & 0x7fff7fffu) ? 1.f : 0.f);
             int to = -1;
             if (slot[it] >= 0 && slot[it] < a.rows) {
                 to = (int)slot_row(a, slot[it], h);
-                *reinterpret_cast<uint4*>(a.K + (int64_t)to * HATA_D + lsub * 8) = x;
-                *reinterpret_cast<uint4*>(a.V + (int64_t)to * HATA_D + lsub * 8) = vpre[it];
+#pragma unroll
+                for (int p = 0; p < PARTS; ++p) {
+                    *reinterpret_cast<uint4*>(a.K + (int64_t)to * HATA_D + at[p]) = pre[it][p];
+                    *reinterpret_cast<uint4*>(a.V + (int64_t)to * HATA_D + at[p]) = vpre[it][p];
+                }
             }
             if (lsub == 0) {
                 // (a row of zeros projects to zero, in any arithmetic that holds the weights, and so does a finite row where they are zeros)
@@ -468,6 +554,7 @@ __global__ __launch_bounds__(R <= 128 ? 256 : 512, 2) void write_mfma_kernel(con
             if (half == 0) s_code[(t0 - first + row) * WD + w] = word;
         }
     }
+    if constexpr (ROTATE) asm volatile("s_waitcnt vmcnt(0)" ::: "memory");  // keys that are read again
     __syncthreads();
     // Bits in doubt, sixteen a wave: hash_pass' instruction and its order of the channels, so that the sums round as they do there.  Its
     // four blocks take four columns and four vectors each, of which the diagonal is looked at: lane l has a part of item l % 16, and
@@ -476,7 +563,8 @@ __global__ __launch_bounds__(R <= 128 ? 256 : 512, 2) void write_mfma_kernel(con
         for (int i0 = 16 * wave; i0 < n; i0 += THREADS / 4) {
             const uint32_t item = item_of(min(i0 + (lane & 15), n - 1));
             uint4 x[4];
-            hash_load_x(Kh + (first + (int)(item / R)) * a.st, x);
+            if constexpr (ROTATE) hash_load_x(a.K + (int64_t)s_row[item / R] * HATA_D, x);  // (as it was written)
+            else hash_load_x(Kh + (first + (int)(item / R)) * a.st, x);
             const float* wc = a.W_H + ((int64_t)h * HATA_D + 32 * (lane >> 4)) * R + item % R;
             float wv[32];
 #pragma unroll
@@ -525,12 +613,31 @@ static int write_rows_per_wg(int n, int Hkv, int r) {
     return (int)per * 64;
 }
 
+static bool write_on_matrix_cores(const WriteSlots& a, int n_tokens) {
+    return a.codes && n_tokens > HATA_WRITE_FEW && (a.r == 32 || a.r == 64 || a.r == 128 || a.r == 256);
+}
+template <bool ROTATE>
+static hipError_t launch_write_mfma(const hata_ctx* c, const WriteSlots& a, hipStream_t s) {
+    // the weight planes prepared for exactly this weight tensor, if any
+    const uint4* planes = (c->prepared_W_H == a.W_H && c->wplanes) ? (const uint4*)c->wplanes : nullptr;
+    const int per = write_rows_per_wg(a.n, a.Hkv, a.r);
+    const dim3 grid((a.n + per - 1) / per, a.Hkv);
+#define HATA_LAUNCH_WRITE(R_) \
+    hipLaunchKernelGGL((planes ? write_mfma_kernel<R_, true, ROTATE> : write_mfma_kernel<R_, false, ROTATE>), grid, dim3(R_ <= 128 ? 256 : 512), 0, s, a, planes, per)
+    if (a.r == 32) HATA_LAUNCH_WRITE(32);
+    else if (a.r == 64) HATA_LAUNCH_WRITE(64);
+    else if (a.r == 128) HATA_LAUNCH_WRITE(128);
+    else HATA_LAUNCH_WRITE(256);
+#undef HATA_LAUNCH_WRITE
+    return hipGetLastError();
+}
+
 hipError_t launch_write_slots(const hata_ctx* c, const void* K_new, const void* V_new, int64_t stride_t, int64_t stride_h,
                               const int32_t* slots, int n_tokens, void* K_pool, void* V_pool, uint32_t* codes, int shift, int n_pages,
                               const float* W_H, hipStream_t s) {
     const hata_config& f = c->cfg;
     const WriteSlots all = {(const uint16_t*)K_new, (const uint16_t*)V_new, slots, (uint16_t*)K_pool, (uint16_t*)V_pool, codes, W_H,
-                            stride_t, stride_h, n_tokens, f.Hkv, f.r, shift, n_pages << shift, false};
+                            stride_t, stride_h, n_tokens, f.Hkv, f.r, shift, n_pages << shift, {}, nullptr, nullptr, 0, 0, 0};
     const int most = 65535 * WRITE_ROWS;  // rows of a launch
     for (int t0 = 0; t0 < n_tokens; t0 += most) {
         WriteSlots a = all;
@@ -538,19 +645,8 @@ hipError_t launch_write_slots(const hata_ctx* c, const void* K_new, const void* 
         a.V_new += t0 * stride_t;
         a.slots += t0;
         a.n = std::min(most, n_tokens - t0);
-        if (codes && n_tokens > HATA_WRITE_FEW && (f.r == 32 || f.r == 64 || f.r == 128 || f.r == 256)) {
-            // the weight planes prepared for exactly this weight tensor, if any
-            const uint4* planes = (c->prepared_W_H == W_H && c->wplanes) ? (const uint4*)c->wplanes : nullptr;
-            const int per = write_rows_per_wg(a.n, f.Hkv, f.r);
-            const dim3 grid((a.n + per - 1) / per, f.Hkv);
-#define HATA_LAUNCH_WRITE(R_) \
-    hipLaunchKernelGGL((planes ? write_mfma_kernel<R_, true> : write_mfma_kernel<R_, false>), grid, dim3(R_ <= 128 ? 256 : 512), 0, s, a, planes, per)
-            if (f.r == 32) HATA_LAUNCH_WRITE(32);
-            else if (f.r == 64) HATA_LAUNCH_WRITE(64);
-            else if (f.r == 128) HATA_LAUNCH_WRITE(128);
-            else HATA_LAUNCH_WRITE(256);
-#undef HATA_LAUNCH_WRITE
-            const hipError_t e = hipGetLastError();
+        if (write_on_matrix_cores(a, n_tokens)) {
+            const hipError_t e = launch_write_mfma<false>(c, a, s);
             if (e != hipSuccess) return e;
             if (n_tokens - t0 <= most) break;
             continue;
@@ -565,21 +661,42 @@ hipError_t launch_write_slots(const hata_ctx* c, const void* K_new, const void* 
     return hipSuccess;
 }
 
-hipError_t launch_slot_codes(const hata_ctx* c, const int32_t* slots, int n_tokens, const void* K_pool, uint32_t* codes, int shift,
-                             int n_pages, const float* W_H, hipStream_t s) {
+// With rotation: few rows in one launch; many without codes in that of hata_rotate; many with codes the queries there, keys and values on the
+// matrix cores
+hipError_t launch_rotate_write(const hata_ctx* c, const RotateRows& rows, uint32_t* codes, const float* W_H, hipStream_t s) {
     const hata_config& f = c->cfg;
-    const int most = 65535 * WRITE_ROWS, cols = f.r % 64 == 0 ? 64 : 32;
-    for (int t0 = 0; t0 < n_tokens;) {
-        const int n = std::min(most, n_tokens - t0);
-        const WriteSlots a = {nullptr, nullptr, slots + t0, (uint16_t*)K_pool, nullptr, codes, W_H, 0, 0, n, f.Hkv, f.r, shift, n_pages << shift, true};
-        hipLaunchKernelGGL((cols == 64 ? write_few_kernel<64> : write_few_kernel<32>), dim3(f.r / cols, f.Hkv, (n + WRITE_ROWS - 1) / WRITE_ROWS),
-                           dim3(256), 0, s, a);
-        const hipError_t e = hipGetLastError();
+    const WriteSlots all = {rows.K_new, rows.V_new, rows.slots, rows.K, rows.V, codes, W_H, rows.kv_st, rows.kv_sh, rows.n, f.Hkv, f.r, rows.shift,
+                            rows.rows, {rows.freq, rows.positions, rows.magnitude, rows.dims, rows.interleaved}, rows.x, rows.out, rows.st, rows.sh, c->G};
+    if (!codes) return launch_rotate(rows, s);
+    const bool many = write_on_matrix_cores(all, rows.n);
+    if (many && rows.heads) {
+        RotateRows q = rows;
+        q.Hkv = 0;
+        const hipError_t e = launch_rotate(q, s);
         if (e != hipSuccess) return e;
-        if (n_tokens - t0 <= most) break;
-        t0 += most;
     }
-    return hipSuccess;
+    const int most = 65535 * WRITE_ROWS;  // rows of a launch
+    for (int t0 = 0;; t0 += most) {
+        WriteSlots a = all;
+        a.K_new += t0 * rows.kv_st;
+        a.V_new += t0 * rows.kv_st;
+        a.q += t0 * rows.st;
+        a.q_out += t0 * rows.out_st;
+        a.slots += t0;
+        a.rot.positions += t0;
+        a.n = std::min(most, rows.n - t0);
+        hipError_t e;
+        if (many) {
+            e = launch_write_mfma<true>(c, a, s);
+        } else {
+            const int cols = f.r % 64 == 0 ? 64 : 32;
+            hipLaunchKernelGGL((cols == 64 ? rotate_write_few_kernel<64> : rotate_write_few_kernel<32>),
+                               dim3(f.r / cols + (rows.heads ? 1 : 0), f.Hkv, (a.n + WRITE_ROWS - 1) / WRITE_ROWS), dim3(256), 0, s, a);
+            e = hipGetLastError();
+        }
+        if (e != hipSuccess) return e;
+        if (rows.n - t0 <= most) return hipSuccess;  // (t0 stays below 2^31)
+    }
 }
 
 }  // namespace hata

@@ -58,6 +58,13 @@ __device__ __forceinline__ uint32_t bf16_pair(double lo, double hi) {
     return __builtin_bit_cast(uint32_t, __builtin_convertvector(f, bf16x2));
 }
 
+struct RotaryArgs {
+    const double* freq;
+    const int32_t* positions;
+    double magnitude;
+    int dims, interleaved;
+};
+
 // A row goes in eight pieces of 32 bytes.  Piece p < dims / 16 holds pairs 8 p .. 8 p + 7, as two 16-byte parts: with halves the first
 // channels of those pairs and the second ones, with neighbours one behind the other.  The other pieces hold channels 16 p .. 16 p + 15.
 struct RotaryPiece {
@@ -88,5 +95,27 @@ __device__ __forceinline__ void rotate_piece(uint4 (&x)[2], const double (&c)[8]
         }
     }
 }
+
+// The piece's frequencies, and a row's angles from them
+struct RotaryAngles {
+    double f[8];
+    bool turns;  // the piece's channels are rotated at all
+    __device__ __forceinline__ RotaryAngles(const RotaryArgs& a, int p) {
+        turns = 16 * p < a.dims;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) f[i] = a.freq[min(8 * p + i, a.dims / 2 - 1)];
+    }
+    __device__ __forceinline__ void rotate(const RotaryArgs& a, uint4 (&x)[2], int position) const {
+        if (!turns) return;
+        double c[8], s[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            cos_sin((double)position * f[i], c[i], s[i]);
+            c[i] *= a.magnitude;
+            s[i] *= a.magnitude;
+        }
+        rotate_piece(x, c, s, a.interleaved);
+    }
+};
 
 }  // namespace hata
