@@ -389,7 +389,8 @@ __global__ __launch_bounds__(R <= 128 ? 256 : 512, 2) void write_mfma_kernel(con
 
     const int lrow = tid / LANES, lsub = tid % LANES;
     int at[PARTS];  // first channels of this thread's parts
-    uint4 pre[NIT][PARTS], vpre[NIT][PARTS];
+    uint4 pre[NIT][PARTS];
+    [[maybe_unused]] uint4 vpre[NIT][PARTS];
     int slot[NIT];
     [[maybe_unused]] int position[NIT];
     if constexpr (ROTATE) {
@@ -413,7 +414,7 @@ __global__ __launch_bounds__(R <= 128 ? 256 : 512, 2) void write_mfma_kernel(con
 #pragma unroll
             for (int p = 0; p < PARTS; ++p) {
                 pre[it][p] = load_once(Kh + o + at[p]);
-                vpre[it][p] = load_once(Vh + o + at[p]);
+                if constexpr (!ROTATE) vpre[it][p] = load_once(Vh + o + at[p]);
             }
         }
     };
@@ -461,16 +462,35 @@ __global__ __launch_bounds__(R <= 128 ? 256 : 512, 2) void write_mfma_kernel(con
     const float wn = no_w ? 0.f : doubt || norm2 < 0x1p-80f ? __builtin_huge_valf() : sqrtf(norm2);
 
     for (int t0 = first; t0 < last; t0 += STAGE) {
+        [[maybe_unused]] int slot_now[NIT];
+        [[maybe_unused]] uint4 now[NIT][PARTS];
+        if constexpr (ROTATE) {  // (the next stage's requests ahead of the angles)
+            uint4 x[NIT][PARTS];
+            int at_position[NIT];
+#pragma unroll
+            for (int it = 0; it < NIT; ++it) {
+#pragma unroll
+                for (int p = 0; p < PARTS; ++p) x[it][p] = pre[it][p];
+                at_position[it] = position[it];
+                slot_now[it] = slot[it];
+            }
+            if (t0 + STAGE < last) load_stage(t0 + STAGE);
+#pragma unroll
+            for (int it = 0; it < NIT; ++it) {
+                angles.rotate(a.rot, x[it], at_position[it]);
+#pragma unroll
+                for (int p = 0; p < PARTS; ++p) now[it][p] = x[it][p];
+            }
+        }
         __syncthreads();  // the previous stage has been consumed
 #pragma unroll
         for (int it = 0; it < NIT; ++it) {
             const int row = it * ROWS_PER_IT + lrow;
-            if constexpr (ROTATE) angles.rotate(a.rot, pre[it], position[it]);
             float n2 = 0.f;
             uint32_t bits = 0;
 #pragma unroll
             for (int p = 0; p < PARTS; ++p) {
-                const uint4 x = pre[it][p];
+                const uint4 x = ROTATE ? now[it][p] : pre[it][p];
                 *reinterpret_cast<uint4*>(&tile[row * HATA_MFMA_PITCH + at[p]]) = F16 ? __builtin_bit_cast(uint4, bf16x8_to_f16(x)) : x;
                 n2 = dot2_bf16(x.x, x.x, dot2_bf16(x.y, x.y, dot2_bf16(x.z, x.z, dot2_bf16(x.w, x.w, n2))));
                 bits |= x.x | x.y | x.z | x.w;
@@ -478,12 +498,12 @@ __global__ __launch_bounds__(R <= 128 ? 256 : 512, 2) void write_mfma_kernel(con
             n2 = ROTATE ? row_sum8(n2) : row_sum16(n2);
             const float some = ROTATE ? row_max8((bits & 0x7fff7fffu) ? 1.f : 0.f) : row_max16((bits & 0x7fff7fffu) ? 1.f : 0.f);
             int to = -1;
-            if (slot[it] >= 0 && slot[it] < a.rows) {
-                to = (int)slot_row(a, slot[it], h);
+            if ((ROTATE ? slot_now[it] : slot[it]) >= 0 && (ROTATE ? slot_now[it] : slot[it]) < a.rows) {
+                to = (int)slot_row(a, (ROTATE ? slot_now[it] : slot[it]), h);
 #pragma unroll
                 for (int p = 0; p < PARTS; ++p) {
-                    *reinterpret_cast<uint4*>(a.K + (int64_t)to * HATA_D + at[p]) = pre[it][p];
-                    *reinterpret_cast<uint4*>(a.V + (int64_t)to * HATA_D + at[p]) = vpre[it][p];
+                    *reinterpret_cast<uint4*>(a.K + (int64_t)to * HATA_D + at[p]) = ROTATE ? now[it][p] : pre[it][p];
+                    if constexpr (!ROTATE) *reinterpret_cast<uint4*>(a.V + (int64_t)to * HATA_D + at[p]) = vpre[it][p];
                 }
             }
             if (lsub == 0) {
@@ -494,7 +514,9 @@ __global__ __launch_bounds__(R <= 128 ? 256 : 512, 2) void write_mfma_kernel(con
             }
         }
         __syncthreads();
-        if (t0 + STAGE < last) load_stage(t0 + STAGE);  // overlaps the products below
+        if constexpr (!ROTATE) {
+            if (t0 + STAGE < last) load_stage(t0 + STAGE);  // overlaps the products below
+        }
 
         f32x16_t acc[NT];
 #pragma unroll
@@ -661,18 +683,18 @@ hipError_t launch_write_slots(const hata_ctx* c, const void* K_new, const void* 
     return hipSuccess;
 }
 
-// With rotation: few rows in one launch; many without codes in that of hata_rotate; many with codes the queries there, keys and values on the
-// matrix cores
+// With rotation: few rows in one launch; without codes in that of hata_rotate; many with codes the queries and values there, the keys
+// on the matrix cores
 hipError_t launch_rotate_write(const hata_ctx* c, const RotateRows& rows, uint32_t* codes, const float* W_H, hipStream_t s) {
     const hata_config& f = c->cfg;
     const WriteSlots all = {rows.K_new, rows.V_new, rows.slots, rows.K, rows.V, codes, W_H, rows.kv_st, rows.kv_sh, rows.n, f.Hkv, f.r, rows.shift,
                             rows.rows, {rows.freq, rows.positions, rows.magnitude, rows.dims, rows.interleaved}, rows.x, rows.out, rows.st, rows.sh, c->G};
     if (!codes) return launch_rotate(rows, s);
     const bool many = write_on_matrix_cores(all, rows.n);
-    if (many && rows.heads) {
-        RotateRows q = rows;
-        q.Hkv = 0;
-        const hipError_t e = launch_rotate(q, s);
+    if (many) {
+        RotateRows others = rows;
+        others.no_keys = 1;
+        const hipError_t e = launch_rotate(others, s);
         if (e != hipSuccess) return e;
     }
     const int most = 65535 * WRITE_ROWS;  // rows of a launch

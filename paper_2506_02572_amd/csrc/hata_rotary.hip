@@ -2,21 +2,53 @@
 // hata_rotate_write_slots).
 #include <math.h>
 #include <algorithm>
+#include "hata_encode_core.h"
 #include "hata_internal.h"
 #include "hata_rotary.h"
 
 namespace hata {
 
 // A wave has a packed row and `per` of its heads, eight at a time: lane = (head % 8, piece of 32 bytes).  The angles of the
-// row's pairs, one a lane, pass through LDS.
+// row's pairs, one a lane, pass through LDS.  Bound by the bytes, 256 read and written a row and head: the requests of ROTATE_BATCH
+// times eight heads are outstanding together.
 #define ROTATE_WAVES 4
+#define ROTATE_BATCH 3
 
 __global__ __launch_bounds__(64 * ROTATE_WAVES) void rotate_kernel(const RotateRows a) {
     __shared__ double s_cos[ROTATE_WAVES][HATA_D / 2], s_sin[ROTATE_WAVES][HATA_D / 2];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const bool row = (int)blockIdx.x * ROTATE_WAVES + wave < a.n;
-    const int t = row ? blockIdx.x * ROTATE_WAVES + wave : a.n - 1;
-    const int pairs = a.dims / 2, heads = a.heads + 2 * a.Hkv;
+    const int t = min((int)blockIdx.x * ROTATE_WAVES + wave, a.n - 1), p = lane & 7;
+    const RotaryPiece piece(p, a.dims, a.interleaved);
+    const int slot = a.Hkv ? a.slots[t] : -1;
+    // heads: the queries, the keys (unless they go elsewhere), the values; the last ones only where the row has a slot
+    const int keys = a.no_keys ? 0 : a.Hkv;
+    int h_end = slot >= 0 && slot < a.rows ? a.heads + keys + a.Hkv : a.heads;
+    if ((int)blockIdx.x * ROTATE_WAVES + wave >= a.n) h_end = 0;
+    h_end = min(h_end, (int)(blockIdx.y + 1) * a.per);
+    const uint16_t *x_row = a.x + t * a.st, *k_row = a.K_new + t * a.kv_st, *v_row = a.V_new + t * a.kv_st;
+    uint16_t* out_row = a.out + t * a.out_st;
+    const int64_t kv_at = ((((int64_t)(slot >> a.shift) * a.Hkv) << a.shift) + (slot & ((1 << a.shift) - 1))) * HATA_D;
+    auto source = [&](int h) {
+        return h < a.heads ? x_row + h * a.sh : h < a.heads + keys ? k_row + (h - a.heads) * a.kv_sh : v_row + (h - a.heads - keys) * a.kv_sh;
+    };
+    auto target = [&](int h) {
+        return h < a.heads ? out_row + h * a.out_sh
+               : h < a.heads + keys ? a.K + kv_at + ((int64_t)(h - a.heads) << a.shift) * HATA_D
+                                    : a.V + kv_at + ((int64_t)(h - a.heads - keys) << a.shift) * HATA_D;
+    };
+    uint4 x[ROTATE_BATCH][2];
+    auto load = [&](int h0) {
+#pragma unroll
+        for (int j = 0; j < ROTATE_BATCH; ++j)
+            if (h0 + 8 * j < h_end) {
+                const uint16_t* from = source(h0 + 8 * j);
+#pragma unroll
+                for (int i = 0; i < 2; ++i) x[j][i] = load_once(from + piece.at[i]);
+            }
+    };
+    const int first = blockIdx.y * a.per + (lane >> 3);
+    load(first);
+    const int pairs = a.dims / 2;
     if (lane < pairs) {
         double c, s;
         cos_sin((double)a.positions[t] * a.freq[lane], c, s);
@@ -24,36 +56,30 @@ __global__ __launch_bounds__(64 * ROTATE_WAVES) void rotate_kernel(const RotateR
         s_sin[wave][lane] = (a.back ? -s : s) * a.magnitude;
     }
     __syncthreads();
-    const int p = lane & 7;
     double c[8], s[8];
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
         c[i] = s_cos[wave][min(8 * p + i, pairs - 1)];
         s[i] = s_sin[wave][min(8 * p + i, pairs - 1)];
     }
-    const RotaryPiece piece(p, a.dims, a.interleaved);
-    const int slot = a.Hkv ? a.slots[t] : -1;
-    const bool live = slot >= 0 && slot < a.rows;
-    const int h_end = row ? min(heads, (int)(blockIdx.y + 1) * a.per) : 0;
-    for (int h = blockIdx.y * a.per + (lane >> 3); h < h_end; h += 8) {
-        const int kv = (h - a.heads) % max(a.Hkv, 1);
-        const bool is_q = h < a.heads, is_k = !is_q && h < a.heads + a.Hkv;
-        if (!is_q && !live) continue;
-        const uint16_t* from = is_q ? a.x + t * a.st + h * a.sh : (is_k ? a.K_new : a.V_new) + t * a.kv_st + kv * a.kv_sh;
-        uint16_t* to = is_q ? a.out + t * a.out_st + h * a.out_sh
-                            : (is_k ? a.K : a.V) + ((((int64_t)(slot >> a.shift) * a.Hkv + kv) << a.shift) + (slot & ((1 << a.shift) - 1))) * HATA_D;
-        uint4 x[2];
+    for (int h0 = first; h0 < h_end; h0 += 8 * ROTATE_BATCH) {
 #pragma unroll
-        for (int i = 0; i < 2; ++i) x[i] = *reinterpret_cast<const uint4*>(from + piece.at[i]);
-        if ((is_q || is_k) && 16 * p < a.dims) rotate_piece(x, c, s, a.interleaved);
+        for (int j = 0; j < ROTATE_BATCH; ++j) {
+            const int h = h0 + 8 * j;
+            if (h < h_end) {
+                if (h < a.heads + keys && 16 * p < a.dims) rotate_piece(x[j], c, s, a.interleaved);
+                uint16_t* to = target(h);
 #pragma unroll
-        for (int i = 0; i < 2; ++i) *reinterpret_cast<uint4*>(to + piece.at[i]) = x[i];
+                for (int i = 0; i < 2; ++i) *reinterpret_cast<uint4*>(to + piece.at[i]) = x[j][i];
+            }
+        }
+        load(h0 + 8 * ROTATE_BATCH);
     }
 }
 
 hipError_t launch_rotate(const RotateRows& all, hipStream_t s) {
     const int most = 1 << 20;  // rows of a launch
-    const int heads = all.heads + 2 * all.Hkv;
+    const int heads = all.heads + (all.no_keys ? 1 : 2) * all.Hkv;
     for (int t0 = 0; t0 < all.n;) {
         RotateRows a = all;
         a.n = std::min(most, all.n - t0);
@@ -63,7 +89,8 @@ hipError_t launch_rotate(const RotateRows& all, hipStream_t s) {
         a.V_new += t0 * all.kv_st;
         a.positions += t0;
         if (all.slots) a.slots += t0;
-        a.per = 8;
+        // all heads by one wave, unless the rows are so few that the waves are
+        a.per = a.n >= 2048 ? (heads + 7) / 8 * 8 : 8;
         hipLaunchKernelGGL(rotate_kernel, dim3((a.n + ROTATE_WAVES - 1) / ROTATE_WAVES, (heads + a.per - 1) / a.per), dim3(64 * ROTATE_WAVES), 0, s, a);
         const hipError_t e = hipGetLastError();
         if (e != hipSuccess) return e;
