@@ -62,16 +62,6 @@ __device__ __forceinline__ float row_sum16(float v) {
     v += HATA_DPP(v, 0x140);  // row_mirror
     return v;
 }
-__device__ __forceinline__ float row_sum8(float v) {  // over half a row
-    v += HATA_DPP(v, 0xB1);
-    v += HATA_DPP(v, 0x4E);
-    return v + HATA_DPP(v, 0x141);
-}
-__device__ __forceinline__ float row_max8(float v) {
-    v = fmaxf(v, HATA_DPP(v, 0xB1));
-    v = fmaxf(v, HATA_DPP(v, 0x4E));
-    return fmaxf(v, HATA_DPP(v, 0x141));
-}
 // (written as inline asm: the instruction rewrites BOTH of its registers, and the compiler
 // builtin of this toolchain returns the first register for both results; the s_nop cover the
 // VALU-write -> lane-swap read hazard the compiler would otherwise handle)

@@ -138,7 +138,6 @@ struct RotateRows {
     int64_t st, sh, out_st, out_sh, kv_st, kv_sh;  // strides in elements
     double magnitude;
     int n, heads, Hkv, dims, interleaved, back, shift, rows, per;  // rows: of one head in the pools; per: heads of a wave
-    int no_keys;  // the values alone go into the slots
 };
 hipError_t launch_rotate(const RotateRows& a, hipStream_t s);
 hipError_t launch_rotate_write(const hata_ctx* c, const RotateRows& rows, uint32_t* codes, const float* W_H, hipStream_t s);

@@ -367,13 +367,12 @@ __global__ __launch_bounds__(256) void rotate_write_few_kernel(const WriteSlots 
 #define WRITE_ERROR 0x1p-16f
 #define WRITE_MAX_ROWS 1024  // of a workgroup
 #define WRITE_DOUBTS 512
-// ROTATE: a thread has a piece of a row instead (RotaryPiece: two parts of 16 bytes), and rotates the key between the load and its uses.
-template <int R, bool F16, bool ROTATE>
+// HELD: the rows lie in their slots already (rotated, by the launch before: read from the caches), and their codes alone are wanted.
+template <int R, bool F16, bool HELD>
 __global__ __launch_bounds__(R <= 128 ? 256 : 512, 2) void write_mfma_kernel(const WriteSlots a, const uint4* __restrict__ planes, int rows_per_wg) {
     constexpr int COLW = R / 32, KP = R >= 128 ? 1 : 128 / R;  // waves by columns, by rows
     constexpr int THREADS = 64 * COLW * KP, NT = R >= 128 ? 2 : 1, STAGE = 32 * NT * KP, WD = R / 32;
-    constexpr int PARTS = ROTATE ? 2 : 1, LANES = 16 / PARTS;  // of 16 bytes; threads of a row
-    constexpr int ROWS_PER_IT = THREADS / LANES, NIT = STAGE / ROWS_PER_IT;
+    constexpr int ROWS_PER_IT = THREADS / 16, NIT = STAGE / ROWS_PER_IT;
     __shared__ __attribute__((aligned(16))) uint16_t tile[STAGE * HATA_MFMA_PITCH];
     __shared__ __attribute__((aligned(16))) uint32_t s_code[WRITE_MAX_ROWS * WD];
     __shared__ float s_norm[STAGE];
@@ -387,39 +386,44 @@ __global__ __launch_bounds__(R <= 128 ? 256 : 512, 2) void write_mfma_kernel(con
     const uint16_t* Kh = a.K_new + h * a.sh;
     const uint16_t* Vh = a.V_new + h * a.sh;
 
-    const int lrow = tid / LANES, lsub = tid % LANES;
-    int at[PARTS];  // first channels of this thread's parts
-    uint4 pre[NIT][PARTS];
-    [[maybe_unused]] uint4 vpre[NIT][PARTS];
+    const int lrow = tid >> 4, lsub = tid & 15;
+    uint4 pre[NIT];
+    [[maybe_unused]] uint4 vpre[NIT];
     int slot[NIT];
-    [[maybe_unused]] int position[NIT];
-    if constexpr (ROTATE) {
-        const RotaryPiece piece(lsub, a.rot.dims, a.rot.interleaved);
-        at[0] = piece.at[0];
-        at[1] = piece.at[1];
-    } else {
-        at[0] = lsub * 8;
-    }
+    [[maybe_unused]] int slot_next[NIT];  // HELD: of the stage behind the one requested
+    [[maybe_unused]] auto load_slots = [&](int t0) {
+#pragma unroll
+        for (int it = 0; it < NIT; ++it) {
+            const int t = t0 + it * ROWS_PER_IT + lrow;
+            slot_next[it] = a.slots[min(t, last - 1)];
+            if (t >= last) slot_next[it] = -1;
+        }
+    };
     auto load_stage = [&](int t0) {
+        if constexpr (HELD) {
+#pragma unroll
+            for (int it = 0; it < NIT; ++it) {
+                slot[it] = slot_next[it];
+                pre[it] = *reinterpret_cast<const uint4*>(a.K + slot_row(a, clampi(slot[it], 0, a.rows - 1), h) * HATA_D + lsub * 8);
+            }
+            load_slots(t0 + STAGE);
+            return;
+        }
 #pragma unroll
         for (int it = 0; it < NIT; ++it) {
             const int t = t0 + it * ROWS_PER_IT + lrow;
             slot[it] = a.slots[min(t, last - 1)];
-            if constexpr (ROTATE) position[it] = a.rot.positions[min(t, last - 1)];
             if (t >= last) slot[it] = -1;
         }
 #pragma unroll
         for (int it = 0; it < NIT; ++it) {
-            const int64_t o = min(t0 + it * ROWS_PER_IT + lrow, last - 1) * a.st;
-#pragma unroll
-            for (int p = 0; p < PARTS; ++p) {
-                pre[it][p] = load_once(Kh + o + at[p]);
-                if constexpr (!ROTATE) vpre[it][p] = load_once(Vh + o + at[p]);
-            }
+            const int64_t o = min(t0 + it * ROWS_PER_IT + lrow, last - 1) * a.st + lsub * 8;
+            pre[it] = load_once(Kh + o);
+            vpre[it] = load_once(Vh + o);
         }
     };
+    if constexpr (HELD) load_slots(first);
     load_stage(first);
-    [[maybe_unused]] const RotaryAngles angles(a.rot, ROTATE ? lsub : 0);
     if (tid == 0) s_doubts = s_wholes = 0;
     if (tid < WRITE_MAX_ROWS / 32) s_whole[tid] = 0;
 
@@ -462,48 +466,20 @@ __global__ __launch_bounds__(R <= 128 ? 256 : 512, 2) void write_mfma_kernel(con
     const float wn = no_w ? 0.f : doubt || norm2 < 0x1p-80f ? __builtin_huge_valf() : sqrtf(norm2);
 
     for (int t0 = first; t0 < last; t0 += STAGE) {
-        [[maybe_unused]] int slot_now[NIT];
-        [[maybe_unused]] uint4 now[NIT][PARTS];
-        if constexpr (ROTATE) {  // (the next stage's requests ahead of the angles)
-            uint4 x[NIT][PARTS];
-            int at_position[NIT];
-#pragma unroll
-            for (int it = 0; it < NIT; ++it) {
-#pragma unroll
-                for (int p = 0; p < PARTS; ++p) x[it][p] = pre[it][p];
-                at_position[it] = position[it];
-                slot_now[it] = slot[it];
-            }
-            if (t0 + STAGE < last) load_stage(t0 + STAGE);
-#pragma unroll
-            for (int it = 0; it < NIT; ++it) {
-                angles.rotate(a.rot, x[it], at_position[it]);
-#pragma unroll
-                for (int p = 0; p < PARTS; ++p) now[it][p] = x[it][p];
-            }
-        }
         __syncthreads();  // the previous stage has been consumed
 #pragma unroll
         for (int it = 0; it < NIT; ++it) {
             const int row = it * ROWS_PER_IT + lrow;
-            float n2 = 0.f;
-            uint32_t bits = 0;
-#pragma unroll
-            for (int p = 0; p < PARTS; ++p) {
-                const uint4 x = ROTATE ? now[it][p] : pre[it][p];
-                *reinterpret_cast<uint4*>(&tile[row * HATA_MFMA_PITCH + at[p]]) = F16 ? __builtin_bit_cast(uint4, bf16x8_to_f16(x)) : x;
-                n2 = dot2_bf16(x.x, x.x, dot2_bf16(x.y, x.y, dot2_bf16(x.z, x.z, dot2_bf16(x.w, x.w, n2))));
-                bits |= x.x | x.y | x.z | x.w;
-            }
-            n2 = ROTATE ? row_sum8(n2) : row_sum16(n2);
-            const float some = ROTATE ? row_max8((bits & 0x7fff7fffu) ? 1.f : 0.f) : row_max16((bits & 0x7fff7fffu) ? 1.f : 0.f);
+            const uint4 x = pre[it];
+            *reinterpret_cast<uint4*>(&tile[row * HATA_MFMA_PITCH + lsub * 8]) = F16 ? __builtin_bit_cast(uint4, bf16x8_to_f16(x)) : x;
+            const float n2 = row_sum16(dot2_bf16(x.x, x.x, dot2_bf16(x.y, x.y, dot2_bf16(x.z, x.z, dot2_bf16(x.w, x.w, 0.f)))));
+            const float some = row_max16(((x.x | x.y | x.z | x.w) & 0x7fff7fffu) ? 1.f : 0.f);
             int to = -1;
-            if ((ROTATE ? slot_now[it] : slot[it]) >= 0 && (ROTATE ? slot_now[it] : slot[it]) < a.rows) {
-                to = (int)slot_row(a, (ROTATE ? slot_now[it] : slot[it]), h);
-#pragma unroll
-                for (int p = 0; p < PARTS; ++p) {
-                    *reinterpret_cast<uint4*>(a.K + (int64_t)to * HATA_D + at[p]) = ROTATE ? now[it][p] : pre[it][p];
-                    if constexpr (!ROTATE) *reinterpret_cast<uint4*>(a.V + (int64_t)to * HATA_D + at[p]) = vpre[it][p];
+            if (slot[it] >= 0 && slot[it] < a.rows) {
+                to = (int)slot_row(a, slot[it], h);
+                if constexpr (!HELD) {
+                    *reinterpret_cast<uint4*>(a.K + (int64_t)to * HATA_D + lsub * 8) = x;
+                    *reinterpret_cast<uint4*>(a.V + (int64_t)to * HATA_D + lsub * 8) = vpre[it];
                 }
             }
             if (lsub == 0) {
@@ -514,9 +490,7 @@ __global__ __launch_bounds__(R <= 128 ? 256 : 512, 2) void write_mfma_kernel(con
             }
         }
         __syncthreads();
-        if constexpr (!ROTATE) {
-            if (t0 + STAGE < last) load_stage(t0 + STAGE);  // overlaps the products below
-        }
+        if (t0 + STAGE < last) load_stage(t0 + STAGE);  // overlaps the products below
 
         f32x16_t acc[NT];
 #pragma unroll
@@ -576,7 +550,6 @@ __global__ __launch_bounds__(R <= 128 ? 256 : 512, 2) void write_mfma_kernel(con
             if (half == 0) s_code[(t0 - first + row) * WD + w] = word;
         }
     }
-    if constexpr (ROTATE) asm volatile("s_waitcnt vmcnt(0)" ::: "memory");  // keys that are read again
     __syncthreads();
     // Bits in doubt, sixteen a wave: hash_pass' instruction and its order of the channels, so that the sums round as they do there.  Its
     // four blocks take four columns and four vectors each, of which the diagonal is looked at: lane l has a part of item l % 16, and
@@ -585,7 +558,7 @@ __global__ __launch_bounds__(R <= 128 ? 256 : 512, 2) void write_mfma_kernel(con
         for (int i0 = 16 * wave; i0 < n; i0 += THREADS / 4) {
             const uint32_t item = item_of(min(i0 + (lane & 15), n - 1));
             uint4 x[4];
-            if constexpr (ROTATE) hash_load_x(a.K + (int64_t)s_row[item / R] * HATA_D, x);  // (as it was written)
+            if constexpr (HELD) hash_load_x(a.K + (int64_t)s_row[item / R] * HATA_D, x);
             else hash_load_x(Kh + (first + (int)(item / R)) * a.st, x);
             const float* wc = a.W_H + ((int64_t)h * HATA_D + 32 * (lane >> 4)) * R + item % R;
             float wv[32];
@@ -638,14 +611,14 @@ static int write_rows_per_wg(int n, int Hkv, int r) {
 static bool write_on_matrix_cores(const WriteSlots& a, int n_tokens) {
     return a.codes && n_tokens > HATA_WRITE_FEW && (a.r == 32 || a.r == 64 || a.r == 128 || a.r == 256);
 }
-template <bool ROTATE>
+template <bool HELD>
 static hipError_t launch_write_mfma(const hata_ctx* c, const WriteSlots& a, hipStream_t s) {
     // the weight planes prepared for exactly this weight tensor, if any
     const uint4* planes = (c->prepared_W_H == a.W_H && c->wplanes) ? (const uint4*)c->wplanes : nullptr;
     const int per = write_rows_per_wg(a.n, a.Hkv, a.r);
     const dim3 grid((a.n + per - 1) / per, a.Hkv);
 #define HATA_LAUNCH_WRITE(R_) \
-    hipLaunchKernelGGL((planes ? write_mfma_kernel<R_, true, ROTATE> : write_mfma_kernel<R_, false, ROTATE>), grid, dim3(R_ <= 128 ? 256 : 512), 0, s, a, planes, per)
+    hipLaunchKernelGGL((planes ? write_mfma_kernel<R_, true, HELD> : write_mfma_kernel<R_, false, HELD>), grid, dim3(R_ <= 128 ? 256 : 512), 0, s, a, planes, per)
     if (a.r == 32) HATA_LAUNCH_WRITE(32);
     else if (a.r == 64) HATA_LAUNCH_WRITE(64);
     else if (a.r == 128) HATA_LAUNCH_WRITE(128);
@@ -683,8 +656,9 @@ hipError_t launch_write_slots(const hata_ctx* c, const void* K_new, const void* 
     return hipSuccess;
 }
 
-// With rotation: few rows in one launch; without codes in that of hata_rotate; many with codes the queries and values there, the keys
-// on the matrix cores
+// With rotation: few rows in one launch; without codes in that of hata_rotate; many with codes there, and the codes behind it from the
+// slots.  (Rotated between load and products, a key's angles are worked out once for every KV head, 1700 instructions of the
+// vector ALU for 64 rows and wave: 16411 rows, eight heads, with 32 of queries 113 us; 8192 rows of 32 heads, r = 256, 157.)
 hipError_t launch_rotate_write(const hata_ctx* c, const RotateRows& rows, uint32_t* codes, const float* W_H, hipStream_t s) {
     const hata_config& f = c->cfg;
     const WriteSlots all = {rows.K_new, rows.V_new, rows.slots, rows.K, rows.V, codes, W_H, rows.kv_st, rows.kv_sh, rows.n, f.Hkv, f.r, rows.shift,
@@ -692,9 +666,7 @@ hipError_t launch_rotate_write(const hata_ctx* c, const RotateRows& rows, uint32
     if (!codes) return launch_rotate(rows, s);
     const bool many = write_on_matrix_cores(all, rows.n);
     if (many) {
-        RotateRows others = rows;
-        others.no_keys = 1;
-        const hipError_t e = launch_rotate(others, s);
+        const hipError_t e = launch_rotate(rows, s);
         if (e != hipSuccess) return e;
     }
     const int most = 65535 * WRITE_ROWS;  // rows of a launch

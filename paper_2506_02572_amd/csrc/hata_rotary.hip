@@ -20,9 +20,9 @@ __global__ __launch_bounds__(64 * ROTATE_WAVES) void rotate_kernel(const RotateR
     const int t = min((int)blockIdx.x * ROTATE_WAVES + wave, a.n - 1), p = lane & 7;
     const RotaryPiece piece(p, a.dims, a.interleaved);
     const int slot = a.Hkv ? a.slots[t] : -1;
-    // heads: the queries, the keys (unless they go elsewhere), the values; the last ones only where the row has a slot
-    const int keys = a.no_keys ? 0 : a.Hkv;
-    int h_end = slot >= 0 && slot < a.rows ? a.heads + keys + a.Hkv : a.heads;
+    // heads: the queries, the keys, the values; the last ones only where the row has a slot
+    const int keys = a.Hkv;
+    int h_end = slot >= 0 && slot < a.rows ? a.heads + 2 * keys : a.heads;
     if ((int)blockIdx.x * ROTATE_WAVES + wave >= a.n) h_end = 0;
     h_end = min(h_end, (int)(blockIdx.y + 1) * a.per);
     const uint16_t *x_row = a.x + t * a.st, *k_row = a.K_new + t * a.kv_st, *v_row = a.V_new + t * a.kv_st;
@@ -79,7 +79,7 @@ __global__ __launch_bounds__(64 * ROTATE_WAVES) void rotate_kernel(const RotateR
 
 hipError_t launch_rotate(const RotateRows& all, hipStream_t s) {
     const int most = 1 << 20;  // rows of a launch
-    const int heads = all.heads + (all.no_keys ? 1 : 2) * all.Hkv;
+    const int heads = all.heads + 2 * all.Hkv;
     for (int t0 = 0; t0 < all.n;) {
         RotateRows a = all;
         a.n = std::min(most, all.n - t0);
