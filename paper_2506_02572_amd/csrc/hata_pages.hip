@@ -373,9 +373,10 @@ __global__ __launch_bounds__(R <= 128 ? 256 : 512, 2) void write_mfma_kernel(con
     constexpr int COLW = R / 32, KP = R >= 128 ? 1 : 128 / R;  // waves by columns, by rows
     constexpr int THREADS = 64 * COLW * KP, NT = R >= 128 ? 2 : 1, STAGE = 32 * NT * KP, WD = R / 32;
     constexpr int ROWS_PER_IT = THREADS / 16, NIT = STAGE / ROWS_PER_IT;
-    __shared__ __attribute__((aligned(16))) uint16_t tile[STAGE * HATA_MFMA_PITCH];
+    constexpr int BUFS = HELD ? 2 : 1;  // stages in LDS
+    __shared__ __attribute__((aligned(16))) uint16_t s_tile[BUFS][STAGE * HATA_MFMA_PITCH];
     __shared__ __attribute__((aligned(16))) uint32_t s_code[WRITE_MAX_ROWS * WD];
-    __shared__ float s_norm[STAGE];
+    __shared__ float s_norms[BUFS][STAGE];
     __shared__ int s_row[WRITE_MAX_ROWS];
     __shared__ uint32_t s_doubt[WRITE_DOUBTS];  // row of the workgroup * R + column
     __shared__ int s_doubts, s_wholes;
@@ -387,10 +388,10 @@ __global__ __launch_bounds__(R <= 128 ? 256 : 512, 2) void write_mfma_kernel(con
     const uint16_t* Vh = a.V_new + h * a.sh;
 
     const int lrow = tid >> 4, lsub = tid & 15;
-    uint4 pre[NIT];
+    uint4 pre[BUFS][NIT];  // (HELD: two stages requested ahead, and the slots of a third)
     [[maybe_unused]] uint4 vpre[NIT];
-    int slot[NIT];
-    [[maybe_unused]] int slot_next[NIT];  // HELD: of the stage behind the one requested
+    int slot[BUFS][NIT];
+    [[maybe_unused]] int slot_next[NIT];
     [[maybe_unused]] auto load_slots = [&](int t0) {
 #pragma unroll
         for (int it = 0; it < NIT; ++it) {
@@ -399,31 +400,34 @@ __global__ __launch_bounds__(R <= 128 ? 256 : 512, 2) void write_mfma_kernel(con
             if (t >= last) slot_next[it] = -1;
         }
     };
-    auto load_stage = [&](int t0) {
+    auto load_stage = [&](int t0, uint4 (&x)[NIT], int (&to)[NIT]) {
         if constexpr (HELD) {
+            if (t0 >= last) return;
 #pragma unroll
-            for (int it = 0; it < NIT; ++it) {
-                slot[it] = slot_next[it];
-                pre[it] = *reinterpret_cast<const uint4*>(a.K + slot_row(a, clampi(slot[it], 0, a.rows - 1), h) * HATA_D + lsub * 8);
-            }
-            load_slots(t0 + STAGE);
+            for (int it = 0; it < NIT; ++it) to[it] = slot_next[it];
+            load_slots(t0 + STAGE);  // (ahead of the rows: what waits for them waits for nothing behind them)
+            __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+            for (int it = 0; it < NIT; ++it)
+                x[it] = *reinterpret_cast<const uint4*>(a.K + slot_row(a, clampi(to[it], 0, a.rows - 1), h) * HATA_D + lsub * 8);
             return;
         }
 #pragma unroll
         for (int it = 0; it < NIT; ++it) {
             const int t = t0 + it * ROWS_PER_IT + lrow;
-            slot[it] = a.slots[min(t, last - 1)];
-            if (t >= last) slot[it] = -1;
+            to[it] = a.slots[min(t, last - 1)];
+            if (t >= last) to[it] = -1;
         }
 #pragma unroll
         for (int it = 0; it < NIT; ++it) {
             const int64_t o = min(t0 + it * ROWS_PER_IT + lrow, last - 1) * a.st + lsub * 8;
-            pre[it] = load_once(Kh + o);
+            x[it] = load_once(Kh + o);
             vpre[it] = load_once(Vh + o);
         }
     };
     if constexpr (HELD) load_slots(first);
-    load_stage(first);
+    load_stage(first, pre[0], slot[0]);
+    if constexpr (HELD) load_stage(first + STAGE, pre[1], slot[1]);
     if (tid == 0) s_doubts = s_wholes = 0;
     if (tid < WRITE_MAX_ROWS / 32) s_whole[tid] = 0;
 
@@ -441,6 +445,9 @@ __global__ __launch_bounds__(R <= 128 ? 256 : 512, 2) void write_mfma_kernel(con
             for (int e = 0; e < 8; ++e) norm2 = fmaf((float)afrag16[0][kk][e], (float)afrag16[0][kk][e], norm2);
         }
         some_w = norm2;  // (the largest weight of a tile is scaled to 2^13 or more)
+        // (used here, or the wait for these loads stands in the loop, where it is one for the rows requested ahead as well)
+#pragma unroll
+        for (int kk = 0; kk < 8; ++kk) asm volatile("" : "+v"(afrag16[0][kk]), "+v"(afrag16[1][kk]));
     } else {
         const float* wp = a.W_H + (int64_t)h * HATA_D * R + w * 32 + m;
 #pragma unroll
@@ -465,18 +472,19 @@ __global__ __launch_bounds__(R <= 128 ? 256 : 512, 2) void write_mfma_kernel(con
     const bool no_w = !doubt && __builtin_amdgcn_ballot_w64(some_w != 0.f) == 0ull;
     const float wn = no_w ? 0.f : doubt || norm2 < 0x1p-80f ? __builtin_huge_valf() : sqrtf(norm2);
 
-    for (int t0 = first; t0 < last; t0 += STAGE) {
-        __syncthreads();  // the previous stage has been consumed
+    const int row0 = part * 32 * NT;
+    // the rows requested, of the stage at t0, into LDS (and into their slots)
+    auto put_stage = [&](int t0, const uint4 (&rows)[NIT], const int (&slots)[NIT], uint16_t* tile, float* s_norm) {
 #pragma unroll
         for (int it = 0; it < NIT; ++it) {
             const int row = it * ROWS_PER_IT + lrow;
-            const uint4 x = pre[it];
+            const uint4 x = rows[it];
             *reinterpret_cast<uint4*>(&tile[row * HATA_MFMA_PITCH + lsub * 8]) = F16 ? __builtin_bit_cast(uint4, bf16x8_to_f16(x)) : x;
             const float n2 = row_sum16(dot2_bf16(x.x, x.x, dot2_bf16(x.y, x.y, dot2_bf16(x.z, x.z, dot2_bf16(x.w, x.w, 0.f)))));
             const float some = row_max16(((x.x | x.y | x.z | x.w) & 0x7fff7fffu) ? 1.f : 0.f);
             int to = -1;
-            if (slot[it] >= 0 && slot[it] < a.rows) {
-                to = (int)slot_row(a, slot[it], h);
+            if (slots[it] >= 0 && slots[it] < a.rows) {
+                to = (int)slot_row(a, slots[it], h);
                 if constexpr (!HELD) {
                     *reinterpret_cast<uint4*>(a.K + (int64_t)to * HATA_D + lsub * 8) = x;
                     *reinterpret_cast<uint4*>(a.V + (int64_t)to * HATA_D + lsub * 8) = vpre[it];
@@ -489,15 +497,12 @@ __global__ __launch_bounds__(R <= 128 ? 256 : 512, 2) void write_mfma_kernel(con
                 s_row[t0 - first + row] = to;
             }
         }
-        __syncthreads();
-        if (t0 + STAGE < last) load_stage(t0 + STAGE);  // overlaps the products below
-
-        f32x16_t acc[NT];
+    };
+    auto products = [&](const uint16_t* tile, f32x16_t (&acc)[NT]) {
 #pragma unroll
         for (int t = 0; t < NT; ++t)
 #pragma unroll
             for (int i = 0; i < 16; ++i) acc[t][i] = 0.f;
-        const int row0 = part * 32 * NT;
         uint4 bfrag[NT];  // (a channel step ahead)
 #pragma unroll
         for (int t = 0; t < NT; ++t) bfrag[t] = *reinterpret_cast<const uint4*>(&tile[(row0 + t * 32 + m) * HATA_MFMA_PITCH + 8 * half]);
@@ -517,6 +522,8 @@ __global__ __launch_bounds__(R <= 128 ? 256 : 512, 2) void write_mfma_kernel(con
                 if (kk + 1 < 8)
                     bfrag[t] = *reinterpret_cast<const uint4*>(&tile[(row0 + t * 32 + m) * HATA_MFMA_PITCH + (kk + 1) * 16 + 8 * half]);
             }
+    };
+    auto signs = [&](int t0, const float* s_norm, const f32x16_t (&acc)[NT]) {
         // this lane holds hash columns 8 (i / 4) + 4 half + i % 4 of row t * 32 + m
 #pragma unroll
         for (int t = 0; t < NT; ++t) {
@@ -548,6 +555,35 @@ __global__ __launch_bounds__(R <= 128 ? 256 : 512, 2) void write_mfma_kernel(con
             word <<= 4 * half;
             word |= (uint32_t)__shfl_xor((int)word, 32, 64);
             if (half == 0) s_code[(t0 - first + row) * WD + w] = word;
+        }
+    };
+    if constexpr (HELD) {
+        // the next stage goes into LDS beside this one's products
+        put_stage(first, pre[0], slot[0], s_tile[0], s_norms[0]);
+        load_stage(first + 2 * STAGE, pre[0], slot[0]);
+        auto step = [&](int t0, int buf) {
+            __syncthreads();
+            f32x16_t acc[NT];
+            products(s_tile[buf], acc);
+            if (t0 + STAGE < last) {
+                put_stage(t0 + STAGE, pre[buf ^ 1], slot[buf ^ 1], s_tile[buf ^ 1], s_norms[buf ^ 1]);
+                load_stage(t0 + 3 * STAGE, pre[buf ^ 1], slot[buf ^ 1]);
+            }
+            signs(t0, s_norms[buf], acc);
+        };
+        for (int t0 = first; t0 < last; t0 += 2 * STAGE) {
+            step(t0, 0);
+            if (t0 + STAGE < last) step(t0 + STAGE, 1);
+        }
+    } else {
+        for (int t0 = first; t0 < last; t0 += STAGE) {
+            __syncthreads();  // the previous stage has been consumed
+            put_stage(t0, pre[0], slot[0], s_tile[0], s_norms[0]);
+            __syncthreads();
+            if (t0 + STAGE < last) load_stage(t0 + STAGE, pre[0], slot[0]);  // overlaps the products below
+            f32x16_t acc[NT];
+            products(s_tile[0], acc);
+            signs(t0, s_norms[0], acc);
         }
     }
     __syncthreads();
