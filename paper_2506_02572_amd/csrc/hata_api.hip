@@ -832,7 +832,7 @@ int hata_keep_rows(hata_ctx* ctx, void* K_pool, void* V_pool, uint32_t* codes_po
     const int64_t cap = (int64_t)max_blocks * page_rows;
     const hata_config& f = ctx->cfg;
     const hata::KeepRows a = {(uint16_t*)K_pool, (uint16_t*)V_pool, codes_pool, base_len, seq_len, path, n_path, seq_len_out, pv,
-                              f.Hkv, ctx->Wd, cap < f.L_cap ? (int)cap : f.L_cap, max_path};
+                              f.Hkv, ctx->Wd, cap < f.L_cap ? (int)cap : f.L_cap, max_path, 1};
     return hip_rc(hata::launch_keep_rows(a, B, (hipStream_t)stream));
 }
 

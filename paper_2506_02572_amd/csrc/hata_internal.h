@@ -168,7 +168,7 @@ struct KeepRows {
     const int32_t *base, *seq_len, *path, *n_path;
     int32_t* seq_len_out;
     PageView pv;
-    int Hkv, Wd, L_cap, max_path;
+    int Hkv, Wd, L_cap, max_path, heads;  // heads: of a workgroup
 };
 hipError_t launch_keep_rows(const KeepRows& a, int B, hipStream_t s);
 hipError_t prepare_topk();   // once per context

@@ -19,10 +19,13 @@ __device__ __forceinline__ int pool_row(const PageView& pv, int b, int n, int h,
 // tree_weight.  All units, one behind the other, are cut into as many equal pieces as there are workgroups, wherever that
 // falls; a workgroup goes through what lies in its piece.  Of these at most its first and its last one share a unit with
 // other workgroups: they leave partial results (2 i, or 2 i + 1 where the unit begins in workgroup i), and the workgroup with the unit's
-// first rows a record for the second launch.  Every workgroup works its share out from the lengths.
+// first rows a record for the second launch.  A few units are cut into whole pieces each, of the shortest run of tiles at which the
+// workgroups suffice.  Every workgroup works its share out from the lengths.
 #define TREE_ROWS 256
 #define TREE_WGS 256
-#define TREE_LEAST 35   // what a piece costs at least: the largest weight
+#define TREE_LEAST 35   // what a piece costs at least: the largest weight (or, of 32 query rows, a turn of four waves)
+#define TREE_LEAST_SMALL 16
+#define TREE_WHOLE 64   // up to so many units no workgroup has parts of two
 struct TreeRun { int members, t0, t1, h, first, lead, item, base, end, draft0; bool final; };
 struct TreeSequence { int t0, n, base, end; };
 
@@ -38,18 +41,28 @@ __device__ __forceinline__ TreeSequence tree_sequence(const TreeArgs& a, int b) 
 }
 // Tenths of a microsecond: of a tile of rows, with 32, 64, 128 and 256 query rows, and of a unit beside its rows (measured in ragged batches)
 __device__ __forceinline__ int tree_weight(int rows) { return rows <= 32 ? 8 : rows <= 64 ? 12 : rows <= 128 ? 21 : 35; }
-__device__ __forceinline__ int tree_start(int weight) { return weight == 8 ? 70 : 130; }
+// (where the units are fewer than the workgroups they are cut anyway, and every part has its own beginning)
+__device__ __forceinline__ int tree_start(int weight, int units) { return (weight == 8 ? 70 : 130) * min(units, TREE_WGS) / TREE_WGS; }
+// run > 0: a unit is cut into whole pieces of at most that, and its cost is their number
+struct TreeCuts { int units, run; };
 struct TreeCosts {
     int tiles, qt, full, last;  // weights of a tile of TREE_ROWS query rows and of the last one
-    __device__ __forceinline__ TreeCosts(const TreeSequence& q, int G) {
+    TreeCuts cuts;
+    __device__ __forceinline__ TreeCosts(const TreeSequence& q, int G, const TreeCuts& by) : cuts(by) {
         const int mpt = TREE_ROWS / G;
         tiles = max(1, (q.end + PREFIX_TILE - 1) / PREFIX_TILE);
         qt = (q.n + mpt - 1) / mpt;
         full = tree_weight(TREE_ROWS);
         last = tree_weight((q.n - (qt - 1) * mpt) * G);
     }
-    __device__ __forceinline__ int64_t unit(int weight) const { return tree_start(weight) + (int64_t)tiles * weight; }
+    __device__ __forceinline__ int64_t unit(int weight) const {
+        return cuts.run ? min((tiles * weight + cuts.run - 1) / cuts.run, tiles) : tree_start(weight, cuts.units) + (int64_t)tiles * weight;
+    }
     __device__ __forceinline__ int64_t head() const { return qt ? (qt - 1) * unit(full) + unit(last) : 0; }
+    // the tile of rows at x of a unit
+    __device__ __forceinline__ int tile_at(int x, int weight) const {
+        return cuts.run ? (int)((int64_t)tiles * x / unit(weight)) : (int)((uint32_t)max(x - tree_start(weight, cuts.units), 0) / (uint32_t)weight);
+    }
 };
 
 // x / d of numbers that are not negative, mostly below 2^32
@@ -63,6 +76,7 @@ struct TreeShare {
     int64_t at;        // the sequence that the next unit belongs to, and what lies in front of it
     int b;
     TreeSequence q;
+    float tiles[4];
     uint32_t seen[TREE_ROWS * SEEN_WORDS];
     int row[TREE_ROWS], member[TREE_ROWS];  // of DraftTables
 };
@@ -84,42 +98,68 @@ __global__ __launch_bounds__(256, 1) void tree_kernel(const TreeArgs a) {
     __shared__ TreeShare s;
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     const int wg = (int)((blockIdx.x % 8) * (TREE_WGS / 8) + blockIdx.x / 8), G = a.G, mpt = TREE_ROWS / G;
-    // what every thread's sequences cost, and all of them
-    const int per = (a.B + 255) / 256, b0 = tid * per;
+    // what every thread's sequences cost, and all of them (of up to 64 every wave finds that out for itself)
+    const bool few = a.B <= 64;
+    const int per = few ? 1 : (a.B + 255) / 256, b0 = few ? lane : tid * per, owners = few ? 64 : 256;
     const TreeSequence own = tree_sequence(a, b0);
-    int64_t mine = a.Hkv * TreeCosts(own, G).head();
-    for (int b = b0 + 1; b < b0 + per; ++b) mine += a.Hkv * TreeCosts(tree_sequence(a, b), G).head();
+    TreeCuts cuts = {0, 0};
+    {
+        float n = (float)((own.n + mpt - 1) / mpt);
+        for (int b = b0 + 1; b < b0 + per; ++b) n += (float)((tree_sequence(a, b).n + mpt - 1) / mpt);
+        n = wave_sum64(n);
+        if (!few) {
+            if (lane == 0) s.tiles[wave] = n;
+            __syncthreads();
+            n = s.tiles[0] + s.tiles[1] + s.tiles[2] + s.tiles[3];
+        }
+        cuts.units = a.Hkv * (int)fminf(n, (float)TREE_WGS);  // (more do not matter)
+    }
+    if (few && cuts.units <= TREE_WHOLE) {
+        const TreeCosts c(own, G, cuts);
+        const int full = c.tiles * c.full, last = c.tiles * c.last;
+        const float all = wave_sum64(c.qt ? (float)(c.qt - 1) * full + last : 0.f) * a.Hkv;
+        for (cuts.run = max(SMALL ? TREE_LEAST_SMALL : TREE_LEAST, (int)ceilf(all / TREE_WGS));; cuts.run += max(1, cuts.run >> 4))
+            if (wave_sum64((float)TreeCosts(own, G, cuts).head()) * a.Hkv <= (float)TREE_WGS) break;
+    }
+    int64_t mine = a.Hkv * TreeCosts(own, G, cuts).head();
+    for (int b = b0 + 1; b < b0 + per; ++b) mine += a.Hkv * TreeCosts(tree_sequence(a, b), G, cuts).head();
     {
         int64_t upto = mine;
-        for (int d = 1; d < 64; d <<= 1) {
-            const int64_t v = __shfl_up(upto, d, 64);
-            if (lane >= d) upto += v;
+        if (cuts.run) {
+            upto = (int64_t)wave_incl_scan((uint32_t)mine);
+        } else {
+            for (int d = 1; d < 64; d <<= 1) {
+                const int64_t v = __shfl_up(upto, d, 64);
+                if (lane >= d) upto += v;
+            }
         }
-        if (lane == 63) s.pre[wave] = upto;
-        __syncthreads();
         int64_t front = 0;
-        for (int k = 0; k < wave; ++k) front += s.pre[k];
-        __syncthreads();
-        s.pre[tid + 1] = front + upto;
+        if (!few) {
+            if (lane == 63) s.pre[wave] = upto;
+            __syncthreads();
+            for (int k = 0; k < wave; ++k) front += s.pre[k];
+            __syncthreads();
+        }
+        if (tid < owners) s.pre[tid + 1] = front + upto;
         if (tid == 0) s.pre[0] = 0;
-        __syncthreads();
     }
     s.row[tid] = tid / G * a.Hq + tid % G;
     s.member[tid] = tid / G;
     const DraftTables tables = {s.seen, s.row, s.member};
-    const int64_t total = s.pre[256];
-    const int pieces = (int)max((int64_t)1, min((int64_t)TREE_WGS, total / TREE_LEAST));
+    __syncthreads();
+    const int64_t total = s.pre[owners];
+    const int pieces = (int)max((int64_t)1, min((int64_t)TREE_WGS, cuts.run ? total : total / (SMALL ? TREE_LEAST_SMALL : TREE_LEAST)));
     const int64_t p0 = quotient(total * min(wg, pieces), pieces), p1 = quotient(total * min(wg + 1, pieces), pieces);
     TreeSplit split = {-1, 0, 0, 0};  // the unit that begins here and goes on elsewhere
     int seen_of = -1, seen_first = -1;
     int64_t pos = p0;
     while (pos < p1) {
         // the sequence that has the unit at pos
-        if (s.pre[tid] <= pos && pos < s.pre[tid + 1]) {
+        if (tid < owners && s.pre[tid] <= pos && pos < s.pre[tid + 1]) {
             int b = b0;
             int64_t at = s.pre[tid];
             TreeSequence q = own;
-            for (int64_t c = a.Hkv * TreeCosts(q, G).head(); at + c <= pos; c = a.Hkv * TreeCosts(q, G).head()) {
+            for (int64_t c = a.Hkv * TreeCosts(q, G, cuts).head(); at + c <= pos; c = a.Hkv * TreeCosts(q, G, cuts).head()) {
                 at += c;
                 q = tree_sequence(a, ++b);
             }
@@ -131,7 +171,7 @@ __global__ __launch_bounds__(256, 1) void tree_kernel(const TreeArgs a) {
         const TreeSequence q = {__builtin_amdgcn_readfirstlane(s.q.t0), __builtin_amdgcn_readfirstlane(s.q.n),
                                 __builtin_amdgcn_readfirstlane(s.q.base), __builtin_amdgcn_readfirstlane(s.q.end)};
         const int b = __builtin_amdgcn_readfirstlane(s.b);
-        const TreeCosts c(q, G);
+        const TreeCosts c(q, G, cuts);
         const int64_t at = s.at, head = c.head(), full = c.unit(c.full);
         int h = __builtin_amdgcn_readfirstlane((int)quotient(pos - at, head));
         int tile = __builtin_amdgcn_readfirstlane(min((int)quotient(pos - at - h * head, full), c.qt - 1));
@@ -141,10 +181,9 @@ __global__ __launch_bounds__(256, 1) void tree_kernel(const TreeArgs a) {
             for (; tile < c.qt && pos < p1; ++tile) {
                 const int weight = tile == c.qt - 1 ? c.last : c.full;
                 const int64_t u1 = u0 + c.unit(weight);
-                auto tile_at = [&](int64_t x) { return (int)((uint32_t)max((int)(x - u0) - tree_start(weight), 0) / (uint32_t)weight); };
                 TreeRun w;
-                w.t0 = __builtin_amdgcn_readfirstlane(p0 <= u0 ? 0 : tile_at(p0));
-                w.t1 = __builtin_amdgcn_readfirstlane(p1 >= u1 ? c.tiles : tile_at(p1));
+                w.t0 = __builtin_amdgcn_readfirstlane(p0 <= u0 ? 0 : c.tile_at((int)(p0 - u0), weight));
+                w.t1 = __builtin_amdgcn_readfirstlane(p1 >= u1 ? c.tiles : c.tile_at((int)(p1 - u0), weight));
                 w.h = h;
                 w.lead = b;
                 w.base = q.base;
@@ -186,6 +225,7 @@ __global__ __launch_bounds__(256, 1) void tree_kernel(const TreeArgs a) {
 
 // The results of the units that several workgroups have, joined: eight query rows a workgroup, half a wave each
 #define TREE_MERGE_ROWS 8
+#define TREE_MERGE_BATCH 16  // partial results requested together
 __global__ __launch_bounds__(256) void tree_merge_kernel(const TreeArgs a) {
     __shared__ float s_f[TREE_MERGE_ROWS][TREE_WGS];
     const TreeSplit u = a.splits[blockIdx.x];
@@ -204,6 +244,12 @@ __global__ __launch_bounds__(256) void tree_merge_kernel(const TreeArgs a) {
         if (s < ns) ml[j] = *reinterpret_cast<const float2*>(of_split(s) + a.part_rows * HATA_D + 2 * at);
         top = fmaxf(top, ml[j].x);
     }
+    float4 v[TREE_MERGE_BATCH];
+    auto load = [&](int s0) {
+#pragma unroll
+        for (int j = 0; j < TREE_MERGE_BATCH; ++j) v[j] = *reinterpret_cast<const float4*>(of_split(min(s0 + j, ns - 1)) + at * HATA_D + 4 * lane);
+    };
+    load(0);  // (on their way with the references)
     for (int m = 16; m; m >>= 1) top = fmaxf(top, __shfl_xor(top, m, 64));
     const float sub = top == HATA_NEG_INF ? 0.f : top;
 #pragma unroll
@@ -218,12 +264,10 @@ __global__ __launch_bounds__(256) void tree_merge_kernel(const TreeArgs a) {
     for (int m = 16; m; m >>= 1) l += __shfl_xor(l, m, 64);
     __syncthreads();
     float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
-    for (int s0 = 0; s0 < ns; s0 += 8) {
-        float4 v[8];
+    for (int s0 = 0; s0 < ns; s0 += TREE_MERGE_BATCH) {
+        if (s0) load(s0);
 #pragma unroll
-        for (int j = 0; j < 8; ++j) v[j] = *reinterpret_cast<const float4*>(of_split(min(s0 + j, ns - 1)) + at * HATA_D + 4 * lane);
-#pragma unroll
-        for (int j = 0; j < 8; ++j) {
+        for (int j = 0; j < TREE_MERGE_BATCH; ++j) {
             if (s0 + j >= ns) break;
             const float f = s_f[row][s0 + j];
             o.x = fmaf(f, v[j].x, o.x); o.y = fmaf(f, v[j].y, o.y); o.z = fmaf(f, v[j].z, o.z); o.w = fmaf(f, v[j].w, o.w);
@@ -266,51 +310,81 @@ hipError_t launch_tree(const TreeArgs& args, void* scratch, hipStream_t s) {
 
 // ---- the accepted path ----
 //
-// A workgroup has a KV head of a sequence.  Rows go KEEP_ROWS at a time, all read before the first is written: a path's rows move
-// to the front only, so rows that are still to be read are never written.
-#define KEEP_ROWS 32
+// A workgroup has some KV heads of a sequence.  The rows' places are looked up once for all of them; then rows go as many at a time as the
+// threads have registers for, all read before the first is written: a path's rows move to the front only, so rows that are still to be
+// read are never written.  Bound by latency: lengths and path, places, rows, one after the other.
 __global__ __launch_bounds__(256) void keep_rows_kernel(const KeepRows a) {
-    __shared__ int s_path[HATA_TREE_MAX_DRAFT], s_kept;
-    const int tid = threadIdx.x, h = blockIdx.x, b = blockIdx.y;
+    __shared__ int s_from[HATA_TREE_MAX_DRAFT], s_to[HATA_TREE_MAX_DRAFT];  // row of the first KV head in the pools; -1: is there already
+    __shared__ int s_kept;
+    const int tid = threadIdx.x, b = blockIdx.y, h0 = blockIdx.x * a.heads, heads = min(a.heads, a.Hkv - h0);
+    const int* path = a.path + (int64_t)b * a.max_path;
+    const int j = tid < a.max_path ? path[tid] : -1, before = tid > 0 && tid < a.max_path ? path[tid - 1] : -1;
     const int L = clampi(a.seq_len[b], 0, a.L_cap), base = clampi(a.base[b], 0, L);
     const int most = clampi(a.n_path[b], 0, min(a.max_path, HATA_TREE_MAX_DRAFT));
     if (tid == 0) s_kept = most;
     __syncthreads();
-    const int* path = a.path + (int64_t)b * a.max_path;
-    for (int i = tid; i < most; i += 256) {
-        const int j = path[i];
-        s_path[i] = j;
-        if (j < 0 || j >= L - base || (i > 0 && path[i - 1] >= j)) atomicMin(&s_kept, i);
-    }
+    if (tid < most && (j < 0 || j >= L - base || before >= j)) atomicMin(&s_kept, tid);
     __syncthreads();
-    const int kept = s_kept, col = tid & 31, r8 = tid >> 5;
-    for (int i0 = 0; i0 < kept; i0 += KEEP_ROWS) {
-        uint4 v[4];
-        uint32_t code = 0;
-        uint16_t* pool = (col < 16 ? a.K : a.V) + (col & 15) * 8;
-#pragma unroll
-        for (int u = 0; u < 4; ++u) {
-            const int i = i0 + 8 * u + r8;
-            if (i < kept) v[u] = *reinterpret_cast<const uint4*>(pool + (int64_t)pool_row(a.pv, b, base + s_path[i], h, a.Hkv) * HATA_D);
-        }
-        const int ic = i0 + (tid >> 3), w = tid & 7;
-        const bool has_code = a.codes && ic < kept && w < a.Wd;
-        if (has_code) code = a.codes[(int64_t)pool_row(a.pv, b, base + s_path[ic], h, a.Hkv) * a.Wd + w];
-        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-        __syncthreads();
-#pragma unroll
-        for (int u = 0; u < 4; ++u) {
-            const int i = i0 + 8 * u + r8;
-            if (i < kept && s_path[i] != i) *reinterpret_cast<uint4*>(pool + (int64_t)pool_row(a.pv, b, base + i, h, a.Hkv) * HATA_D) = v[u];
-        }
-        if (has_code && s_path[ic] != ic) a.codes[(int64_t)pool_row(a.pv, b, base + ic, h, a.Hkv) * a.Wd + w] = code;
-        __syncthreads();
+    const int kept = s_kept;
+    if (tid < kept) {
+        s_from[tid] = pool_row(a.pv, b, base + j, 0, a.Hkv);
+        s_to[tid] = j == tid ? -1 : pool_row(a.pv, b, base + tid, 0, a.Hkv);
     }
-    if (h == 0 && tid == 0) a.seq_len_out[b] = base + kept;
+    if (blockIdx.x == 0 && tid == 0) a.seq_len_out[b] = base + kept;
+    __syncthreads();
+    // A turn: 2048 pieces of 16 bytes, 16 of K and 16 of V a row and head, and 512 words of codes, eight a row and head (heads to a
+    // power of two)
+    const int hs = heads > 1 ? 32 - __clz(heads - 1) : 0, rows = max(64 >> hs, 1);
+    for (int i0 = 0; i0 < kept; i0 += rows)
+        for (int e0 = 0; e0 < 32 << hs; e0 += 2048) {  // (more than once with 128 heads and more: a part of the heads at a time)
+            uint4 v[8];
+            uint32_t code[2];
+            uint16_t* at[8];
+            uint32_t* code_at[2];
+            auto place = [&](int e, int shift, int& i, int& h) {  // items of 1 << shift a row and head
+                i = i0 + (e >> (shift + hs));
+                h = h0 + (e >> shift & ((1 << hs) - 1));
+                return i < min(kept, i0 + rows) && h < h0 + heads && s_to[i] >= 0;
+            };
+#pragma unroll
+            for (int u = 0; u < 8; ++u) {
+                const int e = e0 + u * 256 + tid;
+                int i, h;
+                at[u] = nullptr;
+                v[u] = make_uint4(0, 0, 0, 0);
+                if (place(e, 5, i, h)) {
+                    uint16_t* pool = (e & 16 ? a.V : a.K) + (e & 15) * 8;
+                    v[u] = *reinterpret_cast<const uint4*>(pool + (s_from[i] + ((int64_t)h << a.pv.shift)) * HATA_D);
+                    at[u] = pool + (s_to[i] + ((int64_t)h << a.pv.shift)) * HATA_D;
+                }
+            }
+#pragma unroll
+            for (int u = 0; u < 2; ++u) {
+                const int e = e0 / 4 + u * 256 + tid;
+                int i, h;
+                code_at[u] = nullptr;
+                code[u] = 0;
+                if (a.codes && (e & 7) < a.Wd && place(e, 3, i, h)) {
+                    code[u] = a.codes[(s_from[i] + ((int64_t)h << a.pv.shift)) * a.Wd + (e & 7)];
+                    code_at[u] = a.codes + (s_to[i] + ((int64_t)h << a.pv.shift)) * a.Wd + (e & 7);
+                }
+            }
+            asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+            __syncthreads();
+#pragma unroll
+            for (int u = 0; u < 8; ++u)
+                if (at[u]) *reinterpret_cast<uint4*>(at[u]) = v[u];
+#pragma unroll
+            for (int u = 0; u < 2; ++u)
+                if (code_at[u]) *code_at[u] = code[u];
+        }
 }
 
-hipError_t launch_keep_rows(const KeepRows& a, int B, hipStream_t s) {
-    hipLaunchKernelGGL(keep_rows_kernel, dim3(a.Hkv, B), dim3(256), 0, s, a);
+hipError_t launch_keep_rows(const KeepRows& args, int B, hipStream_t s) {
+    KeepRows a = args;
+    a.heads = 1;  // of a workgroup: two rounds of them at most
+    while ((int64_t)B * ((a.Hkv + a.heads - 1) / a.heads) > 512 && a.heads < a.Hkv) a.heads *= 2;
+    hipLaunchKernelGGL(keep_rows_kernel, dim3((a.Hkv + a.heads - 1) / a.heads, B), dim3(256), 0, s, a);
     return hipGetLastError();
 }
 
