@@ -293,53 +293,54 @@ __global__ __launch_bounds__(256) void write_few_kernel(const WriteSlots a) {
 }
 
 // The same with the keys rotated on the way, through LDS, and one workgroup more for every KV head: the queries of its group.  A thread
-// has a piece of a row (RotaryPiece) and works its angles out for itself, for all of the group's heads.
+// has a piece of a row (RotaryPiece).
 template <int COLS>
 __global__ __launch_bounds__(256) void rotate_write_few_kernel(const WriteSlots a) {
     constexpr int WPS = COLS / 32;
     __shared__ uint32_t s_codes[(WRITE_ROWS + 4) * WPS];
     __shared__ __attribute__((aligned(16))) uint16_t s_key[WRITE_ROWS * HATA_D];
+    __shared__ RotaryTable s_angles;
     const int tid = threadIdx.x, h = blockIdx.y, t0 = blockIdx.z * WRITE_ROWS, nv = min(WRITE_ROWS, a.n - t0);
     const int p = tid & 7, v = (tid >> 3) & (WRITE_ROWS - 1), second = tid >> 7, t = t0 + min(v, nv - 1);
     const RotaryPiece piece(p, a.rot.dims, a.rot.interleaved);
-    const int slices = a.codes ? a.r / COLS : 1;
-    if ((int)blockIdx.x == slices) {  // queries
-        const RotaryAngles angles(a.rot, p);
-        const int position = a.rot.positions[t];
+    if ((int)blockIdx.x == a.r / COLS) {  // queries
+        s_angles.fill(a.rot, t0, nv);
+        __syncthreads();
         if (v >= nv) return;
         for (int g = second; g < a.G; g += 2) {
             const uint16_t* from = a.q + t * a.q_st + (h * a.G + g) * a.q_sh;
             uint16_t* to = a.q_out + ((int64_t)t * a.Hkv * a.G + h * a.G + g) * HATA_D;
             uint4 x[2] = {*reinterpret_cast<const uint4*>(from + piece.at[0]), *reinterpret_cast<const uint4*>(from + piece.at[1])};
-            angles.rotate(a.rot, x, position);
+            s_angles.rotate(a.rot, x, v, p);
             *reinterpret_cast<uint4*>(to + piece.at[0]) = x[0];
             *reinterpret_cast<uint4*>(to + piece.at[1]) = x[1];
         }
         return;
     }
     HashWeights<COLS> hw;
-    if (a.codes) hw.fetch(a.W_H + (int64_t)h * HATA_D * a.r + blockIdx.x * COLS, a.r);
+    hw.fetch(a.W_H + (int64_t)h * HATA_D * a.r + blockIdx.x * COLS, a.r);
     const int slot = a.slots[t];
     const bool live = v < nv && slot >= 0 && slot < a.rows;
     const int64_t from = t * a.st + h * a.sh, to = live ? slot_row(a, slot, h) * HATA_D : 0;
-    if (!second) {  // keys
-        uint4 x[2] = {*reinterpret_cast<const uint4*>(a.K_new + from + piece.at[0]), *reinterpret_cast<const uint4*>(a.K_new + from + piece.at[1])};
-        RotaryAngles(a.rot, p).rotate(a.rot, x, a.rot.positions[t]);
+    const uint16_t* source = (second ? a.V_new : a.K_new) + from;
+    uint4 x[2] = {*reinterpret_cast<const uint4*>(source + piece.at[0]), *reinterpret_cast<const uint4*>(source + piece.at[1])};
+    s_angles.fill(a.rot, t0, nv);
+    __syncthreads();
+    if (!second) {
+        s_angles.rotate(a.rot, x, v, p);
 #pragma unroll
-        for (int i = 0; i < 2; ++i) {
-            *reinterpret_cast<uint4*>(s_key + v * HATA_D + piece.at[i]) = x[i];
-            if (live && blockIdx.x == 0) *reinterpret_cast<uint4*>(a.K + to + piece.at[i]) = x[i];
-        }
-    } else if (live && blockIdx.x == 0) {
-#pragma unroll
-        for (int i = 0; i < 2; ++i) *reinterpret_cast<uint4*>(a.V + to + piece.at[i]) = *reinterpret_cast<const uint4*>(a.V_new + from + piece.at[i]);
+        for (int i = 0; i < 2; ++i) *reinterpret_cast<uint4*>(s_key + v * HATA_D + piece.at[i]) = x[i];
     }
-    if (!a.codes) return;
+    if (live && blockIdx.x == 0) {
+        uint16_t* pool = (second ? a.V : a.K) + to;
+#pragma unroll
+        for (int i = 0; i < 2; ++i) *reinterpret_cast<uint4*>(pool + piece.at[i]) = x[i];
+    }
     __syncthreads();
     for (int v0 = 0; v0 < nv; v0 += 4) {
-        uint4 x[4];
-        hash_load_x(s_key + min(v0 + (tid & 3), nv - 1) * HATA_D, x);
-        hash_pass<COLS>(hw, x, s_codes, WPS, v0, nv);
+        uint4 k[4];
+        hash_load_x(s_key + min(v0 + (tid & 3), nv - 1) * HATA_D, k);
+        hash_pass<COLS>(hw, k, s_codes, WPS, v0, nv);
     }
     __syncthreads();
     for (int i = tid; i < nv * WPS; i += 256) {

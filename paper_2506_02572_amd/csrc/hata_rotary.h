@@ -96,23 +96,29 @@ __device__ __forceinline__ void rotate_piece(uint4 (&x)[2], const double (&c)[8]
     }
 }
 
-// The piece's frequencies, and a row's angles from them
-struct RotaryAngles {
-    double f[8];
-    bool turns;  // the piece's channels are rotated at all
-    __device__ __forceinline__ RotaryAngles(const RotaryArgs& a, int p) {
-        turns = 16 * p < a.dims;
+// Angles of up to 16 rows in LDS, four pairs a thread of 256
+struct RotaryTable {
+    double cos[16][HATA_D / 2], sin[16][HATA_D / 2];
+    __device__ __forceinline__ void fill(const RotaryArgs& a, int t0, int rows) {
+        const int v = threadIdx.x >> 4, pairs = a.dims / 2;
+        const double position = a.positions[t0 + min(v, rows - 1)];
 #pragma unroll
-        for (int i = 0; i < 8; ++i) f[i] = a.freq[min(8 * p + i, a.dims / 2 - 1)];
+        for (int i = 0; i < 4; ++i) {
+            const int p = (threadIdx.x & 15) + 16 * i;
+            double c, s;
+            cos_sin(position * a.freq[min(p, pairs - 1)], c, s);
+            cos[v][p] = c * a.magnitude;
+            sin[v][p] = s * a.magnitude;
+        }
     }
-    __device__ __forceinline__ void rotate(const RotaryArgs& a, uint4 (&x)[2], int position) const {
-        if (!turns) return;
+    // piece p of row v
+    __device__ __forceinline__ void rotate(const RotaryArgs& a, uint4 (&x)[2], int v, int p) const {
+        if (16 * p >= a.dims) return;
         double c[8], s[8];
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
-            cos_sin((double)position * f[i], c[i], s[i]);
-            c[i] *= a.magnitude;
-            s[i] *= a.magnitude;
+            c[i] = cos[v][8 * p + i];
+            s[i] = sin[v][8 * p + i];
         }
         rotate_piece(x, c, s, a.interleaved);
     }
