@@ -1,5 +1,6 @@
 // Pages of a paged cache: block tables and slot maps from request lengths, and packed rows written through a slot map.
 #include <algorithm>
+#include <type_traits>
 #include "hata_attn_core.h"
 #include "hata_device.h"
 #include "hata_encode_core.h"
@@ -367,21 +368,25 @@ __global__ __launch_bounds__(256) void rotate_write_few_kernel(const WriteSlots 
 // Rounds of resident workgroups (write_rows_per_wg): 45.4 us with twice as many of half the rows.
 #define WRITE_ERROR 0x1p-16f
 #define WRITE_MAX_ROWS 1024  // of a workgroup
+#define HELD_MAX_ROWS 1536
 #define WRITE_DOUBTS 512
+// (codes of r = 32 in stages of twice the rows leave no room for more)
+constexpr int write_max_rows(int r, bool held) { return held && r > 32 ? HELD_MAX_ROWS : WRITE_MAX_ROWS; }
 // HELD: the rows lie in their slots already (rotated, by the launch before: read from the caches), and their codes alone are wanted.
 template <int R, bool F16, bool HELD>
 __global__ __launch_bounds__(R <= 128 ? 256 : 512, 2) void write_mfma_kernel(const WriteSlots a, const uint4* __restrict__ planes, int rows_per_wg) {
     constexpr int COLW = R / 32, KP = R >= 128 ? 1 : 128 / R;  // waves by columns, by rows
     constexpr int THREADS = 64 * COLW * KP, NT = R >= 128 ? 2 : 1, STAGE = 32 * NT * KP, WD = R / 32;
     constexpr int ROWS_PER_IT = THREADS / 16, NIT = STAGE / ROWS_PER_IT;
+    constexpr int MAX_ROWS = write_max_rows(R, HELD);
     constexpr int BUFS = HELD ? 2 : 1;  // stages in LDS
     __shared__ __attribute__((aligned(16))) uint16_t s_tile[BUFS][STAGE * HATA_MFMA_PITCH];
-    __shared__ __attribute__((aligned(16))) uint32_t s_code[WRITE_MAX_ROWS * WD];
+    __shared__ __attribute__((aligned(16))) uint32_t s_code[MAX_ROWS * WD];
     __shared__ float s_norms[BUFS][STAGE];
-    __shared__ int s_row[WRITE_MAX_ROWS];
+    __shared__ int s_row[MAX_ROWS];
     __shared__ uint32_t s_doubt[WRITE_DOUBTS];  // row of the workgroup * R + column
     __shared__ int s_doubts, s_wholes;
-    __shared__ uint32_t s_whole[WRITE_MAX_ROWS / 32];  // rows of which every bit is in doubt
+    __shared__ uint32_t s_whole[MAX_ROWS / 32];  // rows of which every bit is in doubt
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int w = wave % COLW, part = wave / COLW, m = lane & 31, half = lane >> 5, h = blockIdx.y;
     const int first = blockIdx.x * rows_per_wg, last = min(first + rows_per_wg, a.n);
@@ -430,7 +435,7 @@ __global__ __launch_bounds__(R <= 128 ? 256 : 512, 2) void write_mfma_kernel(con
     load_stage(first, pre[0], slot[0]);
     if constexpr (HELD) load_stage(first + STAGE, pre[1], slot[1]);
     if (tid == 0) s_doubts = s_wholes = 0;
-    if (tid < WRITE_MAX_ROWS / 32) s_whole[tid] = 0;
+    if (tid < MAX_ROWS / 32) s_whole[tid] = 0;
 
     // weight fragments, and the largest norm of this wave's columns (of the fp16 planes: scaled as they are)
     bf16x8_t afrag[F16 ? 1 : 3][F16 ? 1 : 8];
@@ -562,7 +567,8 @@ __global__ __launch_bounds__(R <= 128 ? 256 : 512, 2) void write_mfma_kernel(con
         // the next stage goes into LDS beside this one's products
         put_stage(first, pre[0], slot[0], s_tile[0], s_norms[0]);
         load_stage(first + 2 * STAGE, pre[0], slot[0]);
-        auto step = [&](int t0, int buf) {
+        auto step = [&](int t0, auto of) __attribute__((always_inline)) {
+            constexpr int buf = decltype(of)::value;  // (or the rows requested ahead would lie in memory)
             __syncthreads();
             f32x16_t acc[NT];
             products(s_tile[buf], acc);
@@ -573,8 +579,8 @@ __global__ __launch_bounds__(R <= 128 ? 256 : 512, 2) void write_mfma_kernel(con
             signs(t0, s_norms[buf], acc);
         };
         for (int t0 = first; t0 < last; t0 += 2 * STAGE) {
-            step(t0, 0);
-            if (t0 + STAGE < last) step(t0 + STAGE, 1);
+            step(t0, std::integral_constant<int, 0>());
+            if (t0 + STAGE < last) step(t0 + STAGE, std::integral_constant<int, 1>());
         }
     } else {
         for (int t0 = first; t0 < last; t0 += STAGE) {
@@ -615,7 +621,7 @@ __global__ __launch_bounds__(R <= 128 ? 256 : 512, 2) void write_mfma_kernel(con
         }
     };
     settle(min(s_doubts, WRITE_DOUBTS), [&](int i) { return s_doubt[i]; });
-    for (int k = 0; k < (s_wholes ? WRITE_MAX_ROWS / 32 : 0); ++k)
+    for (int k = 0; k < (s_wholes ? MAX_ROWS / 32 : 0); ++k)
         for (uint32_t rows = s_whole[k]; rows; rows &= rows - 1) {
             const uint32_t row = 32 * k + __ffs(rows) - 1;
             settle(R, [&](int i) { return row * R + i; });
@@ -635,13 +641,14 @@ __global__ __launch_bounds__(R <= 128 ? 256 : 512, 2) void write_mfma_kernel(con
 
 // Rows of a workgroup: a round of as many workgroups as are resident (two of four waves on a compute unit, one of eight), or several
 // equal rounds
-static int write_rows_per_wg(int n, int Hkv, int r) {
+static int write_rows_per_wg(int n, int Hkv, int r, bool held) {
     const int64_t resident = (r <= 128 ? 2 : 1) * 256;
     const int64_t stages = (n + 63) / 64;
+    const int most = write_max_rows(r, held) / 64;
     int64_t rounds = 1, per;
     do per = (stages * Hkv + rounds * resident - 1) / (rounds * resident), ++rounds;
-    while (per > WRITE_MAX_ROWS / 64);
-    while ((stages + per - 1) / per * Hkv > (rounds - 1) * resident && per < WRITE_MAX_ROWS / 64) ++per;  // (whole stages of every head)
+    while (per > most);
+    while ((stages + per - 1) / per * Hkv > (rounds - 1) * resident && per < most) ++per;  // (whole stages of every head)
     return (int)per * 64;
 }
 
@@ -652,7 +659,7 @@ template <bool HELD>
 static hipError_t launch_write_mfma(const hata_ctx* c, const WriteSlots& a, hipStream_t s) {
     // the weight planes prepared for exactly this weight tensor, if any
     const uint4* planes = (c->prepared_W_H == a.W_H && c->wplanes) ? (const uint4*)c->wplanes : nullptr;
-    const int per = write_rows_per_wg(a.n, a.Hkv, a.r);
+    const int per = write_rows_per_wg(a.n, a.Hkv, a.r, HELD);
     const dim3 grid((a.n + per - 1) / per, a.Hkv);
 #define HATA_LAUNCH_WRITE(R_) \
     hipLaunchKernelGGL((planes ? write_mfma_kernel<R_, true, HELD> : write_mfma_kernel<R_, false, HELD>), grid, dim3(R_ <= 128 ? 256 : 512), 0, s, a, planes, per)
