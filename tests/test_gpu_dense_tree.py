@@ -196,6 +196,25 @@ def test_many_sequences(hata, B, Hq, Hkv):
     s.ctx.close()
 
 
+@pytest.mark.parametrize("B,Hq,Hkv,draft", [(257, 8, 1, 3), (700, 4, 4, 2), (1500, 2, 1, 5), (513, 8, 2, 40)])
+def test_more_sequences_than_workgroups(hata, B, Hq, Hkv, draft):
+    """Several sequences a workgroup and a thread; every seventh without tokens, the last one long."""
+    rng = np.random.default_rng(B)
+    base = rng.integers(0, 100, B)
+    base[-1] = 5000
+    s = Drafts(hata, base.tolist(), [0 if b % 7 == 3 else draft for b in range(B)], Hq, Hkv, seed=B)
+    s.check()
+    s.ctx.close()
+
+
+@pytest.mark.parametrize("Hq,Hkv,draft,L", [(8, 2, 64, 30000), (4, 1, 256, 40000), (2, 1, 9, 100000), (8, 8, 256, 9000)])
+def test_units_of_many_parts(hata, Hq, Hkv, draft, L):
+    """One sequence, few units: a unit's rows in up to 256 parts, joined in batches."""
+    s = Drafts(hata, [L], [draft], Hq, Hkv, P=64, seed=L)
+    s.check()
+    s.ctx.close()
+
+
 @pytest.mark.parametrize("mask", ["none", "any"])
 def test_tokens_that_see_nothing(hata, mask):
     """No committed rows and an empty mask: zeros."""
