@@ -264,9 +264,9 @@ __global__ __launch_bounds__(256, 1) void tree_kernel(const TreeArgs a) {
 // The results of the units that several workgroups have, joined: eight query rows a workgroup, half a wave each
 #define TREE_MERGE_ROWS 8
 #define TREE_MERGE_BATCH 16  // partial results requested together
-// (A unit's groups take turns on the XCDs.  Where they are all on the XCD of workgroup i, units of 32 parts, which begin in workgroups
-// 0, 32, 64 .., are all on one XCD: eight of them with 256 query rows 47 us instead of 9; 140 units of two parts and 128 query rows 23 us
-// instead of 15)
+// (A unit's groups take turns on the XCDs.  With those of unit i all on XCD i % 8, units of 32 parts, which begin in workgroups 0, 32,
+// 64 .., are all on one: eight of them with 256 query rows 47 us instead of 9, 150 units of two parts 23 us instead of 15; each on the XCD that
+// has its parts in its L2 11 and 22 us)
 __global__ __launch_bounds__(256) void tree_merge_kernel(const TreeArgs a) {
     __shared__ float s_f[TREE_MERGE_ROWS][TREE_WGS];
     const int group = blockIdx.y, unit = (blockIdx.x - group) & (TREE_WGS - 1);
