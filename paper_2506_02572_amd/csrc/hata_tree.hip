@@ -263,7 +263,8 @@ __global__ __launch_bounds__(256, 1) void tree_kernel(const TreeArgs a) {
 
 // The results of the units that several workgroups have, joined: eight query rows a workgroup, half a wave each
 #define TREE_MERGE_ROWS 8
-#define TREE_MERGE_BATCH 16  // partial results requested together
+#define TREE_MERGE_BATCH 8  // partial results requested together
+#define TREE_MERGE_FEW 4     // up to so many without LDS
 // (A unit's groups take turns on the XCDs.  With those of unit i all on XCD i % 8, units of 32 parts, which begin in workgroups 0, 32,
 // 64 .., are all on one: eight of them with 256 query rows 47 us instead of 9, 150 units of two parts 23 us instead of 15; each on the XCD that
 // has its parts in its L2 11 and 22 us)
@@ -274,47 +275,65 @@ __global__ __launch_bounds__(256) void tree_merge_kernel(const TreeArgs a) {
     const int row = threadIdx.x >> 5, r = group * TREE_MERGE_ROWS + row, lane = threadIdx.x & 31;
     if (u.last < 0 || group * TREE_MERGE_ROWS >= u.rows) return;
     const int at = min(r, u.rows - 1), ns = u.last - unit + 1;
-    const int64_t size = (int64_t)a.part_rows * (HATA_D + 2);
+    const uint32_t size = a.part_rows * (HATA_D + 2);  // (all of them: below 2^25 floats)
     const float* part = a.part + 2 * (int64_t)unit * size;
-    auto of_split = [&](int s) { return part + (s ? 2 * s : 1) * size; };
+    auto of_split = [&](int s) { return (s ? 2 * s : 1) * size; };
+    auto weight = [](float x, float top) { return x == HATA_NEG_INF ? (top == HATA_NEG_INF ? 1.f : 0.f) : fast_exp2(x - (top == HATA_NEG_INF ? 0.f : top)); };
+    auto sums_of = [&](int s) { return *reinterpret_cast<const float2*>(part + (of_split(s) + a.part_rows * HATA_D + 2 * at)); };
     float top = HATA_NEG_INF, l = 0.f;
-    float2 ml[TREE_WGS / 32];
-#pragma unroll
-    for (int j = 0; j < TREE_WGS / 32; ++j) {
-        const int s = 32 * j + lane;
-        ml[j] = make_float2(HATA_NEG_INF, 0.f);
-        if (s < ns) ml[j] = *reinterpret_cast<const float2*>(of_split(s) + a.part_rows * HATA_D + 2 * at);
-        top = fmaxf(top, ml[j].x);
-    }
-    float4 v[TREE_MERGE_BATCH];
-    auto load = [&](int s0) {
-#pragma unroll
-        for (int j = 0; j < TREE_MERGE_BATCH; ++j) v[j] = *reinterpret_cast<const float4*>(of_split(min(s0 + j, ns - 1)) + at * HATA_D + 4 * lane);
-    };
-    load(0);  // (on their way with the references)
-    for (int m = 16; m; m >>= 1) top = fmaxf(top, __shfl_xor(top, m, 64));
-    const float sub = top == HATA_NEG_INF ? 0.f : top;
-#pragma unroll
-    for (int j = 0; j < TREE_WGS / 32; ++j) {
-        const int s = 32 * j + lane;
-        const float f = ml[j].x == HATA_NEG_INF ? (top == HATA_NEG_INF ? 1.f : 0.f) : fast_exp2(ml[j].x - sub);
-        if (s < ns) {
-            s_f[row][s] = f;
-            l = fmaf(f, ml[j].y, l);
-        }
-    }
-    for (int m = 16; m; m >>= 1) l += __shfl_xor(l, m, 64);
-    __syncthreads();
     float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
-    for (int s0 = 0; s0 < ns; s0 += TREE_MERGE_BATCH) {
-        if (s0) load(s0);
+    // parts s0 .. s0 + N - 1: requested, and added (no branch: requests behind one would go out one by one.  32 partial results of 256 query
+    // rows and eight heads 72 us that way)
+    auto load = [&](auto& v, int s0) {
+        int j = 0;
+        for (float4& x : v) x = *reinterpret_cast<const float4*>(part + (of_split(min(s0 + j++, ns - 1)) + at * HATA_D + 4 * lane));
+    };
+    auto add = [&](const float4& v, float f, bool here) {
+        const uint32_t there = here ? ~0u : 0u;
+        auto one = [&](float& sum, float x) { sum = fmaf(f, __uint_as_float(__float_as_uint(x) & there), sum); };
+        one(o.x, v.x); one(o.y, v.y); one(o.z, v.z); one(o.w, v.w);
+    };
+    if (ns <= TREE_MERGE_FEW) {
+        float2 ml[TREE_MERGE_FEW];
+        float4 v[TREE_MERGE_FEW];
 #pragma unroll
-        for (int j = 0; j < TREE_MERGE_BATCH; ++j) {
-            // (no branch: requests behind one would go out one by one.  32 partial results of 256 query rows and eight heads 72 us that way)
-            const uint32_t there = s0 + j < ns ? ~0u : 0u;
-            const float f = s_f[row][min(s0 + j, ns - 1)];
-            auto add = [&](float& sum, float x) { sum = fmaf(f, __uint_as_float(__float_as_uint(x) & there), sum); };
-            add(o.x, v[j].x); add(o.y, v[j].y); add(o.z, v[j].z); add(o.w, v[j].w);
+        for (int s = 0; s < TREE_MERGE_FEW; ++s) ml[s] = sums_of(min(s, ns - 1));
+        load(v, 0);
+#pragma unroll
+        for (int s = 0; s < TREE_MERGE_FEW; ++s) top = fmaxf(top, ml[s].x);
+#pragma unroll
+        for (int s = 0; s < TREE_MERGE_FEW; ++s) {
+            const float f = weight(ml[s].x, top);
+            l = s < ns ? fmaf(f, ml[s].y, l) : l;
+            add(v[s], f, s < ns);
+        }
+    } else {
+        float2 ml[TREE_WGS / 32];
+#pragma unroll
+        for (int j = 0; j < TREE_WGS / 32; ++j) {
+            const int s = 32 * j + lane;
+            ml[j] = make_float2(HATA_NEG_INF, 0.f);
+            if (s < ns) ml[j] = sums_of(s);
+            top = fmaxf(top, ml[j].x);
+        }
+        float4 v[TREE_MERGE_BATCH];
+        load(v, 0);  // (on their way with the references)
+        for (int m = 16; m; m >>= 1) top = fmaxf(top, __shfl_xor(top, m, 64));
+#pragma unroll
+        for (int j = 0; j < TREE_WGS / 32; ++j) {
+            const int s = 32 * j + lane;
+            const float f = weight(ml[j].x, top);
+            if (s < ns) {
+                s_f[row][s] = f;
+                l = fmaf(f, ml[j].y, l);
+            }
+        }
+        for (int m = 16; m; m >>= 1) l += __shfl_xor(l, m, 64);
+        __syncthreads();
+        for (int s0 = 0; s0 < ns; s0 += TREE_MERGE_BATCH) {
+            if (s0) load(v, s0);
+#pragma unroll
+            for (int j = 0; j < TREE_MERGE_BATCH; ++j) add(v[j], s_f[row][min(s0 + j, ns - 1)], s0 + j < ns);
         }
     }
     if (r >= u.rows) return;
