@@ -407,7 +407,7 @@ typedef struct {
 } hata_rotary_scaling;
 int hata_rotary_frequencies(int32_t dims, double base, const hata_rotary_scaling* scaling, double* freq, float* magnitude);
 
-/* Packed rows rotated: n_heads heads of each of n_tokens rows, x and out with strides as in hata_write_slots.  back != 0: by -t, which
+/* Packed rows rotated: n_heads (1 .. 65535) heads of each of n_tokens rows, x and out with strides as in hata_write_slots.  back != 0: by -t, which
  * is the gradient of the forward call (its transpose, m included).  out may be x with the same strides; otherwise they must not
  * overlap.  Any number of tokens; the context's shape does not matter. */
 int hata_rotate(hata_ctx* ctx, const void* x, int64_t stride_t, int64_t stride_h, int32_t n_heads, const int32_t* positions,
@@ -434,11 +434,11 @@ int hata_rotate_write_slots(hata_ctx* ctx, const void* q, int64_t q_stride_t, in
  *   mask [n_tokens, mask_words] or NULL: bit j % 32 of word j / 32 says whether the row's token sees drafted token j of its
  *                            sequence; nothing is implied, not even that it sees itself.  mask_words >= max_draft / 32.  NULL: j <= i
  *                            (a chain; a chunk of a prompt).  Drafted rows from max_draft on are seen by nobody
- * A token that sees no row gives zeros.  A row that a token does not see has no effect on it, whatever is in the row (NaN,
- * infinities).  out 16-byte aligned, out_f32 NULL or 16-byte aligned.  n_tokens * Hq < 2^24.
- * scratch: device memory of the caller, 256-byte aligned, of hata_tree_scratch_bytes for the same numbers or larger ones; it carries nothing from
- * one call to the next, and calls that may overlap need one each.  (It is not part of the context's workspace: contexts that never draft do
- * not pay for it.)  No residency needed, no in-kernel waits. */
+ * A token that sees no row, or only rows whose scores are -inf, gives zeros.  A row that a token does not see has no effect on it,
+ * whatever is in the row (NaN, infinities).  out 16-byte aligned, out_f32 NULL or 16-byte aligned.  n_tokens * Hq < 2^24.
+ * scratch: device memory of the caller, 256-byte aligned, of hata_tree_scratch_bytes for the same numbers or larger ones (9 MB where
+ * max_draft * Hq / Hkv <= 32, else 68 MB); it carries nothing from one call to the next, and calls that may overlap need one each.  (It is
+ * not part of the context's workspace: contexts that never draft do not pay for it.)  No residency needed, no in-kernel waits. */
 int hata_tree_scratch_bytes(const hata_ctx* ctx, int32_t B, int32_t n_tokens, int32_t max_draft, size_t* out);
 int hata_dense_tree_paged(hata_ctx* ctx, const void* q, const void* K_pool, const void* V_pool, const int32_t* block_table,
                           int32_t max_blocks, int32_t page_rows, int32_t n_pages, const int32_t* base_len, const int32_t* seq_len,

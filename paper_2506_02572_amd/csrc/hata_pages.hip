@@ -294,7 +294,8 @@ __global__ __launch_bounds__(256) void write_few_kernel(const WriteSlots a) {
 }
 
 // The same with the keys rotated on the way, through LDS, and one workgroup more for every KV head: the queries of its group.  A thread
-// has a piece of a row (RotaryPiece).
+// has a piece of a row (RotaryPiece), and a workgroup's angles are worked out once, a pair and row a thread, while weights and rows come.
+// Bound by latencies: 64 rows, eight KV heads of four, r = 128, 6.6 us, of which write_few_kernel takes 5.7.
 template <int COLS>
 __global__ __launch_bounds__(256) void rotate_write_few_kernel(const WriteSlots a) {
     constexpr int WPS = COLS / 32;
@@ -363,7 +364,7 @@ __global__ __launch_bounds__(256) void rotate_write_few_kernel(const WriteSlots 
 // says nothing, because they are as large or as small as the numbers get, infinite or NaN, are evaluated in fp64 as a whole.
 //
 // Bound by the bytes it moves (512 read and 512 written a row), then by the products, which do not overlap with them on this
-// device: those 20711 rows 37.2 us, 4.65 TB/s, where a large copy reaches 4.8; 16384 rows of 32 heads, r = 256, 144 us, 3.9 TB/s.  (Three planes, split
+// device: those 20711 rows 37.2 us, 4.65 TB/s, where a large copy reaches 4.8; 16384 rows of 32 heads, r = 256, 135 us, 4.1 TB/s.  (Three planes, split
 // here by every workgroup, where the weights are not prepared: 42.9 and 168 us.)
 // Rounds of resident workgroups (write_rows_per_wg): 45.4 us with twice as many of half the rows.
 #define WRITE_ERROR 0x1p-16f
@@ -372,7 +373,9 @@ __global__ __launch_bounds__(256) void rotate_write_few_kernel(const WriteSlots 
 #define WRITE_DOUBTS 512
 // (codes of r = 32 in stages of twice the rows leave no room for more)
 constexpr int write_max_rows(int r, bool held) { return held && r > 32 ? HELD_MAX_ROWS : WRITE_MAX_ROWS; }
-// HELD: the rows lie in their slots already (rotated, by the launch before: read from the caches), and their codes alone are wanted.
+// HELD: the rows lie in their slots already (rotated, by the launch before: read from the caches), and their codes alone are wanted.  Rows
+// go one way only, so that two stages are requested ahead and the next one is put into LDS beside this one's products: 16411 rows,
+// eight heads, r = 128, 24 us; 8192 rows of 32 heads, r = 256, 63.
 template <int R, bool F16, bool HELD>
 __global__ __launch_bounds__(R <= 128 ? 256 : 512, 2) void write_mfma_kernel(const WriteSlots a, const uint4* __restrict__ planes, int rows_per_wg) {
     constexpr int COLW = R / 32, KP = R >= 128 ? 1 : 128 / R;  // waves by columns, by rows
@@ -702,7 +705,8 @@ hipError_t launch_write_slots(const hata_ctx* c, const void* K_new, const void* 
 
 // With rotation: few rows in one launch; without codes in that of hata_rotate; many with codes there, and the codes behind it from the
 // slots.  (Rotated between load and products, a key's angles are worked out once for every KV head, 1700 instructions of the
-// vector ALU for 64 rows and wave: 16411 rows, eight heads, with 32 of queries 113 us; 8192 rows of 32 heads, r = 256, 157.)
+// vector ALU for 64 rows and wave: 16411 rows, eight heads, with 32 of queries 113 us, as here 102; 8192 rows of 32 heads,
+// r = 256, 157 and 131.)
 hipError_t launch_rotate_write(const hata_ctx* c, const RotateRows& rows, uint32_t* codes, const float* W_H, hipStream_t s) {
     const hata_config& f = c->cfg;
     const WriteSlots all = {rows.K_new, rows.V_new, rows.slots, rows.K, rows.V, codes, W_H, rows.kv_st, rows.kv_sh, rows.n, f.Hkv, f.r, rows.shift,

@@ -10,7 +10,8 @@ namespace hata {
 
 // A wave has a packed row and `per` of its heads, eight at a time: lane = (head % 8, piece of 32 bytes).  The angles of the
 // row's pairs, one a lane, pass through LDS.  Bound by the bytes, 256 read and written a row and head: the requests of ROTATE_BATCH
-// times eight heads are outstanding together.
+// times eight heads are outstanding together.  All heads by one wave from 2048 rows on (the angles once), else eight, or a few rows would
+// be as many waves: one row of 40 heads 3.4 us (the host needs 5 a call), 6001 rows of 72 heads 45 us, 4.9 TB/s, where a large copy reaches 4.8.
 #define ROTATE_WAVES 4
 #define ROTATE_BATCH 3
 

@@ -1,5 +1,20 @@
 // Decode attention of many query rows over rows that they have in common (hata_prefix.hip: of sequences behind one prompt,
-// hata_tree.hip: of one sequence's drafted tokens).
+// hata_tree.hip: of one sequence's drafted tokens): sums l_i and o_i of the weights 2^(s_in - m_i) of a run of rows n.
+//
+//   - A workgroup of four waves has a tile of 64 WQ query rows and a run of rows.  A wave holds 64 query rows (operands and sums:
+//     192 registers) and goes over 32 rows at a time on v_mfma_f32_32x32x16_bf16: S^T = K Q^T, O^T += V^T P^T.  In S^T a lane has 16
+//     rows of ONE query row, which are what the second product wants from it as P: nothing crosses lanes.
+//   - WQ waves share what they read (rows come into LDS by direct loads, 64 of K and of V a stage), 4 / WQ go over different rows.
+//   - The maximum is followed loosely: scaling a wave's sums takes 1500 cycles, as much as two thirds of the products of 32 rows, so the
+//     reference m_i is set PREFIX_LOOSE (binary) orders above the highest score when one passes it.  Weights are at most 1 all the same,
+//     and as floating-point numbers keep their precision; what is lost are weights 2^-70 of the largest, and values below 2^-70.
+//     (32 sequences behind 32768 rows, 256 heavy ones behind 16384, us with 32, 40 and 56 orders: 77.9 / 74.0 / 70.8, 282 / 277 / 274)
+//   - A weight is two bf16 terms, the upper half of its bits and the rest to nearest (2^-16 relative together; their sum is of the terms),
+//     as in dense_kernel with four heads and more: the fp32 output is as exact as without groups (2-norm of the error, 2112
+//     rows: 3.6e-6, and 6.7e-6 without, where the second term is cut off; 1.9e-7 with the fp32 weights that own rows of fewer heads have).
+//     One term, 2^-8, is a third less to multiply, but made the fp32 output as coarse as the bf16 one: 32 sequences behind 32768 rows, 72
+//     in three groups, 12 behind 131072 and 256 behind 16384 took 65, 170, 109 and 224 us with it, on one card in turn 72, 183, 112 and
+//     280 with two.  The matrix cores bound groups of more than some 140 query rows a KV head.
 #pragma once
 #include "hata_attn_core.h"
 #include "hata_device.h"

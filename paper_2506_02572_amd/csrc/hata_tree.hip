@@ -1,4 +1,13 @@
 // Attention of drafted tokens on block tables (hata_dense_tree_paged), and the rows of the accepted ones (hata_keep_rows).
+//
+// Token i of a sequence of `base` committed rows:  o_i = sum_n w_in V_n / sum_n w_in,  w_in = exp(scale q_i . K_n), over n < base and those
+// drafted rows that i sees.  All tokens read the committed rows, so the tokens and the G heads of a KV head are the query rows of one
+// matrix (hata_shared_rows.h), the rows are read once for up to 256 of them, and the mask costs only in the tiles that have drafted rows:
+// there a score that is not seen becomes -inf in its register.  Bound by the bytes up to some 100 query rows, by the products behind
+// that; they add on this device, and the products count 1.5 times, for the weights' second term.  32 sequences of 8192 rows and eight KV
+// heads, G = 4, us with 1, 8, 16, 32 and 64 tokens each: 171, 170, 196, 295 and 491 (the rows alone, at 6.1 TB/s: 176).  A token
+// and head at a time (the first form) 22400 us for what takes 252 here: 16 sequences of up to 16384 rows, the last up to 33 of them
+// drafted, eight KV heads, G = 8.
 #include <algorithm>
 #include "hata_attn_core.h"
 #include "hata_device.h"
@@ -7,7 +16,7 @@
 
 namespace hata {
 
-// Row n of sequence b in the pools: the row of head h of its page is row_of(n) * 1 (in rows of HATA_D values)
+// Row n of sequence b and KV head h in the pools, in rows of HATA_D values
 __device__ __forceinline__ int pool_row(const PageView& pv, int b, int n, int h, int Hkv) {
     const int page = clampi(pv.table[(int64_t)b * pv.max_blocks + (n >> pv.shift)], 0, pv.n_pages - 1);
     return ((page * Hkv + h) << pv.shift) + (n & ((1 << pv.shift) - 1));
@@ -261,7 +270,10 @@ __global__ __launch_bounds__(256, 1) void tree_kernel(const TreeArgs a) {
     if (tid == 0) a.splits[wg] = split;
 }
 
-// The results of the units that several workgroups have, joined: eight query rows a workgroup, half a wave each
+// The results of the units that several workgroups have, joined: eight query rows a workgroup, half a wave each.  A launch of its own,
+// because a workgroup that waited for the others' parts would need them resident.  Bound by latencies: 4 us of nothing but the
+// launch, the record, the parts; 8.5 for 150 units of two parts (15 with 16 parts requested together, whatever there were, in 121
+// registers, by which half as many workgroups were resident; 10.3 with half the workgroups and twice the rows each).
 #define TREE_MERGE_ROWS 8
 #define TREE_MERGE_BATCH 8  // partial results requested together
 #define TREE_MERGE_FEW 4     // up to so many without LDS
@@ -375,7 +387,9 @@ hipError_t launch_tree(const TreeArgs& args, void* scratch, hipStream_t s) {
 //
 // A workgroup has some KV heads of a sequence.  The rows' places are looked up once for all of them; then rows go as many at a time as the
 // threads have registers for, all read before the first is written: a path's rows move to the front only, so rows that are still to be
-// read are never written.  Bound by latency: lengths and path, places, rows, one after the other.
+// read are never written.  Bound by latency: lengths and path, places, rows, one after the other: 8 sequences 3.5 us (the host needs 5.5 a
+// call), 256 sequences with paths of up to 12, eight KV heads,
+// r = 256, 5.6 us (a workgroup a head, every place looked up by every thread, 19).
 __global__ __launch_bounds__(256) void keep_rows_kernel(const KeepRows a) {
     __shared__ int s_from[HATA_TREE_MAX_DRAFT], s_to[HATA_TREE_MAX_DRAFT];  // row of the first KV head in the pools; -1: is there already
     __shared__ int s_kept;

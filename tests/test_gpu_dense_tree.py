@@ -96,8 +96,9 @@ class Drafts:
         import torch
         return torch.from_numpy(self.table[b, n // self.P].astype(np.int64)).cuda(), torch.from_numpy(n % self.P).cuda()
 
-    def exact(self):
-        """Outputs; sums of weight times absolute value; the largest sum of absolute products of a row (of scores in units of 1)."""
+    def exact(self, committed=True):
+        """Outputs; sums of weight times absolute value; the largest sum of absolute products of a row (of scores in units of 1).
+        committed False: without the committed rows."""
         import torch
         out = torch.zeros((self.T, self.Hq, D), dtype=torch.float64, device="cuda")
         size, products = torch.zeros_like(out), torch.zeros((self.T, self.Hq, 1), dtype=torch.float64, device="cuda")
@@ -106,6 +107,7 @@ class Drafts:
             if n == 0 or L == 0:
                 continue
             see = torch.ones((n, L), dtype=torch.bool, device="cuda")
+            see[:, :self.base[b]] = committed
             see[:, self.base[b]:] = torch.from_numpy(self.seen[b]).cuda()
             page, row = self.where(b, np.arange(L))
             K, V = self.K[page, :, row].double(), self.V[page, :, row].double()
@@ -253,6 +255,19 @@ def test_rows_that_a_token_does_not_see(hata, what, base, draft):
             p = torch.softmax((K[rows, h // s.G] * s.q[t, h].double()).sum(1) * s.scale, 0)
             want = (p[:, None] * V[rows, h // s.G]).sum(0)
             assert torch.equal(torch.isfinite(want), torch.isfinite(s.out32[t, h])), (t, h)
+    s.ctx.close()
+
+
+@pytest.mark.parametrize("draft", [1, 40])
+def test_scores_of_minus_infinity(hata, draft):
+    """Committed rows whose scores are -inf count for nothing; a token that sees no other row gives zeros, and no NaN."""
+    s = Drafts(hata, [5000], [draft], mask="any", seed=draft, outliers=False)
+    s.q.copy_(s.q.abs() + 1)  # (above zero: every product with -inf is -inf)
+    page, row = s.where(0, np.arange(5000))
+    s.K[page, :, row] = -math.inf
+    s.check(s.exact(committed=False))
+    blind = [int(s.start[0]) + i for i in range(draft) if not s.seen[0][i].any()]
+    assert blind and not bool(s.out32[blind].any())
     s.ctx.close()
 
 
