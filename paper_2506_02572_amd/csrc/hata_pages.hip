@@ -655,9 +655,7 @@ static int write_rows_per_wg(int n, int Hkv, int r, bool held) {
     return (int)per * 64;
 }
 
-static bool write_on_matrix_cores(const WriteSlots& a, int n_tokens) {
-    return a.codes && n_tokens > HATA_WRITE_FEW && (a.r == 32 || a.r == 64 || a.r == 128 || a.r == 256);
-}
+static bool has_matrix_form(int r) { return r == 32 || r == 64 || r == 128 || r == 256; }
 template <bool HELD>
 static hipError_t launch_write_mfma(const hata_ctx* c, const WriteSlots& a, hipStream_t s) {
     // the weight planes prepared for exactly this weight tensor, if any
@@ -687,7 +685,7 @@ hipError_t launch_write_slots(const hata_ctx* c, const void* K_new, const void* 
         a.V_new += t0 * stride_t;
         a.slots += t0;
         a.n = std::min(most, n_tokens - t0);
-        if (write_on_matrix_cores(a, n_tokens)) {
+        if (codes && n_tokens > HATA_WRITE_FEW && has_matrix_form(f.r)) {
             const hipError_t e = launch_write_mfma<false>(c, a, s);
             if (e != hipSuccess) return e;
             if (n_tokens - t0 <= most) break;
@@ -703,16 +701,23 @@ hipError_t launch_write_slots(const hata_ctx* c, const void* K_new, const void* 
     return hipSuccess;
 }
 
-// With rotation: few rows in one launch; without codes in that of hata_rotate; many with codes there, and the codes behind it from the
-// slots.  (Rotated between load and products, a key's angles are worked out once for every KV head, 1700 instructions of the
+// With rotation: without codes in the launch of hata_rotate; with codes either in one launch, or there, and the codes behind it from the
+// slots.  One launch takes 7.3 us and 2.8 for every further workgroup a compute unit has, two take 10 to 12 us as long as rows are few.
+// One and two launches, us (32 query heads, eight KV heads, r = 128 unless said): 129 rows (216 workgroups) 7.4 and 10.1, 256 (384) 10.2 and
+// 10.6, 384 (576) 12.1 and 11.1, 1024 (1536) 23 and 15; r = 64, 512 rows (512) 10.3 and 11.1, 768 (768) 13.4 and 12.7; r = 256,
+// 192 (480) 10.4 and 10.7, 256 (640) 13.4 and 11.4; one KV head, r = 32, 2048 (256) 7.4 and 18; 32 KV heads, r = 256, 48 rows (480) 10.1,
+// 129 (1440) 19 and 11.6.
+// (Rotated between load and products, a key's angles are worked out once for every KV head, 1700 instructions of the
 // vector ALU for 64 rows and wave: 16411 rows, eight heads, with 32 of queries 113 us, as here 102; 8192 rows of 32 heads,
 // r = 256, 157 and 131.)
+#define WRITE_ROTATED_WGS 512  // two a compute unit
 hipError_t launch_rotate_write(const hata_ctx* c, const RotateRows& rows, uint32_t* codes, const float* W_H, hipStream_t s) {
     const hata_config& f = c->cfg;
     const WriteSlots all = {rows.K_new, rows.V_new, rows.slots, rows.K, rows.V, codes, W_H, rows.kv_st, rows.kv_sh, rows.n, f.Hkv, f.r, rows.shift,
                             rows.rows, {rows.freq, rows.positions, rows.magnitude, rows.dims, rows.interleaved}, rows.x, rows.out, rows.st, rows.sh, c->G};
     if (!codes) return launch_rotate(rows, s);
-    const bool many = write_on_matrix_cores(all, rows.n);
+    const int cols = f.r % 64 == 0 ? 64 : 32, columns = f.r / cols + (rows.heads ? 1 : 0);
+    const bool many = has_matrix_form(f.r) && (int64_t)columns * f.Hkv * ((rows.n + WRITE_ROWS - 1) / WRITE_ROWS) > WRITE_ROTATED_WGS;
     if (many) {
         const hipError_t e = launch_rotate(rows, s);
         if (e != hipSuccess) return e;
@@ -731,9 +736,8 @@ hipError_t launch_rotate_write(const hata_ctx* c, const RotateRows& rows, uint32
         if (many) {
             e = launch_write_mfma<true>(c, a, s);
         } else {
-            const int cols = f.r % 64 == 0 ? 64 : 32;
             hipLaunchKernelGGL((cols == 64 ? rotate_write_few_kernel<64> : rotate_write_few_kernel<32>),
-                               dim3(f.r / cols + (rows.heads ? 1 : 0), f.Hkv, (a.n + WRITE_ROWS - 1) / WRITE_ROWS), dim3(256), 0, s, a);
+                               dim3(columns, f.Hkv, (a.n + WRITE_ROWS - 1) / WRITE_ROWS), dim3(256), 0, s, a);
             e = hipGetLastError();
         }
         if (e != hipSuccess) return e;

@@ -115,7 +115,11 @@ def test_layouts_of_pairs(hata, T, dims, interleaved):
 @pytest.mark.parametrize("T,Hq,Hkv,r,P,fused,prepared", [
     (33, 32, 8, 128, 64, True, True), (200, 40, 8, 128, 256, False, True), (260, 32, 32, 256, 16, True, False),
     (1500, 64, 8, 128, 64, True, False), (140, 16, 1, 64, 32, False, False), (700, 8, 8, 32, 1024, True, True), (7, 24, 8, 256, 16, True, True),
-    (3000, 32, 8, 128, 64, True, True), (2100, 4, 1, 256, 16, False, True)])
+    (3000, 32, 8, 128, 64, True, True), (2100, 4, 1, 256, 16, False, True),
+    # many rows of few heads in one launch, few of many in two, and either side of where that changes
+    (2048, 8, 1, 32, 64, True, True), (4096, 8, 1, 32, 64, True, True), (4097, 8, 1, 32, 64, False, False), (64, 32, 32, 256, 16, True, True),
+    (48, 32, 32, 256, 64, False, False), (49, 32, 32, 256, 64, True, False), (17, 64, 64, 256, 16, True, True), (512, 16, 8, 64, 32, True, True),
+    (513, 16, 8, 64, 32, True, True)])
 def test_heads_pages_and_weights(hata, T, Hq, Hkv, r, P, fused, prepared):
     s = Rows(hata, T, Hq, Hkv, r, P, fused=fused, prepared=prepared, seed=P)
     s.call()
