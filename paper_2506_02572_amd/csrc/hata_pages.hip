@@ -401,7 +401,7 @@ __global__ __launch_bounds__(R <= 128 ? 256 : 512, 2) void write_mfma_kernel(con
     [[maybe_unused]] uint4 vpre[NIT];
     int slot[BUFS][NIT];
     [[maybe_unused]] int slot_next[NIT];
-    [[maybe_unused]] auto load_slots = [&](int t0) {
+    [[maybe_unused]] auto load_slots = [&](int t0) __attribute__((always_inline)) {
 #pragma unroll
         for (int it = 0; it < NIT; ++it) {
             const int t = t0 + it * ROWS_PER_IT + lrow;
@@ -409,7 +409,8 @@ __global__ __launch_bounds__(R <= 128 ? 256 : 512, 2) void write_mfma_kernel(con
             if (t >= last) slot_next[it] = -1;
         }
     };
-    auto load_stage = [&](int t0, uint4 (&x)[NIT], int (&to)[NIT]) {
+    // (inlined, or what they refer to lies in memory: 16411 rows, eight heads, r = 32, rotated, 132 -> 90 us)
+    auto load_stage = [&](int t0, uint4 (&x)[NIT], int (&to)[NIT]) __attribute__((always_inline)) {
         if constexpr (HELD) {
             if (t0 >= last) return;
 #pragma unroll
@@ -483,7 +484,7 @@ __global__ __launch_bounds__(R <= 128 ? 256 : 512, 2) void write_mfma_kernel(con
 
     const int row0 = part * 32 * NT;
     // the rows requested, of the stage at t0, into LDS (and into their slots)
-    auto put_stage = [&](int t0, const uint4 (&rows)[NIT], const int (&slots)[NIT], uint16_t* tile, float* s_norm) {
+    auto put_stage = [&](int t0, const uint4 (&rows)[NIT], const int (&slots)[NIT], uint16_t* tile, float* s_norm) __attribute__((always_inline)) {
 #pragma unroll
         for (int it = 0; it < NIT; ++it) {
             const int row = it * ROWS_PER_IT + lrow;
@@ -703,10 +704,10 @@ hipError_t launch_write_slots(const hata_ctx* c, const void* K_new, const void* 
 
 // With rotation: without codes in the launch of hata_rotate; with codes either in one launch, or there, and the codes behind it from the
 // slots.  One launch takes 7.3 us and 2.8 for every further workgroup a compute unit has, two take 10 to 12 us as long as rows are few.
-// One and two launches, us (32 query heads, eight KV heads, r = 128 unless said): 129 rows (216 workgroups) 7.4 and 10.1, 256 (384) 10.2 and
-// 10.6, 384 (576) 12.1 and 11.1, 1024 (1536) 23 and 15; r = 64, 512 rows (512) 10.3 and 11.1, 768 (768) 13.4 and 12.7; r = 256,
-// 192 (480) 10.4 and 10.7, 256 (640) 13.4 and 11.4; one KV head, r = 32, 2048 (256) 7.4 and 18; 32 KV heads, r = 256, 48 rows (480) 10.1,
-// 129 (1440) 19 and 11.6.
+// One and two launches, us, and workgroups (32 query heads, eight KV heads, r = 128 unless said): 129 rows (216) 7.5 and 10.0, 256 (384)
+// 10.1 and 10.7, 384 (576) 12.2 and 11.1, 1024 (1536) 23 and 15; r = 64, 512 rows (512) 10.3 and 11.1, 768 (768) 13.4 and 12.7; r = 256, 192
+// (480) 10.4 and 10.7, 256 (640) 13.4 and 11.5; one KV head, r = 32, 2048 (256) 7.5 and 13; 32 KV heads, r = 256, 48 (480) 10.4 and 10.8, 64
+// (640) 13.3 and 10.9, 128 (1280) 20 and 11.2.
 // (Rotated between load and products, a key's angles are worked out once for every KV head, 1700 instructions of the
 // vector ALU for 64 rows and wave: 16411 rows, eight heads, with 32 of queries 113 us, as here 102; 8192 rows of 32 heads,
 // r = 256, 157 and 131.)
