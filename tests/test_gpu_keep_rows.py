@@ -112,6 +112,28 @@ def test_paths_that_break_off(hata):
     s.ctx.close()
 
 
+def test_pools_beyond_4_gb(hata):
+    """A path in the last pages of pools of more than 2^32 bytes: as in pools that are those pages alone."""
+    import torch
+    s = Caches(hata, [700, 90], [60, 40], Hkv=8, r=128, P=256, seed=5)
+    path = np.tile(np.arange(1, 33, dtype=np.int32), (2, 1))
+    s.check(path, [32, 20])
+    n, before = 9000, 9000 - s.n_pages
+    big = []
+    for p in (s.K, s.V, s.codes):
+        t = torch.empty((n,) + p.shape[1:], dtype=dev(p).dtype, device="cuda")
+        t[before:] = dev(p)
+        big.append(t)
+    assert big[0].numel() > 2 ** 31
+    t = dev(np.where((s.table >= 0) & (s.table < s.n_pages), s.table + before, s.table).astype(np.int32))
+    out = torch.full((3,), -5, dtype=torch.int32, device="cuda")
+    s.ctx.hata_keep_rows(*big, t, s.width, s.P, n, s.ints[1], s.ints[2], 2, dev(path), dev(np.asarray([32, 20], np.int32)), 32, out)
+    torch.cuda.synchronize()
+    for a, b in zip(s.dev, big):
+        assert torch.equal(a, b[before:])
+    assert torch.equal(out, s.out)
+
+
 def test_lengths_out_of_range(hata):
     """Lengths are clamped to the cache (base_len <= seq_len <= min(L_cap, table)), pages to the pools; nothing else is touched."""
     import torch

@@ -168,6 +168,59 @@ def test_a_key_has_one_row_and_one_code(hata, T):
     s.ctx.close()
 
 
+@pytest.mark.parametrize("T", [40, 1500])
+def test_pools_beyond_4_gb(hata, T):
+    """Rows in the last pages of pools of more than 2^32 bytes: as in pools that are those pages alone."""
+    import torch
+    few = Rows(hata, T, 32, 8, 128, 256, seed=21)
+    few.slots[few.slots >= few.n_pages * 256] = -1
+    few.call()
+    few.check()
+    many = Rows(hata, T, 32, 8, 128, 256, seed=21)
+    many.n_pages = 9000
+    before = many.n_pages - few.n_pages
+    many.slots = np.where(few.slots >= 0, few.slots + before * 256, -1).astype(np.int32)
+    held = [(t, torch.empty((many.n_pages,) + tuple(t.shape[1:]), dtype=t.dtype, device="cuda")) for t in (many.K, many.V, many.codes)]
+    for small, big in held:
+        big[before:] = small
+    many.K, many.V, many.codes = (big for _, big in held)
+    assert many.K.numel() > 2 ** 31
+    many.call()
+    for a, b in ((few.K, many.K), (few.V, many.V), (few.codes, many.codes)):
+        assert torch.equal(a, b[before:])
+    assert torch.equal(few.q_out, many.q_out)
+
+
+def test_more_rows_than_a_launch_has(hata):
+    """More than 2^20 rows in a call, as the same in calls of a third each."""
+    import torch
+    T, P, Hq, Hkv, r = (1 << 20) + 4321, 1024, 2, 1, 32
+    n_pages = -(-T // P) + 1
+    g = torch.Generator(device="cuda").manual_seed(3)
+    x = torch.randn((T, Hq + 2 * Hkv, D), device="cuda", generator=g).to(torch.bfloat16)
+    slots = torch.randperm(n_pages * P, device="cuda", generator=g)[:T].to(torch.int32)
+    positions = torch.randint(0, 1 << 20, (T,), device="cuda", generator=g, dtype=torch.int32)
+    W = torch.randn((Hkv, D, r), device="cuda", generator=g)
+    ctx, rotary = hata.Context(1, Hq, Hkv, D, r, 64, 64), hata.Rotary.scaled(D, 10000.0)
+    results = []
+    for pieces in ([T], [T // 3, T // 3, T - 2 * (T // 3)]):
+        K, V = (torch.zeros((n_pages, Hkv, P, D), dtype=torch.bfloat16, device="cuda") for _ in range(2))
+        codes, q_out = torch.zeros((n_pages, Hkv, P, r // 32), dtype=torch.int32, device="cuda"), torch.zeros((T, Hq, D), dtype=torch.bfloat16, device="cuda")
+        t = 0
+        for n in pieces:
+            part = x[t:t + n]
+            q, k, v = part[:, :Hq], part[:, Hq:Hq + Hkv], part[:, Hq + Hkv:]
+            ctx.hata_rotate_write_slots(q, x.stride(0), x.stride(1), q_out[t:], k, v, x.stride(0), x.stride(1), positions[t:], slots[t:], n,
+                                        rotary, K, V, codes, P, n_pages, W)
+            t += n
+        torch.cuda.synchronize()
+        results.append((K, V, codes, q_out))
+    for a, b in zip(*results):
+        assert torch.equal(a.view(torch.int16) if a.dtype == torch.bfloat16 else a, b.view(torch.int16) if b.dtype == torch.bfloat16 else b)
+    assert torch.equal(results[0][1].transpose(1, 2).reshape(-1, D)[slots.long()], x[:, 3])
+    ctx.close()
+
+
 @pytest.mark.parametrize("T", [64, 400])
 def test_values_out_of_the_ordinary(hata, T):
     """Rows of zeros, of the smallest and largest numbers and of infinities beside ordinary ones; weights of zeros."""
