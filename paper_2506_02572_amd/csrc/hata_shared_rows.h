@@ -161,7 +161,8 @@ __device__ __forceinline__ void shared_rows(const Args& a, const Work& w, char* 
     for (int i = 0; i < 4; ++i) off[i] = (4 * i + (lane >> 4)) * 256 + ((lane & 15) ^ (lane >> 4 << 2 | i)) * 16;
     // (written as instructions: behind the compiler's builtin for it, every LDS read waits for all requests.  nt where the rows are read
     // by one tile of query rows, mostly: 12 sequences behind 131072 rows 119 -> 108 us, 32 behind 32768 68 -> 63; with eight tiles
-    // it is the same, and slower where the caches hold the rows already)
+    // it is the same, and slower where the caches hold the rows already.  Drafted tokens are one tile mostly: 32 sequences of 8192 rows with
+    // 64 tokens 455 -> 449; 16 of 4096 with 256 tokens of 64 heads, eight tiles, 906 -> 918)
     auto fetch = [&](uint32_t dst, uint32_t o, const uint16_t* p) {
         if constexpr (WQ <= 2 || DRAFT)
             asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2 nt" ::"s"(dst), "v"(o), "s"(p) : "memory", "m0");
