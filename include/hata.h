@@ -397,7 +397,8 @@ typedef struct {
  *   BANDS   by the turns that a pair makes over the original context, original * freq / (2 pi): from `high` turns on kept, up to `low`
  *           divided by factor, in between a mean of both, weighted linearly by the turns
  *   RAMP    the same by the pair's number, linearly between the pair that makes `high` turns (rounded down) and the one that makes `low`
- *           (rounded up), found from freq[i] = base^(-2 i / dims); *magnitude = 0.1 ln(factor) + 1 for factor > 1
+ *           (rounded up), found from freq[i] = base^(-2 i / dims), at least pair 0 and at most pair dims - 1: behind the last pair, dims / 2 - 1,
+ *           where that still makes more than `low` turns; *magnitude = 0.1 ln(factor) + 1 for factor > 1
  * HATA_EUNSUPPORTED for dims as above, HATA_EINVAL for a base not above 1, a factor or original not above 0, high not above low > 0. */
 typedef enum { HATA_ROTARY_NONE = 0, HATA_ROTARY_LINEAR = 1, HATA_ROTARY_BASE = 2, HATA_ROTARY_BANDS = 3, HATA_ROTARY_RAMP = 4 } hata_rotary_kind;
 typedef struct {

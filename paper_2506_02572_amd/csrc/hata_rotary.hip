@@ -119,7 +119,8 @@ int rotary_frequencies(int pairs, double base, const hata_rotary_scaling* sc, do
         }
     } else if (sc && sc->kind == HATA_ROTARY_RAMP) {
         auto at = [&](double turns) { return pairs * log(sc->original / (turns * two_pi)) / log(base); };
-        const double first = std::max(floor(at(sc->high)), 0.0), last = std::min(ceil(at(sc->low)), (double)(pairs - 1));
+        const double first = std::max(floor(at(sc->high)), 0.0), last = std::min(ceil(at(sc->low)), 2.0 * pairs - 1.0);
+        // (`last` may lie behind the last pair, up to dims - 1: a pair that still makes more than `low` turns is on the ramp, not at its end)
         for (int i = 0; i < pairs; ++i) {
             const double keep = 1.0 - std::min(std::max((i - first) / std::max(last - first, 1e-3), 0.0), 1.0);
             freq[i] = freq[i] * keep + freq[i] / sc->factor * (1.0 - keep);

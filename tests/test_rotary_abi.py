@@ -64,3 +64,30 @@ def test_frequencies_refused():
     assert call(kind=1, low=0.0, original=0.0) == 0  # (not of this kind)
     with pytest.raises(hata.HataError):
         hata.rotary_frequencies(128, 1e4, "other")
+
+
+@pytest.mark.parametrize("dims,base,original", [(128, 10000.0, 65536.0), (128, 10000.0, 131072.0), (64, 10000.0, 65536.0), (16, 10000.0, 32768.0),
+                                                (128, 500000.0, 8192.0), (16, 10.0, 100000.0), (32, 10000.0, 150.0)])
+def test_ramps_that_end_behind_the_last_pair(dims, base, original):
+    """Where the last pair makes more than `low` turns over the original context, the ramp goes on behind it, up to pair dims - 1, and where
+    the first one makes fewer than `high` it begins at pair 0.  Every pair's share of the stretched frequency from the formula that the header
+    states: what the pair's number leaves of the distance between the two ends.  (2^-45: differences of logarithms below 2^4, of which 2^-53
+    each is lost, over at least one pair; and no share at all, or the whole, is exact.)"""
+    factor, low, high = 16.0, 1.0, 32.0
+    got = np.asarray(hata.rotary_frequencies(dims, base, "ramp", factor, low, high, original)[0])
+    turns_of = lambda i: original / (2 * math.pi) * base ** (-2.0 * i / dims)
+    ends = []
+    for turns, way in ((high, -1), (low, 1)):
+        i = 0
+        while turns_of(i) > turns and i < dims - 1:  # the pair that makes so many, rounded up ..
+            i += 1
+        if way < 0 and turns_of(i) < turns:          # .. or down
+            i = max(i - 1, 0)
+        ends.append(i)
+    first, last = ends
+    assert last > dims // 2 - 1 or first == 0 or original == 8192.0  # (what the test is about, and one in which neither acts)
+    for i in range(dims // 2):
+        stretched = min(max((i - first) / max(last - first, 1e-3), 0.0), 1.0)  # (both ends the last one: all pairs turn more than `high` times)
+        f = base ** (-2.0 * i / dims)
+        want = f * (1 - stretched) + f / factor * stretched
+        assert abs(got[i] - want) <= 2.0 ** -45 * want, (i, got[i] / want)
