@@ -620,7 +620,8 @@ __device__ __forceinline__ void shared_rows(const Args& a, const Work& w, char* 
                     const int r = i0 + 8 * j + r8;
                     if (r >= rows) continue;
                     const float f = s_inverse[r];
-                    o[j].x *= f; o[j].y *= f; o[j].z *= f; o[j].w *= f;
+                    // (no weight at all: zeros, also where a value that is not finite made the sums NaN)
+                    o[j] = f == 0.f ? make_float4(0.f, 0.f, 0.f, 0.f) : make_float4(o[j].x * f, o[j].y * f, o[j].z * f, o[j].w * f);
                     store_output(a.out, a.out_f32, (int64_t)(w.first * a.Hq + w.h * G + tables.row[r]) * HATA_D + c4, o[j]);
                 }
                 continue;

@@ -349,8 +349,8 @@ __global__ __launch_bounds__(256) void tree_merge_kernel(const TreeArgs a) {
         }
     }
     if (r >= u.rows) return;
-    const float f = l == 0.f ? 0.f : 1.f / l;
-    o.x *= f; o.y *= f; o.z *= f; o.w *= f;
+    const float f = 1.f / l;
+    o = l == 0.f ? make_float4(0.f, 0.f, 0.f, 0.f) : make_float4(o.x * f, o.y * f, o.z * f, o.w * f);  // (NaN too)
     store_output(a.out, a.out_f32, ((int64_t)(u.first + r / a.G) * a.Hq + u.h * a.G + r % a.G) * HATA_D + 4 * lane, o);
 }
 

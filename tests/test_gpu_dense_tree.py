@@ -410,3 +410,38 @@ def test_refusals(hata):
     assert bool((s.out == KEPT).all())
     assert call(out32=None, mask=None, words=-5) == 0
     s.ctx.close()
+
+
+def masked_by(s, seen):
+    """Sequence by sequence, `seen` in the place of the masks."""
+    import torch
+    s.seen = seen
+    bits = np.zeros((s.T, 32 * s.words), bool)
+    for b, n in enumerate(s.draft):
+        bits[s.start[b]:s.start[b + 1], :n] = seen[b]
+    s.mask = torch.from_numpy(np.packbits(bits, axis=1, bitorder="little").view(np.int32)).cuda()
+
+
+@pytest.mark.parametrize("what", [math.inf, -math.inf, math.nan])
+@pytest.mark.parametrize("base,draft,Hq,Hkv", [(0, 6, 8, 2), (40, 30, 8, 2), (5000, 12, 8, 2), (5000, 100, 8, 1), (700, 256, 8, 8)])
+def test_scores_of_minus_infinity_of_rows_that_are_not_finite(hata, what, base, draft, Hq, Hkv):
+    """A token that sees only rows whose scores are -inf gives zeros also where those rows' values are not finite: committed rows, and the first
+    drafted one.  In one workgroup, and in parts that are joined."""
+    s = Drafts(hata, [base], [draft], Hq, Hkv, mask="any", seed=draft, outliers=False)
+    s.q.copy_(s.q.abs() + 1)  # (above zero: every product with -inf is -inf)
+    page, row = s.where(0, np.arange(base + 1))
+    s.K[page, :, row] = -math.inf
+    page, row = s.where(0, np.r_[np.arange(0, base, 7), base])
+    s.V[page, :, row] = what
+    seen = s.seen[0].copy()
+    seen[1::5] = False
+    seen[1::5, 0] = True  # the first drafted row alone
+    masked_by(s, [seen])
+    s.run()
+    import torch
+    torch.cuda.synchronize()
+    blind = [int(s.start[0]) + i for i in range(draft) if not seen[i, 1:].any()]
+    assert len(blind) >= 2 + (draft - 1) // 5
+    assert not bool(s.out32[blind].any()) and not bool(s.out.view(torch.bfloat16)[blind].float().any())
+    assert bool((s.out[int(s.start[-1]):] == KEPT).all())
+    s.ctx.close()
