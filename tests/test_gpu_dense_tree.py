@@ -445,3 +445,35 @@ def test_scores_of_minus_infinity_of_rows_that_are_not_finite(hata, what, base, 
     assert not bool(s.out32[blind].any()) and not bool(s.out.view(torch.bfloat16)[blind].float().any())
     assert bool((s.out[int(s.start[-1]):] == KEPT).all())
     s.ctx.close()
+
+
+@pytest.mark.parametrize("Hq,Hkv,base,draft,mask", [
+    (64, 8, "to 3000", [1, 100, 33, 64, 40, 97, 2, 65, 32, 80, 31, 100, 50, 1, 96, 34], "tree"),  # tiles of 32 tokens, last ones of 1 to 32
+    (64, 8, "to 3000", [1, 100, 33, 64, 40, 97, 2, 65, 32, 80, 31, 100, 50, 1, 96, 34], "chain"),
+    (40, 8, "to 300", [60, 256, 51, 52, 53, 103, 153, 204], "any"),                                # of 51
+    (40, 8, "to 20000", [256, 255, 102, 60], "chain"),
+    (32, 8, "to 900", [65, 128, 129, 64, 200, 256, 1, 63, 100], "tree"),                           # of 64
+    (16, 1, "to 200", [33 if b % 3 else 17 for b in range(90)], "tree"),                           # of 16, more sequences than a wave looks at
+    (16, 1, "to 60", [(7 * b) % 50 for b in range(300)], "any"),
+    (28, 2, "to 3000", [(11 * b) % 200 for b in range(40)], "chain"),                              # of 18
+    (32, 32, "to 700", [256, 256, 255, 200], "any"),                                               # of 256: one
+])
+def test_tiles_of_tokens_in_equal_pieces(hata, Hq, Hkv, base, draft, mask):
+    """Sequences with several tiles of tokens, in batches of more than 64 units (a KV head of such a tile) or sequences: all units one behind
+    the other in equal pieces, full tiles and last ones of other weights, a tile's mask, pieces that end inside a unit."""
+    rng = np.random.default_rng(len(draft) + Hq)
+    rows = rng.integers(0, int(base[3:]), len(draft))
+    rows[len(draft) // 2], rows[0] = int(base[3:]), 0
+    per = 256 // (Hq // Hkv)
+    tiles = [-(-n // per) for n in draft]
+    assert Hkv * sum(tiles) > 64 or len(draft) > 64
+    assert max(tiles) > 1 or per == 256
+    s = Drafts(hata, rows.tolist(), draft, Hq, Hkv, mask=mask, seed=Hq, gap=1)
+    s.check()
+    first = s.out32.clone()
+    s.scratch.fill_(0xff)
+    s.run()
+    import torch
+    torch.cuda.synchronize()
+    assert torch.equal(s.out32, first)
+    s.ctx.close()
