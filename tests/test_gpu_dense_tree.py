@@ -477,3 +477,39 @@ def test_tiles_of_tokens_in_equal_pieces(hata, Hq, Hkv, base, draft, mask):
     torch.cuda.synchronize()
     assert torch.equal(s.out32, first)
     s.ctx.close()
+
+
+@pytest.mark.parametrize("L_cap,width,cap", [(100, 8, 100), (4096, 8, 128), (4096, 7, 112), (97, 8, 97)])
+@pytest.mark.parametrize("Hq,Hkv", [(8, 2), (16, 1)])
+def test_lengths_cut_and_starts_clamped(hata, L_cap, width, cap, Hq, Hkv):
+    """A cache longer than the context or the table says is cut there, starts are clamped to the packed rows, a sequence's tokens to
+    max_draft, base_len to the length: each against attention over what is left, and packed rows of no sequence as they were."""
+    s = Drafts(hata, [120, 120], [8, 8], Hq, Hkv, seed=width, L_cap=L_cap, max_draft=8)
+    s.width, s.table = width, np.ascontiguousarray(s.table[:, :width])
+    most = 2 ** 31 - 1
+
+    def case(lens, bases, starts, want_len, want_base, want_start):
+        s.args = tuple(i32(a) for a in (s.table, bases, lens, starts))
+        s.len, s.base, s.start = want_len, want_base, np.asarray(want_start)
+        s.draft = [min(int(n), 8) for n in np.diff(want_start)]
+        seen = []
+        for b in range(2):  # no token sees more than the drafted rows that are there: those of the tokens that are there
+            n = s.len[b] - s.base[b]
+            assert 0 <= n <= s.draft[b]
+            seen.append(np.random.default_rng(b).random((s.draft[b], n)) < 0.5)
+        bits = np.ones((s.T, 32), bool)
+        for b in range(2):
+            t0 = int(s.start[b])
+            bits[t0:t0 + s.draft[b], :seen[b].shape[1]] = seen[b]
+        s.seen = seen
+        import torch
+        s.mask = torch.from_numpy(np.packbits(bits, axis=1, bitorder="little").view(np.int32)).cuda()
+        s.check()
+    T = s.T
+    assert T == 19
+    case([most, most], [most, most], [-7, 5, 10 ** 6], [cap, cap], [cap, cap], [0, 5, T])      # (14 rows, eight of which are tokens)
+    case([most, cap + 1], [cap - 3, cap - 8], [0, 8, 16], [cap, cap], [cap - 3, cap - 8], [0, 8, 16])
+    case([50, -5], [60, 7], [3, 9, 12], [50, 0], [50, 0], [3, 9, 12])                          # a base behind the length, no rows at all
+    case([most, 90], [-9, 88], [0, 0, T], [0 + 0, 90], [0, 88], [0, 0, T])                     # no tokens in front: nothing of the first
+    case([cap, cap], [cap, -1], [10 ** 6, 10 ** 6, 10 ** 6], [cap, 0], [cap, 0], [T, T, T])
+    s.ctx.close()
