@@ -200,3 +200,40 @@ def test_refusals(hata):
     assert call(most=257) == -2
     assert call(codes=None) == 0 and call() == 0
     s.ctx.close()
+
+
+def heads_of_a_workgroup(B, Hkv):
+    """KV heads that a workgroup takes, so that the launch has up to 512 of them."""
+    heads = 1
+    while B * -(-Hkv // heads) > 512 and heads < Hkv:
+        heads *= 2
+    return heads
+
+
+@pytest.mark.parametrize("B,Hkv,r,P,heads", [
+    (256, 8, 256, 64, 4), (256, 8, 0, 16, 4),
+    (200, 6, 128, 16, 4), (130, 5, 32, 16, 2),      # a tail of two heads, and of one
+    (600, 3, 256, 16, 4), (520, 7, 64, 16, 8),      # all heads, no power of two, in one workgroup
+    (5, 256, 256, 16, 4), (9, 100, 32, 16, 2),      # few sequences of many heads
+    (40, 200, 32, 16, 32),                          # six workgroups of 32 heads and one of eight
+    (129, 256, 32, 16, 128), (130, 300, 256, 16, 128),  # 128 heads: a turn in two parts of them; and a tail of 44
+    (300, 140, 64, 16, 256)])                       # 140 heads, as many as 256 are laid out
+def test_several_heads_a_workgroup(hata, B, Hkv, r, P, heads):
+    """Batches in which a workgroup has several KV heads, some of them with fewer heads behind: paths of no row, of a few, and longer than a
+    turn of rows (64 divided by the heads, but at least one)."""
+    assert heads_of_a_workgroup(B, Hkv) == heads
+    rng = np.random.default_rng(B + Hkv)
+    draft = rng.integers(0, 13, B)
+    base = rng.integers(0, 2 * P if Hkv <= 8 else 8, B)
+    draft[0], base[0], draft[-1] = 12, 3, 12
+    if heads <= 8:
+        draft[1] = 200  # (several turns)
+    s = Caches(hata, base, draft, Hkv, r, P, seed=Hkv, L_cap=64 if Hkv > 8 and heads > 8 else 1024)
+    most = 100 if heads <= 8 else 12
+    path, n_path = np.full((B, most), 5, np.int64), []
+    for b, n in enumerate(draft):
+        k = int(rng.integers(0, min(n, most) + 1)) if 1 < b < B - 1 else min(int(n), most) - (b == 0)
+        path[b, :k] = np.sort(rng.permutation(n)[:k]) if b else 1 + np.arange(k)  # (the first: every source is the row behind its target)
+        n_path.append(k)
+    s.check(path, n_path)
+    s.ctx.close()
