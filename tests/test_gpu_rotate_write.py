@@ -291,3 +291,185 @@ def test_refusals(hata):
     assert bool((s.K == JUNK).all()) and bool((s.q_out == JUNK).all())
     assert call(q=None, q_out=None, qst=-1, qsh=3) == 0  # (strides of nothing)
     s.ctx.close()
+
+
+# ---- calls that go by two launches: rows rotated into the slots, and their codes from there on the matrix cores ----
+
+def launches(s, queries=True):
+    """One, or two where its workgroups would be more than two a compute unit: 16 rows and 64 hash columns of a KV head each (32 where
+    the width is no multiple of 64), and one more for its queries."""
+    columns = s.r // (64 if s.r % 64 == 0 else 32) + (1 if queries else 0)
+    return 2 if s.r in (32, 64, 128, 256) and columns * s.Hkv * -(-s.T // 16) > 512 else 1
+
+
+def check_all(s, queries=True):
+    """As Rows.check, with rows that are not finite or overflow: infinities and NaN where the formula has them, and bits of NaN 0."""
+    host = lambda t: t.cpu().numpy().view({2: np.uint16, 4: np.uint32}[t.element_size()])
+    flat = lambda t: host(t).transpose(0, 2, 1, 3).reshape(s.n_pages * s.P, s.Hkv, -1)
+
+    def held(got, bits, positions, what):
+        with np.errstate(invalid="ignore"):
+            y, size = R.turn(R.values(bits), positions, s.freq, s.m, s.interleaved)
+        whole = np.isfinite(y)
+        want = R.check(np.where(whole, got, 0).astype(np.uint16), np.where(whole, y, 0), np.where(whole, size, 1), what)
+        assert not (abs(want) >= 2.0 ** 128).any()  # (no finite row here overflows)
+        want = np.where(whole, want, y.astype(np.float64))
+        assert np.array_equal(np.isnan(R.values(got)), np.isnan(want)) and np.array_equal(R.values(got)[~np.isnan(want)], want[~np.isnan(want)]), what
+        return want
+    if queries:
+        held(host(s.q_out), s.x[:, :s.Hq], s.positions, "q")
+    else:
+        assert np.all(host(s.q_out) == JUNK)
+    live = np.flatnonzero((s.slots >= 0) & (s.slots < s.n_pages * s.P))
+    at = s.slots[live]
+    K, V, codes = flat(s.K), flat(s.V), flat(s.codes)
+    keys = held(K[at], s.x[live, s.Hq:s.Hq + s.Hkv], s.positions[live], "K")
+    assert np.array_equal(V[at], s.x[live, s.Hq + s.Hkv:])
+    with np.errstate(invalid="ignore"):
+        want = np.stack([keys[:, h] @ s.W[h].astype(np.float64) >= 0 for h in range(s.Hkv)], 1)  # (NaN: false)
+    assert np.array_equal(codes[at], np.packbits(want, axis=2, bitorder="little").view(np.uint32))
+    rest = np.setdiff1d(np.arange(s.n_pages * s.P), at)
+    assert np.all(K[rest] == JUNK) and np.all(V[rest] == JUNK) and np.all(codes[rest] == 77)
+    return live
+
+
+@pytest.mark.parametrize("T,Hq,Hkv,r", [(64, 2, 1, 128), (3000, 2, 1, 128), (3100, 4, 2, 64), (9000, 2, 1, 32), (1000, 2, 2, 256), (500, 4, 4, 256)])
+@pytest.mark.parametrize("prepared", [True, False])
+@pytest.mark.parametrize("interleaved", [False, True])
+def test_rows_out_of_the_ordinary_by_one_launch_and_two(hata, T, Hq, Hkv, r, prepared, interleaved):
+    """Rows of zeros, of the smallest and large numbers, of infinities, of NaN, all over the workgroups' rows; columns of zero weights."""
+    s = Rows(hata, T, Hq=Hq, Hkv=Hkv, r=r, seed=8, far=50, prepared=prepared, interleaved=interleaved)
+    assert launches(s) == (1 if T == 64 else 2)
+    rng = np.random.default_rng(T)
+    s.positions[::7] = 0  # (an angle of zero: what is infinite makes its pair NaN)
+    keys = s.x[:, Hq:Hq + Hkv]
+    kinds = rng.permutation(T)[:max(T // 3, 18)]  # a third of the rows, some of every kind
+    for i, t in enumerate(kinds):
+        kind = i % 9
+        if kind == 0:
+            keys[t] = 0
+        elif kind == 1:
+            keys[t] = 0x8000
+        elif kind == 2:
+            keys[t] = rng.choice(np.array([0x0001, 0x8001, 0x0003, 0x0080, 0], np.uint16), keys[t].shape)  # subnormals
+        elif kind == 3:
+            keys[t] = 0x0100
+        elif kind == 4:
+            keys[t] = rng.choice(np.array([0x7e00, 0xfe00, 0x7d33], np.uint16), keys[t].shape)
+        elif kind == 5:
+            keys[t, :, rng.integers(D)] = 0x7f80
+        elif kind == 6:
+            keys[t, :, rng.integers(D)] = 0xff80
+        elif kind == 7:
+            keys[t, :, [3, 3 + D // 2]] = 0x7f80  # a pair of halves
+            keys[t, :, [10, 11]] = 0xff80         # and of neighbours
+        else:
+            keys[t, :, rng.integers(D)] = 0x7fc0
+    s.W[:, :, 5], s.W[:, :, r - 1] = 0.0, 0.0
+    s.Wd.copy_(dev(s.W))
+    if prepared:
+        s.ctx.hata_prepare_weights(s.Wd)
+    s.call()
+    live = check_all(s)
+    assert len(np.intersect1d(live, kinds)) > len(kinds) // 2
+    s.ctx.close()
+
+
+@pytest.mark.parametrize("interleaved", [False, True])
+@pytest.mark.parametrize("dims", [16, 48, 64, 112])
+def test_layouts_of_pairs_by_two_launches(hata, dims, interleaved):
+    s = Rows(hata, 3000, dims=dims, interleaved=interleaved, m=1.3465735912322998, seed=dims)
+    assert launches(s) == 2
+    s.call()
+    s.check()
+    s.ctx.close()
+
+
+@pytest.mark.parametrize("T,Hkv,r", [(3000, 2, 128), (5000, 2, 64), (700, 8, 256), (9000, 1, 32)])
+def test_without_queries_by_two_launches(hata, T, Hkv, r):
+    import torch
+    s = Rows(hata, T, Hkv=Hkv, r=r, seed=4)
+    assert launches(s, queries=False) == 2
+    torch.cuda.synchronize()
+    s.call(queries=False, stream=torch.cuda.Stream())
+    s.check(queries=False)
+    s.ctx.close()
+
+
+@pytest.mark.parametrize("T,Hkv,r,prepared", [(3000, 2, 128, True), (3000, 2, 128, False), (5000, 2, 64, True), (600, 8, 256, True), (9000, 1, 32, True)])
+def test_one_launch_and_two_give_the_same_bits(hata, T, Hkv, r, prepared):
+    """The same rows by one call of two launches, by calls of one launch, and by hata_rotate and hata_write_slots; projections next to
+    zero among them (columns of weights that a key's first channels cancel in)."""
+    import torch
+    s = Rows(hata, T, Hkv=Hkv, r=r, seed=6, prepared=prepared)
+    # weights of few bits against keys of few values: sums that are zero, or a unit in the last place from it
+    s.W[:, :, 1::4] = np.rint(s.W[:, :, 1::4])
+    s.x[::3, s.Hq:s.Hq + Hkv, 4:] = 0
+    s.positions[::3] = 0
+    s.Wd.copy_(dev(s.W))
+    if prepared:
+        s.ctx.hata_prepare_weights(s.Wd)
+    assert launches(s) == 2 and launches(s, queries=False) == 2
+    s.call()
+    s.check()
+    results = [s.K.clone(), s.V.clone(), s.codes.clone(), s.q_out.clone()]
+    reset = lambda: (s.K.fill_(JUNK), s.V.fill_(JUNK), s.codes.fill_(77), s.q_out.fill_(JUNK))
+    same = lambda: all(torch.equal(a, b) for a, b in zip(results, (s.K, s.V, s.codes, s.q_out)))
+    reset()
+    xd, pos, slots = dev(s.x), dev(s.positions), dev(s.slots)
+    q, k, v = xd[:, :s.Hq], xd[:, s.Hq:s.Hq + Hkv], xd[:, s.Hq + Hkv:]
+    at, piece = 0, 16 * (512 // (Hkv * (-(-r // 64) + 1)))
+    while at < T:
+        n = min(piece - at % 5, T - at)
+        part, s.T = s.T, n
+        assert launches(s) == 1
+        s.T = part
+        s.ctx.hata_rotate_write_slots(q[at:], xd.stride(0), D, s.q_out[at:], k[at:], v[at:], xd.stride(0), D, pos[at:], slots[at:], n, s.rotary,
+                                      s.K, s.V, s.codes, s.P, s.n_pages, s.Wd)
+        at += n
+    torch.cuda.synchronize()
+    assert same()
+    s.call()  # once more, on top of what is there
+    assert same()
+    reset()
+    rows = torch.zeros((T, Hkv, D), dtype=torch.int16, device="cuda")
+    s.ctx.hata_rotate(k, xd.stride(0), D, Hkv, pos, T, s.rotary, False, rows, Hkv * D, D)
+    s.ctx.hata_rotate(q, xd.stride(0), D, s.Hq, pos, T, s.rotary, False, s.q_out, s.Hq * D, D)
+    s.ctx.hata_write_slots(rows, v.contiguous(), Hkv * D, D, slots, T, s.K, s.V, s.codes, s.P, s.n_pages, s.Wd)
+    torch.cuda.synchronize()
+    assert same()
+    s.ctx.close()
+
+
+def test_two_launches_captured_and_replayed(hata):
+    """A call of one launch and one of two in one graph, replayed with other rows and slots, with eager calls between."""
+    import torch
+    few, many = Rows(hata, 21, seed=10), Rows(hata, 3000, seed=11)
+    assert launches(few) == 1 and launches(many) == 2
+    side, graph = torch.cuda.Stream(), torch.cuda.CUDAGraph()
+    static = [(dev(s.x), dev(s.positions), dev(s.slots)) for s in (few, many)]
+
+    def step():
+        for s, (x, pos, slots) in zip((few, many), static):
+            q, k, v = x[:, :s.Hq], x[:, s.Hq:s.Hq + s.Hkv], x[:, s.Hq + s.Hkv:]
+            s.ctx.hata_rotate_write_slots(q, x.stride(0), D, s.q_out, k, v, x.stride(0), D, pos, slots, s.T, s.rotary, s.K, s.V, s.codes,
+                                          s.P, s.n_pages, s.Wd)
+    torch.cuda.synchronize()
+    with torch.cuda.stream(side):
+        with torch.cuda.graph(graph, stream=side):
+            step()
+    rng = np.random.default_rng(12)
+    for turn in range(5):
+        for s, (x, pos, slots) in zip((few, many), static):
+            s.x, s.positions = random_bits(rng, *s.x.shape), rng.integers(0, 9999, s.T).astype(np.int32)
+            s.slots = rng.permutation(s.n_pages * s.P)[:s.T].astype(np.int32)
+            s.slots[rng.random(s.T) < 0.2] = -1
+            x.copy_(dev(s.x)), pos.copy_(dev(s.positions)), slots.copy_(dev(s.slots))
+            for t in (s.K, s.V, s.q_out):
+                t.fill_(JUNK)
+            s.codes.fill_(77)
+        torch.cuda.synchronize()
+        step() if turn == 3 else graph.replay()
+        torch.cuda.synchronize()
+        few.check(), many.check()
+    few.ctx.close(), many.ctx.close()
