@@ -375,7 +375,8 @@ int hata_dense_decode_paged(hata_ctx* ctx, const void* q, const void* K_pool, co
  * Drafted tokens on a paged cache, and rotary positions.  A turn of a server that drafts: hata_plan_pages (len_next = len_now + drafted
  * tokens) -> hata_rotate_write_slots (drafted tokens' keys and values into their slots, rotated by the positions of their depth in the
  * tree) -> hata_dense_tree_paged -> the model's choice of a path -> hata_keep_rows (its rows moved together) -> the next turn's
- * hata_plan_pages, with the pages behind the path set back.  All of them only enqueue, and may be captured.
+ * hata_plan_pages, with the pages behind the path set back.  All of them only enqueue, and may be captured.  (Drafted tokens attend densely:
+ * hata_decode_step_paged, which selects rows by their codes, takes one query a sequence and no mask.)
  *
  * Rotary positions.  Channels come in pairs (a, b), pair i turned by t = position * freq[i]:
  *   y_a = m (x_a cos t - x_b sin t),  y_b = m (x_a sin t + x_b cos t)
@@ -436,7 +437,11 @@ int hata_rotate_write_slots(hata_ctx* ctx, const void* q, int64_t q_stride_t, in
  *                            sequence; nothing is implied, not even that it sees itself.  mask_words >= max_draft / 32.  NULL: j <= i
  *                            (a chain; a chunk of a prompt).  Drafted rows from max_draft on are seen by nobody
  * A token that sees no row, or only rows whose scores are -inf, gives zeros.  A row that a token does not see has no effect on it,
- * whatever is in the row (NaN, infinities).  out 16-byte aligned, out_f32 NULL or 16-byte aligned.  n_tokens * Hq < 2^24.
+ * whatever is in the row (NaN, infinities).  Scores, sums and references are fp32.  Softmax weights are two bf16 terms (16 bits) for any
+ * number of heads, as of shared rows in hata_dense_decode_paged: out_f32 is 3e-6 to 5e-6 off (2-norm), where that call's fp32 weights, with the numbers
+ * of heads named there, are 2e-7 off; out, rounded to bf16 (1.6e-3), is as near to 64 bits with either.  Weights below 2^-70 of the largest one, and
+ * values below 2^-70, may count as zero, and where a value of a committed row is infinite the output may be NaN.  out has the same bits
+ * with and without out_f32.  out 16-byte aligned, out_f32 NULL or 16-byte aligned.  n_tokens * Hq < 2^24.
  * scratch: device memory of the caller, 256-byte aligned, of hata_tree_scratch_bytes for the same numbers or larger ones (9 MB where
  * max_draft * Hq / Hkv <= 32, else 68 MB); it carries nothing from one call to the next, and calls that may overlap need one each.  (It is
  * not part of the context's workspace: contexts that never draft do not pay for it.)  No residency needed, no in-kernel waits. */

@@ -8,6 +8,11 @@
 // heads, G = 4, us with 1, 8, 16, 32 and 64 tokens each: 171, 170, 196, 295 and 491 (the rows alone, at 6.1 TB/s: 176).  A token
 // and head at a time (the first form) 22400 us for what takes 252 here: 16 sequences of up to 16384 rows, the last up to 33 of them
 // drafted, eight KV heads, G = 8.
+// Why two terms: they leave the fp32 output 3e-6 to 5e-6 off (2-norm; normally distributed values, 300 to 32768 rows, any G; 3e-7 to 1.7e-6 with
+// weights in fp32), which the bf16 output, rounded by 1.6e-3, does not show: with scores of tens, as outlier channels make them, 2 sequences of
+// 131072 rows and 48 tokens are 1.60513e-3 off with either, 32 of 8192 rows and 64 tokens 1.53323e-3; 0.2 to 0.3 % of the values differ by
+// a rounding, and in 42 to 50 % of those this one is the nearer.  (The fp32 outputs are 2.2e-6 and 1.9e-6 off there, and 2.7e-6 and 1.8e-6 with weights in
+// fp32: the scores' own roundings.)  A third term would be a third more to multiply.
 #include <algorithm>
 #include "hata_attn_core.h"
 #include "hata_device.h"
